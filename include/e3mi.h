@@ -355,6 +355,86 @@ e3_status e3_tpg_fwd_f64(e3_tpg* tpg, const double* x, const double* y, double* 
 e3_status e3_tpg_bwd_f64(e3_tpg* tpg, const double* x, const double* y, const double* dz, double* dx, double* dy,
                          void* ws, size_t ws_bytes, int64_t rows, int C, e3_stream stream);
 
+/* Invariant layers.  The networks around the convolution that see scalars only
+ * -- the radial network that turns each edge's basis into its weights s (or the
+ * h of the fused radial weights), the readout of scalar channels -- are stacks
+ * of dense layers and layer norms.  Both run forward and backward here, in
+ * float32 or bfloat16, with their saved activations in full or in 8 bits.
+ *
+ * Rows.  Matrices are rows of contiguous elements, row i at p + i ld elements
+ * (ld at least the width: slices of wider tensors, such as the scalar channels
+ * of node features, are rows too); W, dW and vectors are contiguous.  Pointers
+ * need the alignment of an element.  Widths are 1 to 2^20, rows 0 to 2^40.
+ * All tensors of a call have its dtype but mean and rstd, which are float32;
+ * every sum, statistic and activation is computed in float32 (the products of
+ * bfloat16 operands on the matrix cores with float32 sums) and rounded once
+ * when it is stored, but for the dz of a bfloat16 dense backward, which is
+ * rounded to bfloat16 before the products.
+ * Outputs may not overlap inputs, but y may be r itself (same ld). */
+typedef enum { E3_F32 = 0, E3_BF16 = 1 } e3_dtype;
+typedef enum {
+  E3_ACT_NONE = 0,
+  E3_ACT_RELU = 1, /* derivative 0 at 0 */
+  E3_ACT_SILU = 2, /* z / (1 + exp(-z)) */
+  E3_ACT_GELU = 3  /* z Phi(z), Phi the normal distribution's */
+} e3_act;
+
+/* 8-bit checkpoints: q [rows, cols] int8 and c [rows, ceil(cols / 32)], both
+ * contiguous.  Groups of 32 values along a row share the step 2^(c - 127) and
+ * are q 2^(c - 127) with q in [-127, 127]: c - 127 = floor(log2 max|x|) - 6, one
+ * more where the largest would round past 127, at least -127 and at most 121
+ * (from 127.5 2^121 = 3.39e38 on, values read as 127 2^121); q is to nearest,
+ * ties to even.  A value is off by at most half a step, 1/127 of its group's
+ * largest.  A group with an infinity or a NaN has c = 255 and reads as
+ * NaN.  The values are exact in float32 and bfloat16 (8 bits and a power of
+ * two).  float32: 1.03 of 4 bytes per value.
+ * Wherever a call below takes an activation as x or z, it takes xq, xc or zq,
+ * zc instead (the other pointer NULL), and unpacks them on the way to the
+ * registers. */
+e3_status e3_pack8(e3_dtype dtype, const void* x, int64_t ldx, int8_t* q, uint8_t* c, int64_t rows, int64_t cols,
+                   e3_stream stream);
+e3_status e3_unpack8(e3_dtype dtype, const int8_t* q, const uint8_t* c, void* x, int64_t ldx, int64_t rows,
+                     int64_t cols, e3_stream stream);
+
+/* Layer norm over the columns of each row:
+ *   y = (x - mean) rstd gamma + beta,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ * gamma, beta [cols] (NULL: 1, 0); eps >= 0.  Optional outputs (NULL: not
+ * stored): mean, rstd [rows] float32, which the backward takes; xq, xc: x in 8
+ * bits; yq, yc: y as stored, in 8 bits. */
+e3_status e3_layer_norm_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* gamma, const void* beta, float eps,
+                            void* y, int64_t ldy, float* mean, float* rstd, int8_t* xq, uint8_t* xc, int8_t* yq,
+                            uint8_t* yc, int64_t rows, int64_t cols, e3_stream stream);
+/* dx [rows, cols], dgamma, dbeta [cols] (each may be NULL) from dy and the
+ * forward's x (or xq, xc), mean and rstd.  dgamma and dbeta sum over the rows in
+ * a fixed order through ws (at least e3_layer_norm_workspace_size bytes; not
+ * needed without them); they are zero for rows = 0. */
+e3_status e3_layer_norm_workspace_size(e3_dtype dtype, int64_t rows, int64_t cols, size_t* bwd_bytes);
+e3_status e3_layer_norm_bwd(e3_dtype dtype, const void* x, int64_t ldx, const int8_t* xq, const uint8_t* xc,
+                            const void* gamma, const void* dy, int64_t lddy, const float* mean, const float* rstd,
+                            void* dx, int64_t lddx, void* dgamma, void* dbeta, void* ws, size_t ws_bytes, int64_t rows,
+                            int64_t cols, e3_stream stream);
+
+/* Dense layer: z = x W + bias, y = act(z) + r, with x [M, K], W [K, N], bias [N]
+ * and r [M, N] (NULL: none).  Optional outputs (NULL: not stored), for the
+ * backward and for the layer that reads y: z [M, N]; zq, zc: z in 8 bits, from
+ * its float32 values; yq, yc: y as stored, in 8 bits.
+ * ws: at least fwd_bytes of e3_dense_workspace_size (partial sums where a few
+ * rows split the reduction; 0 for most sizes). */
+e3_status e3_dense_workspace_size(e3_dtype dtype, int64_t M, int64_t K, int64_t N, size_t* fwd_bytes,
+                                  size_t* bwd_bytes);
+e3_status e3_dense_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* W, const void* bias, const void* r,
+                       int64_t ldr, e3_act act, void* y, int64_t ldy, void* z, int64_t ldz, int8_t* zq, uint8_t* zc,
+                       int8_t* yq, uint8_t* yc, void* ws, size_t ws_bytes, int64_t M, int64_t K, int64_t N,
+                       e3_stream stream);
+/* With dz = dy act'(z): dx = dz W^T, dW = x^T dz, db = the column sums of dz
+ * (each may be NULL; r's cotangent is dy itself).  x (for dW) and z (but for
+ * E3_ACT_NONE) in full or packed.  dW and db sum over the rows in a fixed order.
+ * M = 0 gives dW = 0 and db = 0.  ws: bwd_bytes, 16-byte aligned. */
+e3_status e3_dense_bwd(e3_dtype dtype, const void* x, int64_t ldx, const int8_t* xq, const uint8_t* xc, const void* W,
+                       const void* z, int64_t ldz, const int8_t* zq, const uint8_t* zc, e3_act act, const void* dy,
+                       int64_t lddy, void* dx, int64_t lddx, void* dW, void* db, void* ws, size_t ws_bytes, int64_t M,
+                       int64_t K, int64_t N, e3_stream stream);
+
 /* Per-kernel timing (instrumentation).  While enabled, every kernel the
  * library launches is bracketed by two HIP events on the caller's stream.
  * e3_timing_read waits for the recorded events and returns, per kernel name

@@ -22,6 +22,8 @@ Everything here is the plain definition, written out in float64:
 * ``conv``    -- the message-passing convolution, eq.
   (message_passing_convolution), and its cotangents, eq. (conv-bwd).
 * ``graph``   -- receiver/sender CSR by a stable argsort.
+* ``layers``  -- the invariant layers (dense, layer norm) with their gradients,
+  and the 8-bit checkpoint format.
 
 Every function says which passage it follows.  Where the paper leaves a
 convention open (normalisation, real-basis phase, axes, path order) the

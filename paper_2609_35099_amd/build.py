@@ -8,8 +8,9 @@
    and their table.
 2. hipcc compiles the core unit (csrc/e3mi.hip: C ABI, graph, linear mixing,
    record tensor product, probes), the record convolution (csrc/convr.hip:
-   layouts without a compiled unit), every layout unit and the builder for
-   gfx950, in parallel, and links libe3mi.so next to this file.
+   layouts without a compiled unit), the invariant layers (csrc/dense.hip,
+   csrc/norm.hip), every layout unit and the builder for gfx950, in parallel,
+   and links libe3mi.so next to this file.
 
 Layouts beyond the defaults compiled into the generator (the benchmark and
 test layouts, natural-parity versions and one reordered block list) are
@@ -93,6 +94,7 @@ def build(verbose: bool = True, extra=None) -> str:
     objdir = os.path.join(BUILD, "obj")
     os.makedirs(objdir, exist_ok=True)
     sources = [os.path.join(CSRC, "e3mi.hip"), os.path.join(CSRC, "convr.hip"),
+               os.path.join(CSRC, "dense.hip"), os.path.join(CSRC, "norm.hip"),
                os.path.join(CSRC, "builder.cpp")] + \
               [os.path.join(GEN, u) for u in units]
     objs = []

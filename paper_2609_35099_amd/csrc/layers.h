@@ -1,0 +1,283 @@
+// Shared by the invariant layers (dense.hip, norm.hip): element types, row
+// access, activations and the 8-bit checkpoint format.
+#pragma once
+#include "e3mi_impl.h"
+
+namespace {
+
+typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
+typedef unsigned u2v __attribute__((ext_vector_type(2)));
+typedef unsigned u4v __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------ element types
+// A lane's piece of a row is 16 bytes: V values of the type.  Rows start at
+// any element (odd widths, slices of wider tensors), so the vector types claim
+// an element's alignment only; the loads are 16-byte instructions either way.
+template <class T>
+struct Elem;
+template <>
+struct Elem<float> {
+  static constexpr int V = 4;
+  typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+  static __device__ __forceinline__ void get(vec u, float (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = u[i];
+  }
+  static __device__ __forceinline__ vec put(const float (&v)[4]) { return vec{v[0], v[1], v[2], v[3]}; }
+  static __device__ __forceinline__ float one(float u) { return u; }
+  static __device__ __forceinline__ float round(float v) { return v; }
+};
+template <>
+struct Elem<__bf16> {
+  static constexpr int V = 8;
+  typedef unsigned vec __attribute__((ext_vector_type(4), aligned(2)));
+  static __device__ __forceinline__ void get(vec u, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(u[i] << 16);
+      v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ vec put(const float (&v)[8]) {
+    vec u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      u[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(f2v{v[2 * i], v[2 * i + 1]}, bf2v));
+    return u;
+  }
+  static __device__ __forceinline__ float one(__bf16 u) { return (float)u; }
+  static __device__ __forceinline__ float round(float v) { return (float)(__bf16)v; }
+};
+
+// The values at p (n of them inside the row; the rest read as zero).
+template <class T>
+__device__ __forceinline__ void ld_piece(const T* p, int n, float (&v)[Elem<T>::V]) {
+  if (n >= Elem<T>::V) {
+    Elem<T>::get(*reinterpret_cast<const typename Elem<T>::vec*>(p), v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < Elem<T>::V; ++i) v[i] = i < n ? Elem<T>::one(p[i]) : 0.0f;
+  }
+}
+template <class T>
+__device__ __forceinline__ void st_piece(T* p, int n, const float (&v)[Elem<T>::V]) {
+  if (n >= Elem<T>::V) {
+    *reinterpret_cast<typename Elem<T>::vec*>(p) = Elem<T>::put(v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < Elem<T>::V; ++i)
+      if (i < n) p[i] = (T)v[i];
+  }
+}
+
+// ------------------------------------------------------------ sums over lanes
+// Over aligned groups of L lanes (a power of two up to 64); every lane of a
+// group ends with the same bits.  All lanes of the group take part.
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp_u(unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+template <int L, class F>
+__device__ __forceinline__ unsigned fold_lanes(unsigned v, F&& f) {
+  if constexpr (L >= 2) v = f(v, dpp_u<0xb1>(v));   // quad_perm [1, 0, 3, 2]
+  if constexpr (L >= 4) v = f(v, dpp_u<0x4e>(v));   // quad_perm [2, 3, 0, 1]
+  if constexpr (L >= 8) v = f(v, dpp_u<0x141>(v));  // row_half_mirror
+  if constexpr (L >= 16) v = f(v, dpp_u<0x140>(v)); // row_mirror
+  if constexpr (L >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f(r[0], r[1]);
+  }
+  if constexpr (L >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = f(r[0], r[1]);
+  }
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float sum_lanes(float v) {
+  return __uint_as_float(fold_lanes<L>(__float_as_uint(v), [](unsigned a, unsigned b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+template <int L>
+__device__ __forceinline__ unsigned max_lanes(unsigned v) {
+  return fold_lanes<L>(v, [](unsigned a, unsigned b) { return a > b ? a : b; });
+}
+
+// ------------------------------------------------------------ 8-bit checkpoints
+// Groups of 32 values along a row share the power of two 2^(c - 127) and hold
+// integers q of [-127, 127].  c - 127 = floor(log2 max|x|) - 6, one more where
+// the largest would round past 127, at least -127; q = x 2^(127 - c) to
+// nearest, ties to even.  The product by a power of two is exact, so a value is
+// off by at most half a step.  The step stays at 2^121 at the range's end, where
+// 64 of the next would be infinite: values from 127.5 of it on read as 127.  An
+// infinity or a NaN in the group makes all of it NaN (c = 255, q = 0).
+constexpr int kGroup = 32;
+
+__device__ __forceinline__ float step8(unsigned c) {
+  return __uint_as_float(c == 255u ? 0x7fc00000u : c == 0u ? 0x00400000u : c << 23);
+}
+// The group's exponent byte from its largest magnitude's bits (NaN above all).
+__device__ __forceinline__ unsigned exp8(unsigned top) {
+  if (top >= 0x7f800000u) return 255u;
+  const int e = (int)((top + 0x10000u) >> 23) - 6;  // 1.1111111 and more in binary carries
+  return e < 0 ? 0u : e > 248 ? 248u : (unsigned)e;
+}
+template <int V>
+struct Bytes;
+template <>
+struct Bytes<4> {
+  typedef unsigned vec __attribute__((aligned(1)));
+};
+template <>
+struct Bytes<8> {
+  typedef u2v vec __attribute__((aligned(1)));
+};
+
+// Packs a lane's V values at column col of a row (n of them inside it); the
+// 32 / V lanes of a group hold consecutive pieces and all take part.  q and c
+// point at the row.
+template <int V>
+__device__ __forceinline__ void pack8_piece(const float (&v)[V], int col, int n, int8_t* q, uint8_t* c) {
+  unsigned top = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const unsigned b = i < n ? __float_as_uint(v[i]) & 0x7fffffffu : 0u;
+    top = b > top ? b : top;
+  }
+  top = max_lanes<kGroup / V>(top);
+  if (n <= 0) return;
+  const unsigned e = exp8(top);
+  const float up = e == 255u ? 0.0f : __uint_as_float((254u - e) << 23);
+  unsigned w[V / 4];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int k = e == 255u ? 0 : (int)fminf(fmaxf(rintf(v[i] * up), -127.0f), 127.0f);
+    if (i % 4 == 0) w[i / 4] = 0;
+    w[i / 4] |= ((unsigned)k & 0xffu) << (8 * (i % 4));
+  }
+  if (n >= V) {
+    if constexpr (V == 4) *reinterpret_cast<typename Bytes<4>::vec*>(q + col) = w[0];
+    else *reinterpret_cast<typename Bytes<8>::vec*>(q + col) = u2v{w[0], w[1]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < n) q[col + i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+  }
+  if (col % kGroup == 0) c[col / kGroup] = (uint8_t)e;
+}
+
+// V packed values at column col (n inside the row; the rest read as zero).
+template <int V>
+__device__ __forceinline__ void unpack8_piece(const int8_t* q, const uint8_t* c, int col, int n, float (&v)[V]) {
+  if (n <= 0) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 0.0f;
+    return;
+  }
+  const float s = step8(c[col / kGroup]);
+  unsigned w[V / 4];
+  if (n >= V) {
+    if constexpr (V == 4) {
+      w[0] = *reinterpret_cast<const typename Bytes<4>::vec*>(q + col);
+    } else {
+      const u2v t = *reinterpret_cast<const typename Bytes<8>::vec*>(q + col);
+      w[0] = t.x, w[1] = t.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (i % 4 == 0) w[i / 4] = 0;
+      if (i < n) w[i / 4] |= ((unsigned)(uint8_t)q[col + i]) << (8 * (i % 4));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = i < n ? (float)(int)(int8_t)(w[i / 4] >> (8 * (i % 4))) * s : 0.0f;
+}
+
+// Values of a row that is kept in full or packed (x null).
+template <class T>
+struct RowsIn {
+  const T* x;
+  int64_t ld;
+  const int8_t* q;
+  const uint8_t* c;
+  __device__ __forceinline__ void load(int64_t row, int col, int cols, float (&v)[Elem<T>::V]) const {
+    const int n = cols - col;
+    if (x) {
+      ld_piece<T>(x + row * ld + col, n, v);
+    } else {
+      unpack8_piece<Elem<T>::V>(q + row * cols, c + row * ((cols + kGroup - 1) / kGroup), col, n, v);
+    }
+  }
+};
+
+// ------------------------------------------------------------ activations
+// gelu is z Phi(z) with the normal distribution's Phi.
+__device__ __forceinline__ float act_of(int act, float z) {
+  if (act == E3_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+  if (act == E3_ACT_SILU) return z / (1.0f + expf(-z));
+  if (act == E3_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+  return z;
+}
+__device__ __forceinline__ float act_grad(int act, float z) {
+  if (act == E3_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+  if (act == E3_ACT_SILU) {
+    const float s = 1.0f / (1.0f + expf(-z));
+    return s * (1.0f + z * (1.0f - s));
+  }
+  if (act == E3_ACT_GELU)
+    return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+  return 1.0f;
+}
+
+// ------------------------------------------------------------ column sums
+// out_s[col] = sum over p of part[p][s][col], s = 0, 1 (either output may be
+// null), in a fixed order: 16 threads of a column take every 16th partial, then
+// their sums are added in order.
+template <class T>
+__global__ __launch_bounds__(256) void k_column_sums(const float* part, int parts, int sets, int cols, T* out0,
+                                                     T* out1) {
+  __shared__ float s[16][17];
+  const int c = threadIdx.x % 16, p0 = threadIdx.x / 16, col = (int)blockIdx.x * 16 + c, set = blockIdx.y;
+  T* out = set ? out1 : out0;
+  if (!out) return;
+  float v = 0.0f;
+  if (col < cols)
+    for (int p = p0; p < parts; p += 16) v += part[((int64_t)p * sets + set) * cols + col];
+  s[p0][c] = v;
+  __syncthreads();
+  if (p0 != 0 || col >= cols) return;
+  v = 0.0f;
+#pragma unroll
+  for (int p = 0; p < 16; ++p) v += s[p][c];
+  out[col] = (T)v;
+}
+
+inline e3_status column_sums(e3_dtype dtype, const float* part, int parts, int sets, int cols, void* out0, void* out1,
+                             hipStream_t st) {
+  TimedLaunch t_("column_sums", st);
+  const dim3 grid((cols + 15) / 16, sets);
+  if (dtype == E3_F32)
+    hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(256), 0, st, part, parts, sets, cols,
+                       static_cast<float*>(out0), static_cast<float*>(out1));
+  else
+    hipLaunchKernelGGL(k_column_sums<__bf16>, grid, dim3(256), 0, st, part, parts, sets, cols,
+                       static_cast<__bf16*>(out0), static_cast<__bf16*>(out1));
+  E3_HIP(hipGetLastError());
+  return E3_OK;
+}
+
+// ------------------------------------------------------------ argument checks
+constexpr int64_t kMaxCols = 1 << 20;               // widths; a row's offsets stay in 32 bits
+constexpr int64_t kMaxRows = (int64_t)1 << 40;
+inline bool good_dtype(e3_dtype t) { return t == E3_F32 || t == E3_BF16; }
+inline bool good_rows(e3_dtype t, int64_t rows, int64_t cols) {
+  return good_dtype(t) && rows >= 0 && rows <= kMaxRows && cols >= 1 && cols <= kMaxCols;
+}
+inline bool misaligned(e3_dtype t, const void* p) {
+  return reinterpret_cast<uintptr_t>(p) & (t == E3_F32 ? 3u : 1u);
+}
+inline bool good_ptr(e3_dtype t, const void* p) { return p && !misaligned(t, p); }
+
+}  // namespace

@@ -89,6 +89,17 @@ SIGNATURES = {
     "e3_conv_workspace_size_f64": (_I, [_P, _P, ct.POINTER(ct.c_size_t)]),
     "e3_conv_fwd_f64": (_I, [_P, _P, _P, _P, _P, _P, _P]),
     "e3_conv_bwd_f64": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, ct.c_size_t, _P]),
+    "e3_pack8": (_I, [_I, _P, _I64, _P, _P, _I64, _I64, _P]),
+    "e3_unpack8": (_I, [_I, _P, _P, _P, _I64, _I64, _I64, _P]),
+    "e3_layer_norm_fwd": (_I, [_I, _P, _I64, _P, _P, ct.c_float, _P, _I64, _P, _P, _P, _P, _P, _P, _I64, _I64, _P]),
+    "e3_layer_norm_workspace_size": (_I, [_I, _I64, _I64, ct.POINTER(ct.c_size_t)]),
+    "e3_layer_norm_bwd": (_I, [_I, _P, _I64, _P, _P, _P, _P, _I64, _P, _P, _P, _I64, _P, _P, _P, ct.c_size_t, _I64,
+                               _I64, _P]),
+    "e3_dense_workspace_size": (_I, [_I, _I64, _I64, _I64, ct.POINTER(ct.c_size_t), ct.POINTER(ct.c_size_t)]),
+    "e3_dense_fwd": (_I, [_I, _P, _I64, _P, _P, _P, _I64, _I, _P, _I64, _P, _I64, _P, _P, _P, _P, _P, ct.c_size_t,
+                          _I64, _I64, _I64, _P]),
+    "e3_dense_bwd": (_I, [_I, _P, _I64, _P, _P, _P, _P, _I64, _P, _P, _I, _P, _I64, _P, _I64, _P, _P, _P, ct.c_size_t,
+                          _I64, _I64, _I64, _P]),
     "e3_probe_stream": (_I, [_P, ct.c_size_t, _P, ct.c_size_t, _I, _I, _I, _U, ct.POINTER(ct.c_size_t),
                              ct.POINTER(ct.c_size_t), _P]),
     "e3_timing_enable": (_I, [_I]),
@@ -128,7 +139,8 @@ def _torch():
     global _modules
     if _modules is None:
         import torch
-        _modules = torch, {"float32": torch.float32, "float64": torch.float64, "int32": torch.int32}
+        _modules = torch, {"float32": torch.float32, "float64": torch.float64, "int32": torch.int32,
+                           "bfloat16": torch.bfloat16, "int8": torch.int8, "uint8": torch.uint8}
     return _modules[0]
 
 
@@ -664,6 +676,269 @@ def conv_bwd_radial(plan: Plan, graph: Graph, x, vec, h, W, dm, dx=None, dvec=No
                                     _ptr(dW, "dW", (K, plan.P, plan.C)), ws.data_ptr(), ws.numel(),
                                     _stream(stream)), "e3_conv_bwd_radial")
     return dx, dvec, dh, dW
+
+
+# ---------------------------------------------------------------- invariant layers
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+_LAYER_DTYPES = {}   # torch dtype -> (e3_dtype, its name)
+
+
+def _layer_dtype(t, name):
+    torch = _torch()
+    if not _LAYER_DTYPES:
+        _LAYER_DTYPES.update({torch.float32: (0, "float32"), torch.bfloat16: (1, "bfloat16")})
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    got = _LAYER_DTYPES.get(t.dtype)
+    if got is None:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    return got
+
+
+def _rows(t, name, shape, dtype):
+    """(pointer, row stride) of a matrix whose rows are contiguous; rows may be strided."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype is not _modules[1][dtype]:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    m, n = shape
+    if m == 0:
+        return None, n
+    ld, one = t.stride()
+    if n > 1 and one != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if m == 1:
+        ld = n
+    elif ld < n:
+        raise ValueError(f"{name} has overlapping rows")
+    return t.data_ptr(), ld
+
+
+class Packed8:
+    """A matrix kept in 8 bits: q [rows, cols] int8 times the step 2^(c - 127) of each group of
+    32 columns, c [rows, ceil(cols / 32)] uint8 (255: the group is NaN)."""
+
+    __slots__ = ("q", "c")
+
+    def __init__(self, q, c):
+        torch = _torch()
+        for t, name, dt in ((q, "q", torch.int8), (c, "c", torch.uint8)):
+            if not isinstance(t, torch.Tensor) or t.dtype is not dt or t.dim() != 2:
+                raise TypeError(f"{name} must be a {dt} matrix")
+        if c.shape[0] != q.shape[0] or c.shape[1] != (q.shape[1] + 31) // 32:
+            raise ValueError(f"c has shape {tuple(c.shape)}, expected {(q.shape[0], (q.shape[1] + 31) // 32)}")
+        self.q, self.c = q, c
+
+    @property
+    def shape(self):
+        return self.q.shape
+
+    @classmethod
+    def empty(cls, rows: int, cols: int) -> "Packed8":
+        torch = _torch()
+        p = cls.__new__(cls)
+        p.q = torch.empty((rows, cols), dtype=torch.int8, device="cuda")
+        p.c = torch.empty((rows, (cols + 31) // 32), dtype=torch.uint8, device="cuda")
+        return p
+
+
+def _packed(p, name, shape):
+    """Pointers of a Packed8 of the given shape."""
+    if not isinstance(p, Packed8):
+        raise TypeError(f"{name} must be a Packed8")
+    m, n = shape
+    return _ptr(p.q, name + ".q", (m, n), "int8"), _ptr(p.c, name + ".c", (m, (n + 31) // 32), "uint8")
+
+
+def _kept(t, name, shape, dtype):
+    """(pointer, row stride, q, c) of an activation in full or packed."""
+    if isinstance(t, Packed8):
+        return (None, 0, *_packed(t, name, shape))
+    return (*_rows(t, name, shape, dtype), None, None)
+
+
+def _matrix(t, name):
+    if len(t.shape) != 2:
+        raise ValueError(f"{name} must be a matrix, got shape {tuple(t.shape)}")
+    return t.shape
+
+
+@_on_stream
+def pack8(x, out=None, stream=None) -> Packed8:
+    """x [rows, cols] (float32 or bfloat16) in 8 bits."""
+    code, dt = _layer_dtype(x, "x")
+    m, n = _matrix(x, "x")
+    out = Packed8.empty(m, n) if out is None else out
+    _check(lib().e3_pack8(code, *_rows(x, "x", (m, n), dt), *_packed(out, "out", (m, n)), m, n, _stream(stream)),
+           "e3_pack8")
+    return out
+
+
+@_on_stream
+def unpack8(p: Packed8, dtype=None, out=None, stream=None):
+    """The values of p, in float32 (or dtype; or in the type of out)."""
+    torch = _torch()
+    if not isinstance(p, Packed8):
+        raise TypeError("p must be a Packed8")
+    m, n = p.shape
+    if out is None:
+        out = torch.empty((m, n), dtype=dtype or torch.float32, device="cuda")
+    code, dt = _layer_dtype(out, "out")
+    _check(lib().e3_unpack8(code, *_packed(p, "p", (m, n)), *_rows(out, "out", (m, n), dt), m, n, _stream(stream)),
+           "e3_unpack8")
+    return out
+
+
+def _keep_of(keep, allowed):
+    for k in keep:
+        if k not in allowed:
+            raise ValueError(f"keep: {k!r} is none of {', '.join(allowed)}")
+    return keep
+
+
+@_on_stream
+def layer_norm_fwd(x, gamma=None, beta=None, eps: float = 1e-5, keep=(), out=None, stream=None):
+    """y = (x - mean) / sqrt(var + eps) gamma + beta over the columns of each row of x [rows, cols].
+
+    keep adds to the result, in this order: "stats" (mean, rstd [rows], float32), "x8" (x as a
+    Packed8), "y8" (y as a Packed8).
+    """
+    code, dt = _layer_dtype(x, "x")
+    m, n = shape = _matrix(x, "x")
+    _keep_of(keep, ("stats", "x8", "y8"))
+    torch = _torch()
+    y = torch.empty((m, n), dtype=x.dtype, device="cuda") if out is None else out
+    got, mean, rstd, xp, yp = [y], None, None, (None, None), (None, None)
+    if "stats" in keep:
+        mean, rstd = _empty((m,)), _empty((m,))
+        got += [mean, rstd]
+        mean, rstd = _ptr(mean, "mean"), _ptr(rstd, "rstd")
+    if "x8" in keep:
+        got.append(Packed8.empty(m, n))
+        xp = _packed(got[-1], "x8", shape)
+    if "y8" in keep:
+        got.append(Packed8.empty(m, n))
+        yp = _packed(got[-1], "y8", shape)
+    _check(lib().e3_layer_norm_fwd(code, *_rows(x, "x", shape, dt),
+                                   None if gamma is None else _ptr(gamma, "gamma", (n,), dt),
+                                   None if beta is None else _ptr(beta, "beta", (n,), dt), eps,
+                                   *_rows(y, "out", shape, dt), mean, rstd, *xp, *yp, m, n, _stream(stream)),
+           "e3_layer_norm_fwd")
+    return tuple(got) if keep else y
+
+
+def layer_norm_workspace_size(rows: int, cols: int, dtype="float32") -> int:
+    b = ct.c_size_t()
+    _check(lib().e3_layer_norm_workspace_size({"float32": 0, "bfloat16": 1}[dtype], rows, cols, ct.byref(b)),
+           "e3_layer_norm_workspace_size")
+    return b.value
+
+
+@_on_stream
+def layer_norm_bwd(x, gamma, dy, mean, rstd, want=("dx", "dgamma", "dbeta"), dx=None, ws=None, stream=None):
+    """(dx, dgamma, dbeta) from dy, the forward's x (a tensor or a Packed8) and its statistics;
+    cotangents not in `want` are not computed (None).  gamma may be None (ones)."""
+    code, dt = _layer_dtype(dy, "dy")
+    m, n = shape = _matrix(dy, "dy")
+    _keep_of(want, ("dx", "dgamma", "dbeta"))
+    torch = _torch()
+    if "dx" in want and dx is None:
+        dx = torch.empty((m, n), dtype=dy.dtype, device="cuda")
+    dg = torch.empty((n,), dtype=dy.dtype, device="cuda") if "dgamma" in want else None
+    db = torch.empty((n,), dtype=dy.dtype, device="cuda") if "dbeta" in want else None
+    if ws is None and (dg is not None or db is not None):
+        ws = workspace(layer_norm_workspace_size(m, n, dt))
+    xp, ldx, xq, xc = _kept(x, "x", shape, dt)
+    _check(lib().e3_layer_norm_bwd(code, xp, ldx, xq, xc, None if gamma is None else _ptr(gamma, "gamma", (n,), dt),
+                                   *_rows(dy, "dy", shape, dt), _ptr(mean, "mean", (m,)), _ptr(rstd, "rstd", (m,)),
+                                   *((None, n) if dx is None else _rows(dx, "dx", shape, dt)),
+                                   None if dg is None else dg.data_ptr(), None if db is None else db.data_ptr(),
+                                   None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), m, n,
+                                   _stream(stream)), "e3_layer_norm_bwd")
+    return dx, dg, db
+
+
+def dense_workspace_size(M: int, K: int, N: int, dtype="float32"):
+    """Bytes of (forward, backward)."""
+    f, b = ct.c_size_t(), ct.c_size_t()
+    _check(lib().e3_dense_workspace_size({"float32": 0, "bfloat16": 1}[dtype], M, K, N, ct.byref(f), ct.byref(b)),
+           "e3_dense_workspace_size")
+    return f.value, b.value
+
+
+def _act_code(act):
+    code = ACTIVATIONS.get(act)
+    if code is None:
+        raise ValueError(f"act: {act!r} is none of {', '.join(ACTIVATIONS)}")
+    return code
+
+
+@_on_stream
+def dense_fwd(x, W, bias=None, res=None, act: str = "none", keep=(), out=None, ws=None, stream=None):
+    """y = act(x W + bias) + res, with x [M, K], W [K, N], bias [N], res [M, N].
+
+    keep adds to the result, in this order: "z" (z = x W + bias [M, N]), "z8" (z as a Packed8),
+    "y8" (y as a Packed8).
+    """
+    code, dt = _layer_dtype(x, "x")
+    M, K = _matrix(x, "x")
+    if _matrix(W, "W")[0] != K:
+        raise ValueError(f"W has shape {tuple(W.shape)}, expected {K} rows")
+    N = W.shape[1]
+    _keep_of(keep, ("z", "z8", "y8"))
+    torch = _torch()
+    shape = (M, N)
+    y = torch.empty(shape, dtype=x.dtype, device="cuda") if out is None else out
+    got, z, zp, yp = [y], None, (None, None), (None, None)
+    if "z" in keep:
+        got.append(torch.empty(shape, dtype=x.dtype, device="cuda"))
+        z = got[-1].data_ptr()
+    if "z8" in keep:
+        got.append(Packed8.empty(M, N))
+        zp = _packed(got[-1], "z8", shape)
+    if "y8" in keep:
+        got.append(Packed8.empty(M, N))
+        yp = _packed(got[-1], "y8", shape)
+    if ws is None:
+        nb = dense_workspace_size(M, K, N, dt)[0]
+        ws = workspace(nb) if nb else None
+    _check(lib().e3_dense_fwd(code, *_rows(x, "x", (M, K), dt), _ptr(W, "W", (K, N), dt),
+                              None if bias is None else _ptr(bias, "bias", (N,), dt),
+                              *((None, N) if res is None else _rows(res, "res", shape, dt)), _act_code(act),
+                              *_rows(y, "out", shape, dt), z, N, *zp, *yp, None if ws is None else ws.data_ptr(),
+                              0 if ws is None else ws.numel(), M, K, N, _stream(stream)), "e3_dense_fwd")
+    return tuple(got) if keep else y
+
+
+@_on_stream
+def dense_bwd(x, W, dy, z=None, act: str = "none", want=("dx", "dW", "db"), dx=None, ws=None, stream=None):
+    """(dx, dW, db) of a dense layer from dy and the forward's x and z, each a tensor or a Packed8 (z may be
+    None for act "none"); cotangents not in `want` are not computed (None).  The residual's cotangent is dy."""
+    code, dt = _layer_dtype(dy, "dy")
+    M, N = shape = _matrix(dy, "dy")
+    if _matrix(W, "W")[1] != N:
+        raise ValueError(f"W has shape {tuple(W.shape)}, expected {N} columns")
+    K = W.shape[0]
+    _keep_of(want, ("dx", "dW", "db"))
+    torch = _torch()
+    if "dx" in want and dx is None:
+        dx = torch.empty((M, K), dtype=dy.dtype, device="cuda")
+    dW = torch.empty((K, N), dtype=dy.dtype, device="cuda") if "dW" in want else None
+    db = torch.empty((N,), dtype=dy.dtype, device="cuda") if "db" in want else None
+    if ws is None:
+        ws = workspace(dense_workspace_size(M, K, N, dt)[1])
+    xp, ldx, xq, xc = (None, K, None, None) if x is None else _kept(x, "x", (M, K), dt)
+    zp, ldz, zq, zc = (None, N, None, None) if z is None else _kept(z, "z", shape, dt)
+    _check(lib().e3_dense_bwd(code, xp, ldx, xq, xc, _ptr(W, "W", (K, N), dt), zp, ldz, zq, zc, _act_code(act),
+                              *_rows(dy, "dy", shape, dt), *((None, K) if dx is None else _rows(dx, "dx", (M, K), dt)),
+                              None if dW is None else dW.data_ptr(), None if db is None else db.data_ptr(),
+                              ws.data_ptr(), ws.numel(), M, K, N, _stream(stream)), "e3_dense_bwd")
+    return dx, dW, db
 
 
 # ---------------------------------------------------------------- instrumentation

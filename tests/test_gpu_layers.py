@@ -1,0 +1,524 @@
+"""Dense layers, layer norm and 8-bit checkpoints against the float64 oracle.
+
+Bars (relative L2 per output):
+  float32   2e-6.  A sum of up to 9,000 products errs by about sqrt(n) / 3 roundings of 6e-8 of its
+            size if added one by one, less in tiles; activations and norms add a few roundings.
+  bfloat16  against the float64 result rounded as the calls say (outputs once; the backward's dz before
+            its products): what is left are single values whose float32 error crosses a tie, a step of
+            2^-8 each: 2e-3, and 3e-3 for the backward.
+8-bit checkpoints of given values are exact.  Those of computed values may differ from the oracle's by
+one step where the value lies within its own error of a tie.
+"""
+
+
+import numpy as np
+import pytest
+
+from gpu_util import rel_l2
+from oracle import layers as ol
+
+pytestmark = pytest.mark.gpu
+
+TOL = {"float32": 2e-6, "bfloat16": 2e-3}
+TOL_BWD = {"float32": 2e-6, "bfloat16": 3e-3}
+SENTINEL = 7.0
+
+
+@pytest.fixture(scope="module")
+def e3():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2609_35099_amd import e3mi
+    e3mi.lib()
+    return e3mi
+
+
+def _rng(*key):
+    return np.random.default_rng([*key])
+
+
+def dev(a, dt, gap=0, shift=0):
+    """a on the device in type dt; as rows of a wider tensor (gap more columns, NaN) starting `shift`
+    elements off its allocation."""
+    import torch
+    t = torch.as_tensor(np.asarray(a, np.float32)).to("cuda").to(getattr(torch, dt))
+    if not gap and not shift:
+        return t
+    if t.dim() == 1:
+        buf = torch.full((t.numel() + shift,), float("nan"), dtype=t.dtype, device="cuda")
+        buf[shift:] = t
+        return buf[shift:]
+    m, n = t.shape
+    buf = torch.full((m * (n + gap) + shift,), float("nan"), dtype=t.dtype, device="cuda")
+    v = buf[shift:].view(m, n + gap)[:, :n]
+    v.copy_(t)
+    return v
+
+
+def out_like(shape, dt, gap, shift):
+    """A strided output filled with the sentinel, and a check that nothing beside it was written."""
+    import torch
+    m, n = shape
+    buf = torch.full((m * (n + gap) + shift,), SENTINEL, dtype=getattr(torch, dt), device="cuda")
+    wide = buf[shift:].view(m, n + gap)
+
+    def untouched():
+        return bool((wide[:, n:] == SENTINEL).all()) and bool((buf[:shift] == SENTINEL).all())
+    return wide[:, :n], untouched
+
+
+def host(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def rounded(a, dt):
+    """float64 values rounded to type dt's (bfloat16) precision, or as they are."""
+    import torch
+    return np.asarray(a) if dt == "float32" else torch.from_numpy(np.asarray(a)).bfloat16().double().numpy()
+
+
+def dense_grads(x, W, dy, z, act, dt):
+    """The oracle's gradients with dz rounded as a bfloat16 backward does."""
+    dz = dy if act == "none" else dy * ol.act(act, z)[1]
+    dx, dW, _ = ol.dense_bwd(x, W, rounded(dz, dt))
+    return [rounded(v, dt) for v in (dx, dW, dz.sum(0))]
+
+
+def packed(e3, a):
+    import torch
+    q, c = ol.pack8(a)
+    return e3.Packed8(torch.from_numpy(q).cuda(), torch.from_numpy(c).cuda())
+
+
+def values(p):
+    return ol.unpack8(p.q.cpu().numpy(), p.c.cpu().numpy())
+
+
+def near_steps(p, ref, share=2e-3):
+    """p is the checkpoint of values computed near ref: nearly all its values are ref's, the others
+    one step off (an exponent may move with its group's largest value)."""
+    q, c = ol.pack8(ref)
+    v, w = values(p), ol.unpack8(q, c)
+    step = np.ldexp(1.0, np.repeat(np.maximum(c.astype(int), p.c.cpu().numpy().astype(int)) - 127, 32, 1)[:, :v.shape[1]])
+    assert (np.abs(v - w) <= step).all()
+    assert (v != w).mean() <= share
+
+
+# ---------------------------------------------------------------- checkpoints
+@pytest.mark.parametrize("dt", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,cols,gap,shift", [(1, 1, 0, 0), (1, 31, 0, 0), (3, 32, 0, 0), (7, 33, 0, 1), (5, 64, 3, 0),
+                                                 (130, 100, 28, 3), (64, 515, 1, 0), (9, 1000, 0, 0), (2, 9001, 7, 5),
+                                                 (3000, 5, 0, 0), (1025, 256, 0, 0), (1, 70000, 0, 0)])
+def test_pack8_is_exact(e3, dt, rows, cols, gap, shift):
+    import torch
+    rng = _rng(rows, cols)
+    x = rng.standard_normal((rows, cols)) * np.exp(4 * rng.standard_normal((rows, 1)))
+    x[rng.random(x.shape) < 0.1] = 0
+    xd = dev(x, dt, gap, shift)
+    x = host(xd)
+    print("[case] pack8", dt, rows, cols, gap, shift, flush=True)
+    p = e3.pack8(xd)
+    q, c = ol.pack8(x)
+    assert np.array_equal(p.q.cpu().numpy(), q) and np.array_equal(p.c.cpu().numpy(), c)
+    y, untouched = out_like((rows, cols), dt, gap, shift)
+    e3.unpack8(p, out=y)
+    assert np.array_equal(host(y), ol.unpack8(q, c)) and untouched()
+    assert torch.equal(e3.unpack8(p, y.dtype), y)
+
+
+@pytest.mark.parametrize("dt", ["float32", "bfloat16"])
+def test_pack8_edges(e3, dt):
+    """The ends of the range, ties, the largest value's carry, infinities and NaNs."""
+    big = 3.4028235e38 if dt == "float32" else 3.3895e38
+    rows = [[1.0, -1.0, 0.0], [127.0, 0.5, 1.5], [127.5, 1.0, 3.0], [254.0, 1.0, -3.0], [big, -big, 1.0], [0.0] * 3,
+            [2.0**-126, -2.0**-127, 2.0**-128], [np.inf, 1.0, 2.0], [1.0, -np.inf, 2.0], [np.nan, 1.0, np.inf],
+            [2.0**-121, 1e-37, -3e-38], [126.5, 2.5, -2.5]]
+    x = np.zeros((len(rows), 70))
+    x[:, 31:34] = np.array(rows)              # across a group's end
+    x[:, 66:69] = np.array(rows)              # in the last, short group
+    xd = dev(x, dt)
+    x = host(xd)
+    p = e3.pack8(xd)
+    q, c = ol.pack8(x)
+    assert np.array_equal(p.c.cpu().numpy(), c)
+    assert np.array_equal(p.q.cpu().numpy(), q)
+    import torch
+    assert np.array_equal(host(e3.unpack8(p, getattr(torch, dt))), ol.unpack8(q, c), equal_nan=True)
+
+
+# ---------------------------------------------------------------- layer norm
+NORM = [(1, 1, 0, 0), (3, 1, 0, 0), (2, 7, 1, 1), (70, 16, 0, 0), (33, 31, 0, 0), (64, 32, 4, 0), (50, 65, 0, 3),
+        (129, 128, 1920, 0), (5003, 64, 0, 0), (31, 250, 2, 1), (40, 256, 0, 0), (10, 515, 0, 0), (9, 1000, 24, 8),
+        (700, 1025, 0, 0), (5, 2047, 1, 0), (4, 2049, 0, 0), (6, 4100, 0, 2), (3, 8192, 0, 0), (3, 8193, 5, 0),
+        (2, 16385, 0, 1), (2, 40001, 0, 0), (1, 4096, 0, 0), (0, 40, 0, 0)]
+
+
+def _norm_inputs(rows, cols, dt, seed=0):
+    rng = _rng(rows, cols, seed)
+    x = rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1))) + 0.5
+    return x, 1 + 0.3 * rng.standard_normal(cols), rng.standard_normal(cols), 1e-3 * rng.standard_normal((rows, cols))
+
+
+@pytest.mark.parametrize("dt", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,cols,gap,shift", NORM)
+@pytest.mark.parametrize("affine", [True, False])
+def test_layer_norm_forward(e3, dt, rows, cols, gap, shift, affine):
+    x, g, b, _ = _norm_inputs(rows, cols, dt)
+    xd, gd, bd = dev(x, dt, gap, shift), dev(g, dt, shift=shift), dev(b, dt, shift=shift)
+    y, untouched = out_like((rows, cols), dt, gap, shift)
+    print("[case] layer_norm_fwd", dt, rows, cols, gap, shift, affine, flush=True)
+    got = e3.layer_norm_fwd(xd, gd if affine else None, bd if affine else None, 1e-5, keep=("stats", "x8", "y8"), out=y)
+    ref, mean, rstd = ol.layer_norm_fwd(host(xd), *((host(gd), host(bd)) if affine else (None, None)))
+    if rows == 0:
+        return
+    assert untouched()
+    if cols > 1:
+        assert rel_l2(host(got[0]), rounded(ref, dt)) < TOL[dt]
+    else:
+        assert np.abs(host(got[0]) - ref).max() < 1e-6 + (0.01 if dt == "bfloat16" else 0)
+    assert rel_l2(got[1].cpu(), mean) < 1e-6 and rel_l2(got[2].cpu(), rstd) < 1e-6
+    for p, v in ((got[3], host(xd)), (got[4], host(y))):
+        q, c = ol.pack8(v)
+        assert np.array_equal(p.q.cpu().numpy(), q) and np.array_equal(p.c.cpu().numpy(), c)
+    # without the extra outputs: the same bits
+    assert np.array_equal(host(e3.layer_norm_fwd(xd, gd if affine else None, bd if affine else None)), host(y))
+
+
+@pytest.mark.parametrize("dt", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,cols,gap,shift", NORM)
+@pytest.mark.parametrize("ckpt", [False, True])
+def test_layer_norm_backward(e3, dt, rows, cols, gap, shift, ckpt):
+    import torch
+    x, g, _, dy = _norm_inputs(rows, cols, dt)
+    xd, gd, dyd = dev(x, dt, gap, shift), dev(g, dt, shift=shift), dev(dy, dt, gap, shift)
+    _, mean, rstd = ol.layer_norm_fwd(host(xd))
+    ms = [torch.from_numpy(v.astype(np.float32)).cuda() for v in (mean, rstd)]
+    xr = host(xd)
+    xin = xd
+    if ckpt:
+        xin = packed(e3, xr)
+        xr = values(xin)
+    dx, untouched = out_like((rows, cols), dt, gap, shift)
+    print("[case] layer_norm_bwd", dt, rows, cols, gap, shift, ckpt, flush=True)
+    got = e3.layer_norm_bwd(xin, gd, dyd, *ms, dx=dx)
+    ref = [rounded(v, dt) for v in ol.layer_norm_bwd(xr, host(gd), host(dyd), host(ms[0]), host(ms[1]))]
+    assert untouched()
+    if rows == 0:
+        assert not host(got[1]).any() and not host(got[2]).any()
+        return
+    # one column: dx is 0 up to a rounding of its terms
+    scale = np.abs(host(dyd)).max() * np.abs(host(gd)).max() * rstd.max()
+    if cols > 2:
+        assert rel_l2(host(got[0]), ref[0]) < TOL[dt]
+    else:
+        assert np.abs(host(got[0]) - ref[0]).max() < 1e-6 * scale
+    n = (xr - mean[:, None]) * rstd[:, None]
+    for k, terms in ((1, host(dyd) * n), (2, host(dyd))):
+        # the terms of a column may cancel: against their size
+        bar = TOL[dt] * np.linalg.norm(ref[k]) + 2e-7 * np.linalg.norm(np.sqrt((terms**2).sum(0)))
+        assert np.linalg.norm(host(got[k]) - ref[k]) <= bar
+    # single outputs are the same bits
+    for k, w in enumerate(("dx", "dgamma", "dbeta")):
+        one = e3.layer_norm_bwd(xin, gd, dyd, *ms, want=(w,))
+        assert torch.equal(one[k], got[k]) and sum(v is not None for v in one) == 1
+
+
+def test_layer_norm_large_mean_and_constant_rows(e3):
+    """A mean 30 times the deviation: its own rounding, 2^-24 of 30, is 2e-6 of the deviations (bar 5e-6).
+    Rows of one value give y = beta exactly where the mean is exact."""
+    rng = _rng(5)
+    x = (rng.standard_normal((64, 300)) + 30).astype(np.float32)
+    assert rel_l2(host(e3.layer_norm_fwd(dev(x, "float32"))), ol.layer_norm_fwd(x)[0]) < 5e-6
+    c = np.full((4, 256), 3.0)
+    c[2] = 0
+    b = rng.standard_normal(256)
+    y = e3.layer_norm_fwd(dev(c, "float32"), None, dev(b, "float32"))
+    assert np.array_equal(host(y), np.tile(b.astype(np.float32), (4, 1)))
+
+
+@pytest.mark.parametrize("cols", [24, 700, 3001, 20000])
+def test_layer_norm_bad_rows_stay_alone(e3, cols):
+    x, g, b, dy = _norm_inputs(9, cols, "float32")
+    xb = x.copy()
+    xb[3, cols // 2], xb[7, 0] = np.inf, np.nan
+    good = [0, 1, 2, 4, 5, 6, 8]
+    y0, m0, r0 = e3.layer_norm_fwd(dev(x, "float32"), dev(g, "float32"), dev(b, "float32"), keep=("stats",))
+    y1, m1, r1 = e3.layer_norm_fwd(dev(xb, "float32"), dev(g, "float32"), dev(b, "float32"), keep=("stats",))
+    assert np.array_equal(host(y0)[good], host(y1)[good])
+    assert np.isnan(host(y1)[[3, 7]]).all()
+    d0 = e3.layer_norm_bwd(dev(x, "float32"), dev(g, "float32"), dev(dy, "float32"), m0, r0, want=("dx",))[0]
+    d1 = e3.layer_norm_bwd(dev(xb, "float32"), dev(g, "float32"), dev(dy, "float32"), m1, r1, want=("dx",))[0]
+    assert np.array_equal(host(d0)[good], host(d1)[good])
+
+
+# ---------------------------------------------------------------- dense layers
+# rows, K, N, gap, shift: single rows, single columns, widths around the tiles, odd ones, splits of K
+DENSE = [(1, 1, 1, 0, 0), (1, 8, 64, 0, 0), (1, 1024, 4096, 0, 0), (1, 515, 1021, 3, 1), (2, 100, 33, 0, 0),
+         (5, 2048, 64, 0, 0), (16, 1000, 500, 0, 0), (17, 64, 1, 0, 0), (40, 1, 40, 5, 0), (63, 65, 66, 0, 0),
+         (64, 64, 64, 0, 0), (100, 96, 128, 8, 8), (128, 128, 128, 0, 0), (129, 127, 130, 0, 0), (300, 64, 64, 0, 0),
+         (257, 256, 255, 1, 0), (1000, 8, 64, 0, 0), (515, 1021, 77, 0, 3), (2000, 300, 260, 4, 0), (700, 64, 1664, 0, 0),
+         (260, 2100, 300, 0, 0), (5000, 17, 9, 0, 0), (1024, 512, 512, 0, 0)]
+DTS = ["float32", "bfloat16"]
+
+
+def _dense_inputs(M, K, N, seed=0):
+    rng = _rng(M, K, N, seed)
+    x = rng.standard_normal((M, K)) * np.exp(0.5 * rng.standard_normal((M, 1))) + 0.2
+    return (x, rng.standard_normal((K, N)) / np.sqrt(K), 0.3 * rng.standard_normal(N), rng.standard_normal((M, N)),
+            1e-3 * rng.standard_normal((M, N)))
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("M,K,N,gap,shift", DENSE)
+def test_dense_forward(e3, dt, M, K, N, gap, shift):
+    import torch
+    x, W, b, r, _ = _dense_inputs(M, K, N)
+    xd, Wd, bd, rd = dev(x, dt, gap, shift), dev(W.reshape(-1), dt, shift=shift).view(K, N), dev(b, dt, shift=shift), \
+        dev(r, dt, gap, shift)
+    for act in ol.ACTIVATIONS:
+        y, untouched = out_like((M, N), dt, gap, shift)
+        print("[case] dense_fwd", dt, M, K, N, gap, shift, act, flush=True)
+        got = e3.dense_fwd(xd, Wd, bd, rd, act=act, keep=("z", "z8", "y8"), out=y)
+        ref, z = ol.dense_fwd(host(xd), host(Wd), host(bd), host(rd), act)
+        assert untouched()
+        assert rel_l2(host(y), rounded(ref, dt)) < TOL[dt] and rel_l2(host(got[1]), rounded(z, dt)) < TOL[dt]
+        near_steps(got[2], z)
+        q, c = ol.pack8(host(y))
+        assert np.array_equal(got[3].q.cpu().numpy(), q) and np.array_equal(got[3].c.cpu().numpy(), c)
+        # without the extra outputs, into fresh memory: the same bits
+        assert torch.equal(e3.dense_fwd(xd, Wd, bd, rd, act=act), y)
+    y = e3.dense_fwd(xd, Wd)
+    assert rel_l2(host(y), rounded(host(xd) @ host(Wd), dt)) < TOL[dt]
+    # the residual's own memory as the output
+    r2 = rd.clone() if not gap else dev(host(rd), dt, gap, shift)
+    e3.dense_fwd(xd, Wd, bd, r2, act="silu", out=r2)
+    assert torch.equal(r2, e3.dense_fwd(xd, Wd, bd, rd, act="silu"))
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("M,K,N,gap,shift", DENSE)
+@pytest.mark.parametrize("ckpt", [False, True])
+def test_dense_backward(e3, dt, M, K, N, gap, shift, ckpt):
+    import torch
+    x, W, b, _, dy = _dense_inputs(M, K, N)
+    xd, Wd, dyd = dev(x, dt, gap, shift), dev(W.reshape(-1), dt, shift=shift).view(K, N), dev(dy, dt, gap, shift)
+    zd = dev(x @ W + b, dt, gap, shift)
+    xr, zr, xin, zin = host(xd), host(zd), xd, zd
+    if ckpt:
+        xin, zin = packed(e3, xr), packed(e3, zr)
+        xr, zr = values(xin), values(zin)
+    for act in ol.ACTIVATIONS:
+        dx, untouched = out_like((M, K), dt, gap, shift)
+        print("[case] dense_bwd", dt, M, K, N, gap, shift, ckpt, act, flush=True)
+        got = e3.dense_bwd(xin, Wd, dyd, None if act == "none" else zin, act=act, dx=dx)
+        ref = dense_grads(xr, host(Wd), host(dyd), zr, act, dt)
+        assert untouched()
+        for k, w in enumerate(("dx", "dW", "db")):
+            size = np.linalg.norm(ref[k])
+            if w == "db":    # the terms of a column may cancel: against their size
+                size += 0.1 * np.linalg.norm(np.sqrt(((host(dyd) * ol.act(act, zr)[1])**2).sum(0)))
+            assert np.linalg.norm(host(got[k]) - ref[k]) <= TOL_BWD[dt] * size, (act, w)
+        # each alone, where the others' kernels do not run: the same bits
+        for k, w in enumerate(("dx", "dW", "db")):
+            one = e3.dense_bwd(xin if w == "dW" else None, Wd, dyd, None if act == "none" else zin, act=act, want=(w,))
+            assert torch.equal(one[k], got[k]), (act, w)
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("M,K,N", [(9001, 128, 256), (20000, 64, 64), (9001, 8, 64), (4099, 64, 1664), (40000, 33, 47)])
+def test_dense_many_rows(e3, dt, M, K, N):
+    x, W, b, r, dy = _dense_inputs(M, K, N)
+    xd, Wd, bd, rd, dyd = (dev(v, dt) for v in (x, W, b, r, dy))
+    print("[case] dense, many rows", dt, M, K, N, flush=True)
+    y, z8, y8 = e3.dense_fwd(xd, Wd, bd, rd, act="silu", keep=("z8", "y8"))
+    ref, z = ol.dense_fwd(host(xd), host(Wd), host(bd), host(rd), "silu")
+    assert rel_l2(host(y), rounded(ref, dt)) < TOL[dt]
+    near_steps(z8, z)
+    x8 = e3.pack8(xd)
+    for xin, zin in ((xd, dev(z, dt)), (x8, z8), (xd, z8), (x8, dev(z, dt))):
+        xr = values(xin) if isinstance(xin, e3.Packed8) else host(xin)
+        zr = values(zin) if isinstance(zin, e3.Packed8) else host(zin)
+        for g, w in zip(e3.dense_bwd(xin, Wd, dyd, zin, act="silu"), dense_grads(xr, host(Wd), host(dyd), zr, "silu", dt)):
+            assert rel_l2(host(g), w) < TOL_BWD[dt]
+
+
+@pytest.mark.parametrize("M,K,N", [(3, 40, 50), (200, 130, 70), (1000, 64, 64)])
+def test_dense_infinities_and_nans_stay_in_their_rows_and_columns(e3, M, K, N):
+    """An infinity in x reaches its own row of y, one in W its own column, as in float32 arithmetic;
+    columns of x and W past the reduction's end are not read."""
+    x, W, _, _, dy = _dense_inputs(M, K, N)
+    x[1, 3], x[2, K - 1] = np.inf, np.nan
+    W[K - 2, 5] = -np.inf
+    with np.errstate(invalid="ignore"):
+        ref = x.astype(np.float32).astype(np.float64) @ W.astype(np.float32).astype(np.float64)
+    for dt in DTS:
+        y = host(e3.dense_fwd(dev(x, dt, 3, 1), dev(W, dt)))
+        with np.errstate(invalid="ignore"):
+            ref = host(dev(x, dt)) @ host(dev(W, dt))
+        assert np.array_equal(np.isnan(y), np.isnan(ref))
+        assert np.array_equal(y[np.isinf(ref)], ref[np.isinf(ref)])
+        fine = np.isfinite(ref)
+        assert rel_l2(y[fine], rounded(ref[fine], dt)) < TOL[dt]
+    dy[0, 2], x[1, 3], x[2, K - 1], W[K - 2, 5] = np.inf, 1.0, 1.0, 1.0
+    for dt in DTS:
+        xd, Wd, dyd = dev(x, dt), dev(W, dt), dev(dy, dt)
+        dx, dW, db = (host(t) for t in e3.dense_bwd(xd, Wd, dyd))
+        r = dense_grads(host(xd), host(Wd), host(dyd), None, "none", dt)
+        for g, w in zip((dx, dW, db), r):
+            fine = np.isfinite(w)
+            assert np.array_equal(np.isfinite(g), fine)
+            assert rel_l2(g[fine], w[fine]) < TOL_BWD[dt]
+
+
+@pytest.mark.parametrize("scale", [1e-36, 1e-30, 1e-12, 1e12, 1e18])
+def test_dense_float32_range(e3, scale):
+    """Operands over the range of float32 (products of both at scale 1e18 reach 1e36)."""
+    x, W, _, _, dy = _dense_inputs(200, 96, 70)
+    xs = x * scale
+    y = e3.dense_fwd(dev(xs, "float32"), dev(W, "float32"))
+    assert rel_l2(host(y) / scale, host(dev(xs, "float32")) / scale @ host(dev(W, "float32"))) < TOL["float32"]
+    if scale in (1e-12, 1e12, 1e18):
+        xd, Wd, dyd = dev(xs, "float32"), dev(W, "float32"), dev(1e3 * dy * scale, "float32")
+        for g, w in zip(e3.dense_bwd(xd, Wd, dyd), ol.dense_bwd(host(xd), host(Wd), host(dyd))):
+            assert rel_l2(host(g) / scale, w / scale) < TOL["float32"]
+
+
+def test_dense_gradient_equals_differences(e3):
+    """The kernels' own forward, differenced in float32 along random directions: 1e-2 steps, second-order
+    error 1e-4 of the curvature, rounding 1e-7 / 1e-2 of y."""
+    rng = _rng(11)
+    x, W, b, _, _ = _dense_inputs(50, 40, 30)
+    dy = rng.standard_normal((50, 30))
+    xd, Wd, bd = (dev(v, "float32") for v in (x, W, b))
+    _, z = e3.dense_fwd(xd, Wd, bd, act="gelu", keep=("z",))
+    grads = [host(g) for g in e3.dense_bwd(xd, Wd, dev(dy, "float32"), z, act="gelu")]
+    h = 1e-2
+    for at, v in enumerate((x, W, b)):
+        d = rng.standard_normal(v.shape) / np.sqrt(v.size)
+        up, lo = [x, W, b], [x, W, b]
+        up[at], lo[at] = v + h * d, v - h * d
+        f = [(host(e3.dense_fwd(*(dev(t, "float32") for t in s), act="gelu")) * dy).sum() for s in (up, lo)]
+        assert abs((f[0] - f[1]) / (2 * h) - (grads[at] * d).sum()) < 2e-3 * np.linalg.norm(grads[at])
+
+
+# ---------------------------------------------------------------- as the calls are used
+def test_empty_rows(e3):
+    import torch
+    for dt in DTS:
+        t = getattr(torch, dt)
+        x, W, dy = (torch.zeros(s, dtype=t, device="cuda") for s in ((0, 9), (9, 5), (0, 5)))
+        y, z8 = e3.dense_fwd(x, W, act="relu", keep=("z8",))
+        assert y.shape == (0, 5) and z8.shape == (0, 5)
+        dx, dW, db = e3.dense_bwd(x, W, dy)
+        assert dx.shape == (0, 9) and not dW.any() and not db.any() and dW.shape == (9, 5)
+        assert e3.pack8(x).shape == (0, 9) and e3.unpack8(e3.pack8(x)).shape == (0, 9)
+
+
+def test_repeats_are_bitwise_equal(e3):
+    import torch
+    x, W, b, r, dy = _dense_inputs(3000, 200, 150)
+    for dt in DTS:
+        xd, Wd, bd, rd, dyd = (dev(v, dt) for v in (x, W, b, r, dy))
+        mean, rstd = e3.layer_norm_fwd(dyd, keep=("stats",))[1:]
+
+        def all_of():
+            y, z, z8 = e3.dense_fwd(xd, Wd, bd, rd, act="silu", keep=("z", "z8"))
+            return [y, z, z8.q, *e3.dense_bwd(xd, Wd, dyd, z, act="silu"),
+                    *e3.layer_norm_bwd(dyd, bd, rd, mean, rstd)]
+        first = all_of()
+        for _ in range(3):
+            assert all(torch.equal(a, c) for a, c in zip(first, all_of()))
+
+
+def test_on_another_stream(e3):
+    """Inputs made on one stream, the calls on another that waits for it: outputs and scratch belong to it."""
+    import torch
+    x, W, b, _, dy = _dense_inputs(4000, 128, 256)
+    ref = None
+    for s in (None, torch.cuda.Stream()):
+        xd, Wd, bd, dyd = (dev(v, "float32") for v in (x, W, b, dy))
+        if s is not None:
+            s.wait_stream(torch.cuda.current_stream())
+        y, z8 = e3.dense_fwd(xd, Wd, bd, act="silu", keep=("z8",), stream=s)
+        g = e3.dense_bwd(xd, Wd, dyd, z8, act="silu", stream=s)
+        n, mean, rstd, x8 = e3.layer_norm_fwd(y, keep=("stats", "x8"), stream=s)
+        h = e3.layer_norm_bwd(x8, None, dyd, mean, rstd, stream=s)
+        if s is not None:
+            s.synchronize()
+        torch.cuda.synchronize()
+        got = [y, z8.q, *g, n, x8.q, *h]
+        if ref is None:
+            ref = got
+        assert all(torch.equal(a, c) for a, c in zip(ref, got))
+
+
+def test_in_a_captured_graph(e3):
+    """A layer's forward and backward captured once and replayed with eager work between: every replay
+    gives the eager result."""
+    import torch
+    x, W, b, _, dy = _dense_inputs(300, 64, 64)
+    xd, Wd, bd, dyd = (dev(v, "float32") for v in (x, W, b, dy))
+    row = dev(x[:1], "float32")
+
+    def step():
+        n, mean, rstd, x8 = e3.layer_norm_fwd(xd, bd, bd, keep=("stats", "x8"))
+        y, z8, y8 = e3.dense_fwd(n, Wd, bd, xd, act="silu", keep=("z8", "y8"))
+        dn, dW, db = e3.dense_bwd(e3.pack8(n), Wd, dyd, z8, act="silu")
+        return [y, y8.q, dW, db, *e3.layer_norm_bwd(x8, bd, dn, mean, rstd), e3.dense_fwd(row, Wd, bd, act="gelu")]
+    ref = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for it in range(4):
+        for t in out:
+            t.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(ref, out)), it
+        step()
+        torch.cuda.synchronize()
+
+
+def test_refusals(e3):
+    import torch
+    f = torch.zeros((4, 8), device="cuda")
+    W = torch.zeros((8, 6), device="cuda")
+    dy = torch.zeros((4, 6), device="cuda")
+    p = e3.pack8(f)
+    for fn, args, kw, err in [
+            (e3.pack8, (f.double(),), {}, TypeError), (e3.pack8, (f.cpu(),), {}, ValueError),
+            (e3.pack8, (f.t(),), {}, ValueError), (e3.pack8, (f[0],), {}, ValueError),
+            (e3.pack8, (f[:1].expand(4, 8),), {}, ValueError),
+            (e3.unpack8, (f,), {}, TypeError), (e3.unpack8, (p, torch.float64), {}, TypeError),
+            (e3.Packed8, (p.q, p.c[:, :0]), {}, ValueError), (e3.Packed8, (p.c, p.c), {}, TypeError),
+            (e3.layer_norm_fwd, (f, torch.zeros(7, device="cuda")), {}, ValueError),
+            (e3.layer_norm_fwd, (f, torch.zeros(8, dtype=torch.bfloat16, device="cuda")), {}, TypeError),
+            (e3.layer_norm_fwd, (f,), {"keep": ("z",)}, ValueError),
+            (e3.layer_norm_fwd, (f, None, None, -1.0), {}, e3.E3Error),
+            (e3.layer_norm_fwd, (f, None, None, float("nan")), {}, e3.E3Error),
+            (e3.layer_norm_bwd, (f, None, dy, f[:, 0].contiguous(), f[:, 0].contiguous()), {}, ValueError),
+            (e3.dense_fwd, (f, W.t().contiguous()), {}, ValueError), (e3.dense_fwd, (f, W.bfloat16()), {}, TypeError),
+            (e3.dense_fwd, (f, W), {"act": "tanh"}, ValueError), (e3.dense_fwd, (f, W), {"keep": ("x8",)}, ValueError),
+            (e3.dense_fwd, (f, W, None, f), {}, ValueError),
+            (e3.dense_bwd, (f, W, dy), {"act": "silu"}, e3.E3Error),                   # needs z
+            (e3.dense_bwd, (None, W, dy), {}, e3.E3Error),                             # dW needs x
+            (e3.dense_bwd, (f, W, dy), {"want": ("dz",)}, ValueError),
+            (e3.dense_bwd, (e3.pack8(dy), W, dy), {}, ValueError)]:
+        with pytest.raises(err):
+            fn(*args, **kw)
+
+
+def test_workspace_too_small_is_refused(e3):
+    import torch
+    x, W, b, _, dy = _dense_inputs(1000, 32, 32)
+    xd, Wd, dyd = (dev(v, "float32") for v in (x, W, dy))
+    small = torch.empty(16, dtype=torch.uint8, device="cuda")
+    with pytest.raises(e3.E3Error) as ei:
+        e3.dense_bwd(xd, Wd, dyd, xd @ Wd, act="silu", ws=small)
+    assert ei.value.status == 4
+    stats = e3.layer_norm_fwd(xd, keep=("stats",))[1:]
+    with pytest.raises(e3.E3Error) as ei:
+        e3.layer_norm_bwd(xd, None, xd, *stats, ws=small)
+    assert ei.value.status == 4
