@@ -2,22 +2,17 @@
 //
 //   z = x W + b, y = act(z) + r
 //   dz = dy act'(z), dx = dz W^T, dW = x^T dz, db = sum_rows dz  (dr = dy)
-#include "layers.h"
+#include "dense_tile.h"
 
 namespace {
 
-constexpr int kTile = 64, kStep = 16;
-
 struct DenseArgs {
-  // operands of the product: rows of A by columns of B over a reduction axis
-  const void *a, *b;
-  int64_t a_row, a_red, b_red, b_col;  // element strides
-  const int8_t* aq;                    // A packed (its rows run along the reduction: dW's x)
-  const uint8_t* ac;
+  Side a, b;  // rows of A by columns of B over the reduction
   int64_t rows, red;
   int cols;
-  int packed_cols;
-  int64_t chunk;  // reduction indexes per split (blockIdx.z)
+  int width;      // columns of a packed A
+  int64_t chunk;  // reduction indexes per split
+  int splits;
   float* part;    // partial sums [splits][rows][cols], instead of the epilogue
   // epilogue
   const void *bias, *res;
@@ -57,64 +52,59 @@ __device__ __forceinline__ void dense_tail(const DenseArgs& a, int64_t row, bool
   if (a.yq) pack8_piece<V>(v, col, n, a.yq + row * a.cols, a.yc + row * groups);
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void k_dense(DenseArgs a) {
-  __shared__ float sA[kStep][kTile + 4], sB[kStep][kTile + 4], sC[kTile][kTile + 4];
-  const int tid = threadIdx.x, tr = tid / 16 * 4, tc = tid % 16 * 4;
-  const int64_t row0 = (int64_t)blockIdx.x * kTile;
-  const int col0 = (int)blockIdx.y * kTile;
-  const int64_t r0 = blockIdx.z * a.chunk, r1 = r0 + a.chunk < a.red ? r0 + a.chunk : a.red;
-  const T* A = static_cast<const T*>(a.a);
-  const T* B = static_cast<const T*>(a.b);
-  float acc[4][4] = {};
-  for (int64_t r = r0; r < r1; r += kStep) {
-    for (int i = tid; i < kStep * kTile; i += 256) {
-      const int k = i % kStep, m = i / kStep, k2 = i / kTile, n = i % kTile;
-      float u = 0.0f, w = 0.0f;
-      if (row0 + m < a.rows && r + k < r1) {
-        if (a.aq) {
-          const int64_t at = r + k;
-          const int col = (int)(row0 + m);
-          u = (float)a.aq[at * a.packed_cols + col] *
-              step8(a.ac[at * ((a.packed_cols + kGroup - 1) / kGroup) + col / kGroup]);
-        } else {
-          u = Elem<T>::one(A[(row0 + m) * a.a_row + (r + k) * a.a_red]);
-        }
-      }
-      if (col0 + n < a.cols && r + k2 < r1) w = Elem<T>::one(B[(r + k2) * a.b_red + (col0 + n) * a.b_col]);
-      sA[k][m] = u;
-      sB[k2][n] = w;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kStep; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sA[k][tr + i], sB[k][tc + j], acc[i][j]);
-    __syncthreads();
+// A sum again from memory, in float32.
+template <class T, Form FA, Form FB, bool QA>
+__device__ __attribute__((noinline)) float dense_again(const Side& a, const Side& b, int64_t row, int col, int64_t k0,
+                                                       int64_t end, int width) {
+  float sum = 0.0f;
+  const int groups = (width + kGroup - 1) / kGroup;
+  for (int64_t k = k0; k < end; ++k) {
+    const int64_t m = FA == kAlong ? row : k, c = FA == kAlong ? k : row;
+    const float u = QA ? (float)a.q[m * width + c] * step8(a.c[m * groups + c / kGroup])
+                       : Elem<T>::one(static_cast<const T*>(a.p)[m * a.ld + c]);
+    const float w = Elem<T>::one(static_cast<const T*>(b.p)[FB == kAlong ? col * b.ld + k : k * b.ld + col]);
+    sum = fmaf(u, w, sum);
   }
+  return sum;
+}
+
+template <class T, Form FA, Form FB, int BM, int BN, int BK, int WM, int WN, bool QA, int BUFS, int OCC>
+__global__ __launch_bounds__(WM* WN* kWave, OCC) void k_dense(DenseArgs a) {
+  using Tl = Tile<T, FA, FB, BM, BN, BK, WM, WN, QA, BUFS>;
+  constexpr int V = Elem<T>::V;
+  __shared__ __align__(16) typename Tl::Shared sh;
+  const int64_t tm = (a.rows + BM - 1) / BM;
+  const int tn = (a.cols + BN - 1) / BN;
+  int64_t u = block_id();
+  if (u >= tm * tn * a.splits) return;
+  const int split = (int)(u / (tm * tn));
+  u -= split * (tm * tn);
+  const int64_t r0 = u / tn * BM;
+  const int c0 = (int)(u % tn) * BN;
+  const int64_t k0 = split * a.chunk, end = k0 + a.chunk < a.red ? k0 + a.chunk : a.red;
+  Tl t;
+  t.run(sh, a.a, a.b, r0, a.rows, c0, a.cols, k0, end, a.width);
+  t.finish(sh, [&](int r, int c, float(&v)[V]) {
+    const int64_t row = r0 + r;
+    const int col = c0 + c;
+    const int n = row < a.rows ? a.cols - col : 0;
+    if constexpr (sizeof(T) == 4) {
+      float z = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+      for (int e = 0; e < V; ++e) z += v[e] * 0.0f;
+      if (z != 0.0f)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sC[tr + i][tc + j] = acc[i][j];
-  __syncthreads();
-  constexpr int V = Elem<T>::V, P = kTile / V;
-  for (int i = tid; i < kTile * P; i += 256) {
-    const int m = i / P, c = i % P * V;
-    const int64_t row = row0 + m;
-    float v[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = sC[m][c + e];
+        for (int e = 0; e < V; ++e)
+          if (e < n && v[e] * 0.0f != 0.0f) v[e] = dense_again<T, FA, FB, QA>(a.a, a.b, row, col + e, k0, end, a.width);
+    }
     if (a.part) {
+      float* p = a.part + ((int64_t)split * a.rows + row) * a.cols + col;
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (row < a.rows && col0 + c + e < a.cols)
-          a.part[((int64_t)blockIdx.z * a.rows + row) * a.cols + col0 + c + e] = v[e];
+      for (int e = 0; e < V; e += 4) st_piece<float>(p + e, n - e, reinterpret_cast<float(&)[4]>(v[e]));
     } else {
-      dense_tail<T, V>(a, row, row < a.rows, col0 + c, v);
+      dense_tail<T, V>(a, row, row < a.rows, col, v);
     }
-  }
+  });
 }
 
 // The partial sums of the splits, in order, and the epilogue.
@@ -174,56 +164,74 @@ __global__ __launch_bounds__(256) void k_dense_dz(RowsIn<T> z, int act, const T*
 }
 
 // ------------------------------------------------------------ host
-int64_t tiles(int64_t n) { return (n + kTile - 1) / kTile; }
-// Splits of a reduction of `red` over a grid of `blocks` tiles: enough to fill
-// the card, each of at least 64 indexes.
-int64_t dense_splits(int64_t blocks, int64_t red) {
-  return std::max<int64_t>(1, std::min<int64_t>({1024 / std::max<int64_t>(blocks, 1), (red + 63) / 64, 64}));
+// How a product is cut: tiles of bm x bn, and splits of its reduction where the
+// tiles alone would leave much of the card idle.
+struct Cut {
+  int bm, bn, splits;
+  int64_t blocks, chunk;
+};
+constexpr int kFill = 512;  // workgroups that fill the card
+Cut dense_cut(int64_t rows, int64_t cols, int64_t red) {
+  Cut c{};
+  auto tiles = [&](int b, int64_t n) { return (n + b - 1) / b; };
+  c.bm = c.bn = 128;
+  if (tiles(128, rows) * tiles(128, cols) < kFill / 2) c.bm = c.bn = 64;
+  if (cols <= 64) c.bn = 64;
+  if (rows <= 64) c.bm = 64;
+  if (c.bn == 64) c.bm = 64;
+  if (c.bm == 64) c.bn = 64;
+  const int64_t t = tiles(c.bm, rows) * tiles(c.bn, cols);
+  const int64_t most = (red + 255) / 256;  // at least 256 indexes each
+  int64_t s = std::max<int64_t>(1, std::min<int64_t>({kFill / std::max<int64_t>(t, 1), most, 256}));
+  c.chunk = std::max<int64_t>(64, ((red + s - 1) / s + 63) / 64 * 64);
+  c.splits = (int)std::max<int64_t>(1, (red + c.chunk - 1) / c.chunk);
+  c.blocks = t * c.splits;
+  return c;
 }
-int64_t dense_chunk(int64_t red, int64_t splits) { return ((red + splits - 1) / splits + 63) / 64 * 64; }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+size_t cut_bytes(const Cut& c, int64_t rows, int64_t cols) {
+  return c.splits > 1 ? up256((size_t)c.splits * rows * cols * sizeof(float)) : 0;
+}
 
 struct DenseBwdWs {
-  size_t dz, db, dw, total;
-  int64_t db_blocks, db_rows, dw_splits;
+  size_t dz, db, part, total;
+  int64_t db_blocks, db_rows;
 };
 DenseBwdWs dense_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   const size_t e = t == E3_F32 ? 4 : 2;
   DenseBwdWs w{};
   w.db_blocks = std::max<int64_t>(1, std::min<int64_t>(512, (M + 63) / 64));
   w.db_rows = (M + w.db_blocks - 1) / w.db_blocks;
-  w.dw_splits = dense_splits(tiles(K) * tiles(N), M);
   w.dz = up256(M * N * e);
   w.db = up256(w.db_blocks * N * 4);
-  w.dw = w.dw_splits > 1 ? up256(w.dw_splits * K * N * 4) : 0;
-  w.total = M == 0 ? 0 : w.dz + w.db + w.dw;
+  w.part = std::max(cut_bytes(dense_cut(M, K, N), M, K), cut_bytes(dense_cut(K, N, M), K, N));
+  w.total = M == 0 ? 0 : w.dz + w.db + w.part;
   return w;
 }
 
-template <class T>
-e3_status dense_product(DenseArgs a, int64_t splits, float* part, const char* name, hipStream_t st) {
-  a.chunk = dense_chunk(a.red, splits);
-  splits = (a.red + a.chunk - 1) / a.chunk;
-  a.part = splits > 1 ? part : nullptr;
+template <class T, Form FA, Form FB, bool QA>
+e3_status dense_product(DenseArgs a, float* part, const char* name, hipStream_t st) {
+  const Cut c = dense_cut(a.rows, a.cols, a.red);
+  a.chunk = c.chunk, a.splits = c.splits, a.part = c.splits > 1 ? part : nullptr;
   {
     TimedLaunch t_(name, st);
-    hipLaunchKernelGGL(k_dense<T>, dim3((unsigned)tiles(a.rows), (unsigned)tiles(a.cols), (unsigned)splits), dim3(256),
-                       0, st, a);
+    constexpr bool f32 = sizeof(T) == 4;
+    constexpr int BK = f32 ? 32 : 64, BUFS = f32 ? 1 : 2;
+    auto* k = c.bm == 128 ? k_dense<T, FA, FB, 128, 128, BK, 2, 2, QA, BUFS, 2>
+                          : k_dense<T, FA, FB, 64, 64, BK, 2, 2, QA, BUFS, 2>;
+    hipLaunchKernelGGL(k, grid_of(c.blocks), dim3(256), 0, st, a);
     E3_HIP(hipGetLastError());
   }
-  if (splits > 1) {
+  if (c.splits > 1) {
     TimedLaunch t_("dense_join", st);
     const int64_t per = (a.cols + kGroup - 1) / kGroup * (kGroup / Elem<T>::V);
-    hipLaunchKernelGGL(k_dense_join<T>, grid_of((a.rows * per + 255) / 256), dim3(256), 0, st, a, (int)splits);
+    hipLaunchKernelGGL(k_dense_join<T>, grid_of((a.rows * per + 255) / 256), dim3(256), 0, st, a, c.splits);
     E3_HIP(hipGetLastError());
   }
   return E3_OK;
 }
 
-size_t dense_fwd_ws(int64_t M, int64_t K, int64_t N) {
-  const int64_t s = dense_splits(tiles(M) * tiles(N), K);
-  return M == 0 || s == 1 ? 0 : up256(s * M * N * 4);
-}
+size_t dense_fwd_ws(int64_t M, int64_t K, int64_t N) { return M == 0 ? 0 : cut_bytes(dense_cut(M, N, K), M, N); }
 
 bool good_dims(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   return good_rows(t, M, K) && N >= 1 && N <= kMaxCols;
@@ -236,7 +244,7 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
   const DenseBwdWs w = dense_bwd_ws(t, M, K, N);
   T* dz = reinterpret_cast<T*>(ws);
   float* dbp = reinterpret_cast<float*>(ws + w.dz);
-  float* dwp = reinterpret_cast<float*>(ws + w.dz + w.db);
+  float* part = reinterpret_cast<float*>(ws + w.dz + w.db);
   const bool own = act != E3_ACT_NONE && (dx || dW);  // else dz is dy
   if (own || db) {
     TimedLaunch t_("dense_dz", st);
@@ -253,16 +261,17 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
   const int64_t ldd = own ? N : lddy;
   if (dx) {
     DenseArgs a{};
-    a.a = d, a.a_row = ldd, a.a_red = 1, a.b = W, a.b_red = 1, a.b_col = N, a.rows = M, a.cols = (int)K, a.red = N;
+    a.a = {d, ldd, nullptr, nullptr}, a.b = {W, N, nullptr, nullptr}, a.rows = M, a.cols = (int)K, a.red = N;
     a.y = dx, a.ldy = lddx;
-    const e3_status s = dense_product<T>(a, 1, nullptr, "dense_bwd_dx", st);
+    const e3_status s = dense_product<T, kAlong, kAlong, false>(a, part, "dense_bwd_dx", st);
     if (s != E3_OK) return s;
   }
   if (dW) {
     DenseArgs a{};
-    a.a = x.x, a.a_row = 1, a.a_red = x.ld, a.aq = x.x ? nullptr : x.q, a.ac = x.c, a.packed_cols = (int)K;
-    a.b = d, a.b_red = ldd, a.b_col = 1, a.rows = K, a.cols = (int)N, a.red = M, a.y = dW, a.ldy = N;
-    return dense_product<T>(a, w.dw_splits, dwp, "dense_bwd_dw", st);
+    a.a = {x.x, x.ld, x.q, x.c}, a.width = (int)K, a.b = {d, ldd, nullptr, nullptr};
+    a.rows = K, a.cols = (int)N, a.red = M, a.y = dW, a.ldy = N;
+    return x.x ? dense_product<T, kAcross, kAcross, false>(a, part, "dense_bwd_dw", st)
+               : dense_product<T, kAcross, kAcross, true>(a, part, "dense_bwd_dw", st);
   }
   return E3_OK;
 }
@@ -310,14 +319,13 @@ e3_status e3_dense_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* W
   if (ws_bytes < need) return E3_ERR_WORKSPACE_TOO_SMALL;
   if (need && (!ws || misaligned(E3_F32, ws))) return E3_ERR_INVALID_ARG;
   DenseArgs a{};
-  a.a = x, a.a_row = ldx, a.a_red = 1, a.b = W, a.b_red = N, a.b_col = 1, a.rows = M, a.cols = (int)N, a.red = K;
+  a.a = {x, ldx, nullptr, nullptr}, a.b = {W, N, nullptr, nullptr}, a.rows = M, a.cols = (int)N, a.red = K;
   a.bias = bias, a.res = res, a.ldr = ldr, a.act = act, a.y = y, a.ldy = ldy, a.z = z, a.ldz = ldz, a.zq = zq;
   a.zc = zc, a.yq = yq, a.yc = yc;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  const int64_t splits = dense_splits(tiles(M) * tiles(N), K);
   float* part = static_cast<float*>(ws);
-  return dtype == E3_F32 ? dense_product<float>(a, splits, part, "dense_fwd", st)
-                         : dense_product<__bf16>(a, splits, part, "dense_fwd", st);
+  return dtype == E3_F32 ? dense_product<float, kAlong, kAcross, false>(a, part, "dense_fwd", st)
+                         : dense_product<__bf16, kAlong, kAcross, false>(a, part, "dense_fwd", st);
 }
 
 e3_status e3_dense_bwd(e3_dtype dtype, const void* x, int64_t ldx, const int8_t* xq, const uint8_t* xc, const void* W,

@@ -1,0 +1,315 @@
+// The tile product behind the dense layers, on the bf16 matrix cores.
+//
+// A workgroup takes a BM x BN tile of the output; the reduction runs in steps of
+// BK.  Per step the threads load both operands' pieces of 16 bytes into
+// registers (the next step's are in flight during the instructions) and write
+// them to LDS as bf16; waves read fragments for v_mfma_f32_32x32x16_bf16, in
+// which lane l holds row (or column) l % 32 at reduction indexes 8 (l / 32) on.
+//
+// An operand lies in memory either with its reduction contiguous (kAlong: x of
+// the forward, dz and W of dx) or with its rows or columns contiguous (kAcross:
+// W of the forward, x and dz of dW).  LDS keeps the order of memory, so global
+// loads and LDS writes are whole pieces either way: fragments of the first come
+// by 16-byte reads, of the second by ds_read_b64_tr_b16, where 16 lanes read
+// four rows of 16 values and receive a column each.
+//
+// float32 operands are split into three bf16 terms of 8 bits each with their
+// signs, h + m + l = x exactly, in three planes; a product is the six term
+// products down to 2^-24 of it (hl, lh, mm, hm, mh, hh, added smallest first in
+// one chain).  The bf16 units run 16 times as fast as the float32 ones, so six
+// products on them beat one there.  Terms are scaled by 2^24, so that none of a
+// normal operand is subnormal (the instruction takes those as zero), and sums
+// scaled back; a sum that is not finite then (an infinity or a NaN among the
+// operands, an operand past 2e31, a sum past 1e24) is computed again from memory
+// in float32.  8-bit operands are exact in one term: three products.
+#pragma once
+#include "layers.h"
+
+namespace {
+
+typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+enum Form { kAlong, kAcross };
+
+constexpr float kTermScale = 0x1p24f, kTermBack = 0x1p-48f;
+
+__device__ __forceinline__ unsigned pack2(float a, float b) {
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(f2v{a, b}, bf2v));
+}
+// The terms of a and b, packed; a and b become what the terms so far leave.
+__device__ __forceinline__ unsigned term2(float& a, float& b) {
+  const unsigned t = pack2(a, b);
+  a -= __uint_as_float(t << 16), b -= __uint_as_float(t & 0xffff0000u);
+  return t;
+}
+
+// One operand of a tile product.
+struct Side {
+  const void* p;      // full: rows (kAlong: output index, kAcross: reduction index) at p + i ld
+  int64_t ld;
+  const int8_t* q;    // packed (p null)
+  const uint8_t* c;
+};
+
+// LDS planes of R rows (or columns) by BK reduction indexes.  16-byte slots are
+// exchanged so that the lanes of one pass of a read cover all banks: along, by
+// the row's number among those that share the banks; across, the pairs of slots
+// of the four rows that one transposing read takes.
+template <Form F, int R, int BK, int P>
+struct Plane {
+  static constexpr int W = F == kAlong ? BK : R;          // values of an LDS row
+  static constexpr int S = W / 8;                         // slots of one
+  static constexpr int kShare = F == kAlong ? (S >= 16 ? 1 : 16 / S) : 1;  // rows over all banks
+  unsigned short v[P][R * BK];
+  static __device__ __forceinline__ int off(int row, int slot) {
+    const int x = F == kAlong ? (row / kShare) & (S - 1 < 7 ? S - 1 : 7) : (2 * (row & 3)) & (S - 1);
+    return row * W + ((slot ^ x) * 8);
+  }
+  // The fragment of rows (columns) r0 + l % 32 at reduction indexes k0 + 8 (l / 32) on.
+  __device__ __forceinline__ bf8v frag(int p, int r0, int k0) const {
+    const int l = threadIdx.x % kWave;
+    if constexpr (F == kAlong) {
+      return *reinterpret_cast<const bf8v*>(&v[p][off(r0 + l % 32, k0 / 8 + l / 32)]);
+    } else {
+      typedef __attribute__((address_space(3))) s4v* lds;
+      const int k = k0 + 8 * (l / 32) + (l % 16) / 4, col = r0 + 16 * ((l / 16) % 2) + 4 * (l % 4);
+      union {
+        s4v h[2];
+        bf8v f;
+      } u;
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(&v[p][off(k, col / 8) + col % 8]));
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(&v[p][off(k + 4, col / 8) + col % 8]));
+      return u.f;
+    }
+  }
+};
+
+// Loads of one operand's tile: N pieces a thread, of V values of memory rows.
+template <class T, Form F, int R, int BK, int THREADS, bool Q>
+struct Loader {
+  static constexpr int V = Elem<T>::V;
+  static constexpr int P = sizeof(T) == 2 || Q ? 1 : 3;   // planes
+  using Lds = Plane<F, R, BK, P>;
+  static constexpr int PER = Lds::W / V;                  // pieces of a memory row
+  static constexpr int N = R * BK / V / THREADS;
+  static_assert(N * V * THREADS == R * BK && THREADS % PER == 0);
+  typename std::conditional<Q, typename std::conditional<V == 4, unsigned, u2v>::type, typename Elem<T>::vec>::type raw[N];
+  unsigned char exps[Q ? N : 1];
+
+  static __device__ __forceinline__ int row_of(int i) { return threadIdx.x / PER + i * (THREADS / PER); }
+  static __device__ __forceinline__ int col_of() { return threadIdx.x % PER * V; }
+
+  // The tile at output index r0 and reduction index k0 of an operand with `rows`
+  // output indexes; reduction indexes from `end` on are zero, output indexes
+  // past the end read as the last row (along) or zero (across): their results
+  // are not stored.
+  __device__ __forceinline__ void load(const Side& s, int64_t r0, int64_t rows, int64_t k0, int64_t end, int width) {
+    const int64_t m0 = F == kAlong ? r0 : k0;              // memory row and column of the tile
+    const int64_t c0 = (F == kAlong ? k0 : r0) + col_of();
+    const int64_t mend = F == kAlong ? rows : end, cend = F == kAlong ? end : rows;
+    const bool whole = (F == kAlong || k0 + BK <= end) && (F == kAlong ? k0 : r0) + Lds::W <= cend;
+    if constexpr (Q) {
+      const int groups = (width + kGroup - 1) / kGroup;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        int64_t m = m0 + row_of(i);
+        const bool in = m < mend && c0 < cend;
+        if (F == kAlong && m >= mend) m = mend - 1;
+        if constexpr (V == 4) raw[i] = 0u; else raw[i] = u2v{0u, 0u};
+        exps[i] = 0;
+        if (!whole && !in) continue;
+        const int8_t* q = s.q + m * width + c0;
+        exps[i] = s.c[m * groups + c0 / kGroup];
+        if (whole || c0 + V <= cend) {
+          raw[i] = *reinterpret_cast<const typename Bytes<V>::vec*>(q);
+        } else {
+          unsigned w[2] = {0, 0};
+          for (int e = 0; e < (int)(cend - c0); ++e) w[e / 4] |= (unsigned)(uint8_t)q[e] << (8 * (e % 4));
+          if constexpr (V == 4) raw[i] = w[0]; else raw[i] = u2v{w[0], w[1]};
+        }
+      }
+    } else {
+      const T* p = static_cast<const T*>(s.p);
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          int64_t m = m0 + row_of(i);
+          if (F == kAlong && m >= mend) m = mend - 1;
+          raw[i] = *reinterpret_cast<const typename Elem<T>::vec*>(p + m * s.ld + c0);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          int64_t m = m0 + row_of(i);
+          int64_t n = m < mend ? cend - c0 : F == kAlong ? cend - c0 : 0;
+          if (F == kAlong && m >= mend) m = mend - 1;
+          float v[V];
+          ld_piece<T>(p + m * s.ld + c0, n < V ? (int)(n < 0 ? 0 : n) : V, v);
+          raw[i] = Elem<T>::put(v);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void store(Lds& l) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int row = row_of(i), col = col_of();
+      const int o = Lds::off(row, col / 8) + col % 8;
+      if constexpr (!Q && sizeof(T) == 2) {
+        *reinterpret_cast<u4v*>(&l.v[0][o]) = raw[i];
+      } else if constexpr (Q) {
+        // q and the step are exact in bf16; float32 tiles are scaled
+        const float st = step8(exps[i]) * (sizeof(T) == 4 ? kTermScale : 1.0f);
+        unsigned w[V / 4], b[V / 2];
+        if constexpr (V == 4) w[0] = raw[i]; else w[0] = raw[i].x, w[1] = raw[i].y;
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) {
+          const unsigned t = w[e / 2] >> (16 * (e % 2));
+          b[e] = pack2((float)(int)(int8_t)t * st, (float)(int)(int8_t)(t >> 8) * st);
+        }
+        if constexpr (V == 4) *reinterpret_cast<u2v*>(&l.v[0][o]) = u2v{b[0], b[1]};
+        else *reinterpret_cast<u4v*>(&l.v[0][o]) = u4v{b[0], b[1], b[2], b[3]};
+      } else {
+        float a = raw[i][0] * kTermScale, b = raw[i][1] * kTermScale;
+        float c = raw[i][2] * kTermScale, d = raw[i][3] * kTermScale;
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+          const unsigned x = term2(a, b), y = term2(c, d);
+          *reinterpret_cast<u2v*>(&l.v[t][o]) = u2v{x, y};
+        }
+      }
+    }
+  }
+};
+
+// The tile and its reduction.  WM x WN waves; acc[i][j]: rows 32 i on and
+// columns 32 j on of the wave's part; the columns take the instruction's A side,
+// so that a lane holds row l % 32 and columns 8 (e / 4) + 4 (l / 32) + e % 4.
+template <class T, Form FA, Form FB, int BM, int BN, int BK, int WM, int WN, bool QA, int BUFS>
+struct Tile {
+  static constexpr int THREADS = WM * WN * kWave, TM = BM / WM, TN = BN / WN, RM = TM / 32, RN = TN / 32;
+  using LA = Loader<T, FA, BM, BK, THREADS, QA>;
+  using LB = Loader<T, FB, BN, BK, THREADS, false>;
+  static constexpr int PITCH = TN + 4;                    // floats of a row of the results' staging
+  union Shared {
+    struct {
+      typename LA::Lds a;
+      typename LB::Lds b;
+    } in[BUFS];
+    float out[WM * WN][32][PITCH];
+  };
+  static constexpr float kBack = sizeof(T) == 2 ? 1.0f : kTermBack;
+
+  f16v acc[RM][RN];
+
+  __device__ __forceinline__ void step(const typename LA::Lds& a, const typename LB::Lds& b, int row0, int col0) {
+    constexpr int PA = LA::P, PB = LB::P;
+#pragma unroll
+    for (int k = 0; k < BK; k += 16) {
+      bf8v x[PA][RM], y[PB][RN];
+#pragma unroll
+      for (int p = 0; p < PA; ++p)
+#pragma unroll
+        for (int i = 0; i < RM; ++i) x[p][i] = a.frag(p, row0 + 32 * i, k);
+#pragma unroll
+      for (int p = 0; p < PB; ++p)
+#pragma unroll
+        for (int j = 0; j < RN; ++j) y[p][j] = b.frag(p, col0 + 32 * j, k);
+      // pairs of terms, smallest products first
+#pragma unroll
+      for (int s = PA + PB - 2 < 2 ? PA + PB - 2 : 2; s >= 0; --s)
+#pragma unroll
+        for (int p = 0; p < PA; ++p) {
+          const int q = s - p;
+          if (q < 0 || q >= PB) continue;
+#pragma unroll
+          for (int i = 0; i < RM; ++i)
+#pragma unroll
+            for (int j = 0; j < RN; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[q][j], x[p][i], acc[i][j], 0, 0, 0);
+        }
+    }
+  }
+
+  // Sums over reduction indexes [k0, end) of the tile at (r0, c0) of rows x cols.
+  __device__ __forceinline__ void run(Shared& sh, const Side& sa, const Side& sb, int64_t r0, int64_t rows, int c0,
+                                      int cols, int64_t k0, int64_t end, int width) {
+    const int w = uniform(threadIdx.x / kWave), row0 = w / WN * TM, col0 = w % WN * TN;
+#pragma unroll
+    for (int i = 0; i < RM; ++i)
+#pragma unroll
+      for (int j = 0; j < RN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    LA la;
+    LB lb;
+    la.load(sa, r0, rows, k0, end, width);
+    lb.load(sb, c0, cols, k0, end, 0);
+    if constexpr (BUFS == 2) {
+      la.store(sh.in[0].a), lb.store(sh.in[0].b);
+      int cur = 0;
+      for (int64_t k = k0; k < end; k += BK) {
+        __syncthreads();
+        const bool more = k + BK < end;
+        if (more) {
+          la.load(sa, r0, rows, k + BK, end, width);
+          lb.load(sb, c0, cols, k + BK, end, 0);
+        }
+        step(sh.in[cur].a, sh.in[cur].b, row0, col0);
+        if (more) la.store(sh.in[cur ^ 1].a), lb.store(sh.in[cur ^ 1].b);
+        cur ^= 1;
+      }
+    } else {
+      for (int64_t k = k0; k < end; k += BK) {
+        la.store(sh.in[0].a), lb.store(sh.in[0].b);
+        __syncthreads();
+        if (k + BK < end) {
+          la.load(sa, r0, rows, k + BK, end, width);
+          lb.load(sb, c0, cols, k + BK, end, 0);
+        }
+        step(sh.in[0].a, sh.in[0].b, row0, col0);
+        __syncthreads();
+      }
+    }
+  }
+
+  // Hands the results out as pieces of V values of a row, f(row, col, v) with row
+  // and col within the tile; the lanes of a wave hold consecutive pieces.  Every
+  // wave goes through memory of its own.
+  template <class Fn>
+  __device__ __forceinline__ void finish(Shared& sh, Fn&& f) {
+    constexpr int V = Elem<T>::V, PER = TN / V, PASS = kWave / PER;
+    static_assert(kWave % PER == 0 && 32 % PASS == 0);
+    const int w = uniform(threadIdx.x / kWave), row0 = w / WN * TM, col0 = w % WN * TN, l = threadIdx.x % kWave;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RM; ++i) {
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int j = 0; j < RN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f4v*>(&sh.out[w][l % 32][32 * j + 8 * g + 4 * (l / 32)]) =
+              f4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+      // the wave's own writes: LDS serves a wave's accesses in order
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int r = 0; r < 32; r += PASS) {
+        const int row = r + l / PER, col = l % PER * V;
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; e += 4) {
+          const f4v t = *reinterpret_cast<const f4v*>(&sh.out[w][row][col + e]);
+          v[e] = t.x * kBack, v[e + 1] = t.y * kBack, v[e + 2] = t.z * kBack, v[e + 3] = t.w * kBack;
+        }
+        f(row0 + 32 * i + row, col0 + col, v);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+};
+
+}  // namespace
