@@ -112,7 +112,7 @@ template <class T>
 __global__ __launch_bounds__(256) void k_dense_join(DenseArgs a, int splits) {
   constexpr int V = Elem<T>::V;
   const int per = (a.cols + kGroup - 1) / kGroup * (kGroup / V);
-  const int64_t i = block_id() * 256 + threadIdx.x, row = i / per;
+  const int64_t i = block_id() * 256 + threadIdx.x, row = div_small(i, per);
   const int col = (int)(i - row * per) * V;
   const bool ok = row < a.rows;
   float v[V] = {};

@@ -9,6 +9,11 @@ typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
 typedef unsigned u2v __attribute__((ext_vector_type(2)));
 typedef unsigned u4v __attribute__((ext_vector_type(4)));
 
+// i / n of block-uniformly small i by a 32-bit division, a few times cheaper.
+__device__ __forceinline__ int64_t div_small(int64_t i, int64_t n) {
+  return block_id() < (1 << 23) && n < (1 << 30) ? (int64_t)((unsigned)i / (unsigned)n) : i / n;
+}
+
 // ------------------------------------------------------------ element types
 // A lane's piece of a row is 16 bytes: V values of the type.  Rows start at
 // any element (odd widths, slices of wider tensors), so the vector types claim
@@ -58,6 +63,15 @@ __device__ __forceinline__ void ld_piece(const T* p, int n, float (&v)[Elem<T>::
 #pragma unroll
     for (int i = 0; i < Elem<T>::V; ++i) v[i] = i < n ? Elem<T>::one(p[i]) : 0.0f;
   }
+}
+// The same as they lie in memory.
+template <class T>
+__device__ __forceinline__ typename Elem<T>::vec ld_raw(const T* p, int n) {
+  if (n >= Elem<T>::V) return *reinterpret_cast<const typename Elem<T>::vec*>(p);
+  float v[Elem<T>::V];
+#pragma unroll
+  for (int i = 0; i < Elem<T>::V; ++i) v[i] = i < n ? Elem<T>::one(p[i]) : 0.0f;
+  return Elem<T>::put(v);
 }
 template <class T>
 __device__ __forceinline__ void st_piece(T* p, int n, const float (&v)[Elem<T>::V]) {
@@ -167,32 +181,37 @@ __device__ __forceinline__ void pack8_piece(const float (&v)[V], int col, int n,
   if (col % kGroup == 0) c[col / kGroup] = (uint8_t)e;
 }
 
-// V packed values at column col (n inside the row; the rest read as zero).
+// V packed values at column col of a row (n inside it; the rest zero) and their
+// group's exponent byte, as they lie in memory.
 template <int V>
-__device__ __forceinline__ void unpack8_piece(const int8_t* q, const uint8_t* c, int col, int n, float (&v)[V]) {
-  if (n <= 0) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = 0.0f;
-    return;
-  }
-  const float s = step8(c[col / kGroup]);
+struct Raw8 {
   unsigned w[V / 4];
+  unsigned e;
+};
+template <int V>
+__device__ __forceinline__ Raw8<V> ld_raw8(const int8_t* q, const uint8_t* c, int col, int n) {
+  Raw8<V> r{};
+  if (n <= 0) return r;
+  r.e = c[col / kGroup];
   if (n >= V) {
     if constexpr (V == 4) {
-      w[0] = *reinterpret_cast<const typename Bytes<4>::vec*>(q + col);
+      r.w[0] = *reinterpret_cast<const typename Bytes<4>::vec*>(q + col);
     } else {
       const u2v t = *reinterpret_cast<const typename Bytes<8>::vec*>(q + col);
-      w[0] = t.x, w[1] = t.y;
+      r.w[0] = t.x, r.w[1] = t.y;
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (i % 4 == 0) w[i / 4] = 0;
-      if (i < n) w[i / 4] |= ((unsigned)(uint8_t)q[col + i]) << (8 * (i % 4));
-    }
+    for (int i = 0; i < V; ++i)
+      if (i < n) r.w[i / 4] |= ((unsigned)(uint8_t)q[col + i]) << (8 * (i % 4));
   }
+  return r;
+}
+template <int V>
+__device__ __forceinline__ void get8(const Raw8<V>& r, float (&v)[V]) {
+  const float s = step8(r.e);
 #pragma unroll
-  for (int i = 0; i < V; ++i) v[i] = i < n ? (float)(int)(int8_t)(w[i / 4] >> (8 * (i % 4))) * s : 0.0f;
+  for (int i = 0; i < V; ++i) v[i] = (float)(int)(int8_t)(r.w[i / 4] >> (8 * (i % 4))) * s;
 }
 
 // Values of a row that is kept in full or packed (x null).
@@ -202,13 +221,22 @@ struct RowsIn {
   int64_t ld;
   const int8_t* q;
   const uint8_t* c;
+  // One of the two, known at compile time, as it lies in memory.
+  template <bool Q>
+  using Raw = typename std::conditional<Q, Raw8<Elem<T>::V>, typename Elem<T>::vec>::type;
+  template <bool Q>
+  __device__ __forceinline__ Raw<Q> raw(int64_t row, int col, int cols) const {
+    if constexpr (Q) return ld_raw8<Elem<T>::V>(q + row * cols, c + row * ((cols + kGroup - 1) / kGroup), col, cols - col);
+    else return ld_raw<T>(x + row * ld + col, cols - col);
+  }
+  template <bool Q>
+  static __device__ __forceinline__ void get(const Raw<Q>& r, float (&v)[Elem<T>::V]) {
+    if constexpr (Q) get8(r, v);
+    else Elem<T>::get(r, v);
+  }
   __device__ __forceinline__ void load(int64_t row, int col, int cols, float (&v)[Elem<T>::V]) const {
-    const int n = cols - col;
-    if (x) {
-      ld_piece<T>(x + row * ld + col, n, v);
-    } else {
-      unpack8_piece<Elem<T>::V>(q + row * cols, c + row * ((cols + kGroup - 1) / kGroup), col, n, v);
-    }
+    if (x) get<false>(raw<false>(row, col, cols), v);
+    else get<true>(raw<true>(row, col, cols), v);
   }
 };
 
@@ -233,24 +261,28 @@ __device__ __forceinline__ float act_grad(int act, float z) {
 
 // ------------------------------------------------------------ column sums
 // out_s[col] = sum over p of part[p][s][col], s = 0, 1 (either output may be
-// null), in a fixed order: 16 threads of a column take every 16th partial, then
-// their sums are added in order.
+// null), in a fixed order: 32 threads of a column take every 32nd partial in
+// eight running sums (loads of 16 columns are in flight together: latency is all
+// there is to it), then their sums are added in order.
 template <class T>
-__global__ __launch_bounds__(256) void k_column_sums(const float* part, int parts, int sets, int cols, T* out0,
+__global__ __launch_bounds__(512) void k_column_sums(const float* part, int parts, int sets, int cols, T* out0,
                                                      T* out1) {
-  __shared__ float s[16][17];
+  __shared__ float s[32][17];
   const int c = threadIdx.x % 16, p0 = threadIdx.x / 16, col = (int)blockIdx.x * 16 + c, set = blockIdx.y;
   T* out = set ? out1 : out0;
   if (!out) return;
-  float v = 0.0f;
+  float t[8] = {};
   if (col < cols)
-    for (int p = p0; p < parts; p += 16) v += part[((int64_t)p * sets + set) * cols + col];
-  s[p0][c] = v;
+    for (int p = p0; p < parts; p += 256)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (p + 32 * i < parts) t[i] += part[((int64_t)(p + 32 * i) * sets + set) * cols + col];
+  s[p0][c] = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
   __syncthreads();
   if (p0 != 0 || col >= cols) return;
-  v = 0.0f;
+  float v = 0.0f;
 #pragma unroll
-  for (int p = 0; p < 16; ++p) v += s[p][c];
+  for (int p = 0; p < 32; ++p) v += s[p][c];
   out[col] = (T)v;
 }
 
@@ -259,10 +291,10 @@ inline e3_status column_sums(e3_dtype dtype, const float* part, int parts, int s
   TimedLaunch t_("column_sums", st);
   const dim3 grid((cols + 15) / 16, sets);
   if (dtype == E3_F32)
-    hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(256), 0, st, part, parts, sets, cols,
+    hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(512), 0, st, part, parts, sets, cols,
                        static_cast<float*>(out0), static_cast<float*>(out1));
   else
-    hipLaunchKernelGGL(k_column_sums<__bf16>, grid, dim3(256), 0, st, part, parts, sets, cols,
+    hipLaunchKernelGGL(k_column_sums<__bf16>, grid, dim3(512), 0, st, part, parts, sets, cols,
                        static_cast<__bf16*>(out0), static_cast<__bf16*>(out1));
   E3_HIP(hipGetLastError());
   return E3_OK;

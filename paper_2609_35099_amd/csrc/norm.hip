@@ -47,10 +47,12 @@ __device__ __forceinline__ float row_sum(float v, float* s) {
 }
 
 // J > 0: the row's pieces stay in registers.  J = 0: any width, piece by piece.
+template <int L>
+constexpr int kNormFwdThreads = L <= kNormThreads ? kNormThreads : L;
 template <class T, int L, int J>
-__global__ __launch_bounds__(kNormThreads) void k_norm_fwd(NormArgs a) {
-  constexpr int V = Elem<T>::V, R = kNormThreads / L, U = J > 0 ? J : 1;
-  __shared__ float s[kNormThreads / kWave];
+__global__ __launch_bounds__(kNormFwdThreads<L>) void k_norm_fwd(NormArgs a) {
+  constexpr int V = Elem<T>::V, R = kNormFwdThreads<L> / L, U = J > 0 ? J : 1;
+  __shared__ float s[kNormFwdThreads<L> / kWave];
   const int lane = threadIdx.x % L, cols = a.cols;
   const int64_t row = block_id() * R + threadIdx.x / L;
   if (row >= a.rows) return;  // whole rows leave: no lane of another row's group
@@ -120,46 +122,63 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_fwd(NormArgs a) {
 }
 
 // dx, and per workgroup the sums of dy n and dy over its rows (rows blockIdx.x
-// R + i, then every gridDim.x R).
-template <class T, int L, int J>
-__global__ __launch_bounds__(kNormThreads) void k_norm_bwd(NormArgs a) {
-  constexpr int V = Elem<T>::V, R = kNormThreads / L;
-  __shared__ float s[kNormThreads / kWave];
-  __shared__ float fold[R > 1 ? R * L * V : 1];
+// R + i, then every gridDim.x R).  The next row's pieces are in flight while a
+// row is worked on.  Workgroups are large and few, so that little is left for
+// the sum over them: 512 threads where a row takes at most a wave (1,024 leave
+// too few registers), one row where it takes more.
+template <int L>
+constexpr int kNormBwdThreads = L <= kWave ? 512 : L;
+template <class T, int L, int J, bool Q>
+__global__ __launch_bounds__(kNormBwdThreads<L>) void k_norm_bwd(NormArgs a) {
+  constexpr int V = Elem<T>::V, NT = kNormBwdThreads<L>, R = NT / L;
+  using In = RowsIn<T>;
+  __shared__ float s[NT / kWave];
+  __shared__ float fold[R > 1 ? NT * V : 1];
   const int lane = threadIdx.x % L, cols = a.cols;
-  const RowsIn<T> xs{static_cast<const T*>(a.x), a.ldx, a.xq_in, a.xc_in};
+  const In xs{static_cast<const T*>(a.x), a.ldx, a.xq_in, a.xc_in};
+  const T* dyp = static_cast<const T*>(a.dy);
   const T* gamma = static_cast<const T*>(a.gamma);
-  float dg[J][V] = {}, db[J][V] = {}, g[J][V];
+  float dg[J][V] = {}, db[J][V] = {};
+  const int64_t stride = (int64_t)gridDim.x * R;
+  int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L;
+  typename In::template Raw<Q> xr[J];
+  typename Elem<T>::vec dr[J], gr[J];
+  if (gamma)
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int col = (j * L + lane) * V;
-    if (gamma) {
-      ld_piece<T>(gamma + col, cols - col, g[j]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) g[j][i] = i < cols - col ? 1.0f : 0.0f;
-    }
-  }
-  for (int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L; row < a.rows; row += (int64_t)gridDim.x * R) {
-    float x[J][V], dy[J][V];
+    for (int j = 0; j < J; ++j) gr[j] = ld_raw<T>(gamma + (j * L + lane) * V, cols - (j * L + lane) * V);
+  float mean = 0.0f, rstd = 0.0f;
+  auto load = [&](int64_t r) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int col = (j * L + lane) * V;
-      xs.load(row, col, cols, x[j]);
-      ld_piece<T>(static_cast<const T*>(a.dy) + row * a.ldy + col, cols - col, dy[j]);
+      xr[j] = xs.template raw<Q>(r, col, cols);
+      dr[j] = ld_raw<T>(dyp + r * a.ldy + col, cols - col);
     }
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    mean = a.mean[r], rstd = a.rstd[r];
+  };
+  if (row < a.rows) load(row);
+  for (; row < a.rows; row += stride) {
+    float x[J][V], dy[J][V];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      In::template get<Q>(xr[j], x[j]);
+      Elem<T>::get(dr[j], dy[j]);
+    }
+    const float m = mean, rs = rstd;
+    if (row + stride < a.rows) load(row + stride);
     float c0 = 0.0f, c1 = 0.0f;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int n = cols - (j * L + lane) * V;
+      const int col = (j * L + lane) * V, n = cols - col;
+      float g[V];
+      if (gamma) Elem<T>::get(gr[j], g);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        // columns past the end have dy = g = 0: x there must not turn them into NaN
-        x[j][i] = i < n ? (x[j][i] - mean) * rstd : 0.0f;
+        // columns past the end have dy = 0: x there must not turn them into NaN
+        x[j][i] = i < n ? (x[j][i] - m) * rs : 0.0f;
         dg[j][i] += dy[j][i] * x[j][i];
         db[j][i] += dy[j][i];
-        dy[j][i] *= g[j][i];
+        if (gamma) dy[j][i] *= g[i];
         c0 += dy[j][i];
         c1 += dy[j][i] * x[j][i];
       }
@@ -171,7 +190,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_bwd(NormArgs a) {
       for (int j = 0; j < J; ++j) {
         const int col = (j * L + lane) * V;
 #pragma unroll
-        for (int i = 0; i < V; ++i) dy[j][i] = rstd * (dy[j][i] - c0 - x[j][i] * c1);
+        for (int i = 0; i < V; ++i) dy[j][i] = rs * (dy[j][i] - c0 - x[j][i] * c1);
         st_piece<T>(static_cast<T*>(a.dx) + row * a.lddx + col, cols - col, dy[j]);
       }
     }
@@ -281,7 +300,7 @@ __global__ __launch_bounds__(256) void k_pack8(const T* x, int64_t ldx, int8_t* 
   constexpr int V = Elem<T>::V;
   const int groups = (cols + kGroup - 1) / kGroup;
   const int64_t per = (int64_t)groups * (kGroup / V);
-  const int64_t i = block_id() * 256 + threadIdx.x, row = i / per;
+  const int64_t i = block_id() * 256 + threadIdx.x, row = div_small(i, per);
   const int col = (int)(i - row * per) * V, n = row < rows ? cols - col : 0;
   float v[V];
   if (n > 0) ld_piece<T>(x + row * ldx + col, n, v);
@@ -293,11 +312,11 @@ __global__ __launch_bounds__(256) void k_unpack8(const int8_t* q, const uint8_t*
   constexpr int V = Elem<T>::V;
   const int groups = (cols + kGroup - 1) / kGroup;
   const int64_t per = (cols + V - 1) / V;
-  const int64_t i = block_id() * 256 + threadIdx.x, row = i / per;
+  const int64_t i = block_id() * 256 + threadIdx.x, row = div_small(i, per);
   if (row >= rows) return;
   const int col = (int)(i - row * per) * V, n = cols - col;
   float v[V];
-  unpack8_piece<V>(q + row * cols, c + row * groups, col, n, v);
+  get8(ld_raw8<V>(q + row * cols, c + row * groups, col, n), v);
   st_piece<T>(x + row * ldx + col, n, v);
 }
 
@@ -314,20 +333,21 @@ auto norm_shape(int cols, F&& f) {
   E3_SHAPE(32, 1);
   E3_SHAPE(64, 1);
   E3_SHAPE(64, 2);
-  E3_SHAPE(64, 4);
+  E3_SHAPE(64, 3);
+  E3_SHAPE(256, 1);
   E3_SHAPE(256, 2);
-  E3_SHAPE(256, 4);
-  E3_SHAPE(256, 8);
+  E3_SHAPE(256, 3);
+  E3_SHAPE(512, 2);
+  E3_SHAPE(512, 4);
 #undef E3_SHAPE
   return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 0>{});
 }
 
-// Workgroups of the backward: enough to fill the card, each at least one round of rows.
-constexpr int kNormBlocks = 1024;
+// Workgroups of the backward: two per CU, each at least one round of rows.
 int norm_blocks(e3_dtype t, int64_t rows, int cols) {
   auto of = [&](auto L, auto J) {
-    constexpr int R = decltype(J)::value > 0 ? kNormThreads / decltype(L)::value : 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(kNormBlocks, (rows + R - 1) / R));
+    constexpr int l = decltype(L)::value, R = decltype(J)::value > 0 ? kNormBwdThreads<l> / l : 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(512, (rows + R - 1) / R));
   };
   return t == E3_F32 ? norm_shape<float>(cols, of) : norm_shape<__bf16>(cols, of);
 }
@@ -335,9 +355,9 @@ int norm_blocks(e3_dtype t, int64_t rows, int cols) {
 template <class T>
 e3_status norm_fwd(const NormArgs& a, hipStream_t st) {
   return norm_shape<T>(a.cols, [&](auto L, auto J) -> e3_status {
-    constexpr int l = decltype(L)::value, j = decltype(J)::value, R = kNormThreads / l;
+    constexpr int l = decltype(L)::value, j = decltype(J)::value, R = kNormFwdThreads<l> / l;
     TimedLaunch t_("layer_norm_fwd", st);
-    hipLaunchKernelGGL((k_norm_fwd<T, l, j>), grid_of((a.rows + R - 1) / R), dim3(kNormThreads), 0, st, a);
+    hipLaunchKernelGGL((k_norm_fwd<T, l, j>), grid_of((a.rows + R - 1) / R), dim3(kNormFwdThreads<l>), 0, st, a);
     E3_HIP(hipGetLastError());
     return E3_OK;
   });
@@ -349,7 +369,8 @@ e3_status norm_bwd(const NormArgs& a, hipStream_t st) {
     constexpr int l = decltype(L)::value, j = decltype(J)::value;
     if constexpr (j > 0) {
       TimedLaunch t_("layer_norm_bwd", st);
-      hipLaunchKernelGGL((k_norm_bwd<T, l, j>), dim3(a.blocks), dim3(kNormThreads), 0, st, a);
+      auto* k = a.x ? k_norm_bwd<T, l, j, false> : k_norm_bwd<T, l, j, true>;
+      hipLaunchKernelGGL(k, dim3(a.blocks), dim3(kNormBwdThreads<l>), 0, st, a);
       E3_HIP(hipGetLastError());
     } else {
       if (a.dx) {

@@ -8,6 +8,7 @@ first call raises (there is no fallback path).
 from __future__ import annotations
 
 import ctypes as ct
+import functools
 import os
 
 import numpy as np
@@ -161,7 +162,10 @@ def _ptr(t, name, shape=None, dtype="float32"):
 
 
 def _stream(stream):
-    return (_torch().cuda.current_stream() if stream is None else stream).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    c = _torch()._C   # torch.cuda.current_stream().cuda_stream, without the stream object (2.8 us a call)
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
 def _on_stream(fn):
@@ -169,8 +173,6 @@ def _on_stream(fn):
     outputs and the workspace it allocates belong to that stream in torch's
     caching allocator (their memory is not handed out again while the kernels
     launched on that stream may still use it)."""
-    import functools
-
     @functools.wraps(fn)
     def wrapped(*args, stream=None, **kw):
         if stream is None:
@@ -811,13 +813,12 @@ def layer_norm_fwd(x, gamma=None, beta=None, eps: float = 1e-5, keep=(), out=Non
     code, dt = _layer_dtype(x, "x")
     m, n = shape = _matrix(x, "x")
     _keep_of(keep, ("stats", "x8", "y8"))
-    torch = _torch()
-    y = torch.empty((m, n), dtype=x.dtype, device="cuda") if out is None else out
+    y = x.new_empty(shape) if out is None else out
     got, mean, rstd, xp, yp = [y], None, None, (None, None), (None, None)
     if "stats" in keep:
-        mean, rstd = _empty((m,)), _empty((m,))
-        got += [mean, rstd]
-        mean, rstd = _ptr(mean, "mean"), _ptr(rstd, "rstd")
+        stats = _empty((2, m)).unbind(0)
+        got += stats
+        mean, rstd = (t.data_ptr() for t in stats)
     if "x8" in keep:
         got.append(Packed8.empty(m, n))
         xp = _packed(got[-1], "x8", shape)
@@ -832,6 +833,7 @@ def layer_norm_fwd(x, gamma=None, beta=None, eps: float = 1e-5, keep=(), out=Non
     return tuple(got) if keep else y
 
 
+@functools.lru_cache(maxsize=1024)   # a function of the sizes alone
 def layer_norm_workspace_size(rows: int, cols: int, dtype="float32") -> int:
     b = ct.c_size_t()
     _check(lib().e3_layer_norm_workspace_size({"float32": 0, "bfloat16": 1}[dtype], rows, cols, ct.byref(b)),
@@ -846,11 +848,10 @@ def layer_norm_bwd(x, gamma, dy, mean, rstd, want=("dx", "dgamma", "dbeta"), dx=
     code, dt = _layer_dtype(dy, "dy")
     m, n = shape = _matrix(dy, "dy")
     _keep_of(want, ("dx", "dgamma", "dbeta"))
-    torch = _torch()
     if "dx" in want and dx is None:
-        dx = torch.empty((m, n), dtype=dy.dtype, device="cuda")
-    dg = torch.empty((n,), dtype=dy.dtype, device="cuda") if "dgamma" in want else None
-    db = torch.empty((n,), dtype=dy.dtype, device="cuda") if "dbeta" in want else None
+        dx = dy.new_empty(shape)
+    dg = dy.new_empty((n,)) if "dgamma" in want else None
+    db = dy.new_empty((n,)) if "dbeta" in want else None
     if ws is None and (dg is not None or db is not None):
         ws = workspace(layer_norm_workspace_size(m, n, dt))
     xp, ldx, xq, xc = _kept(x, "x", shape, dt)
@@ -863,6 +864,7 @@ def layer_norm_bwd(x, gamma, dy, mean, rstd, want=("dx", "dgamma", "dbeta"), dx=
     return dx, dg, db
 
 
+@functools.lru_cache(maxsize=1024)
 def dense_workspace_size(M: int, K: int, N: int, dtype="float32"):
     """Bytes of (forward, backward)."""
     f, b = ct.c_size_t(), ct.c_size_t()
@@ -891,12 +893,11 @@ def dense_fwd(x, W, bias=None, res=None, act: str = "none", keep=(), out=None, w
         raise ValueError(f"W has shape {tuple(W.shape)}, expected {K} rows")
     N = W.shape[1]
     _keep_of(keep, ("z", "z8", "y8"))
-    torch = _torch()
     shape = (M, N)
-    y = torch.empty(shape, dtype=x.dtype, device="cuda") if out is None else out
+    y = x.new_empty(shape) if out is None else out
     got, z, zp, yp = [y], None, (None, None), (None, None)
     if "z" in keep:
-        got.append(torch.empty(shape, dtype=x.dtype, device="cuda"))
+        got.append(x.new_empty(shape))
         z = got[-1].data_ptr()
     if "z8" in keep:
         got.append(Packed8.empty(M, N))
@@ -925,11 +926,10 @@ def dense_bwd(x, W, dy, z=None, act: str = "none", want=("dx", "dW", "db"), dx=N
         raise ValueError(f"W has shape {tuple(W.shape)}, expected {N} columns")
     K = W.shape[0]
     _keep_of(want, ("dx", "dW", "db"))
-    torch = _torch()
     if "dx" in want and dx is None:
-        dx = torch.empty((M, K), dtype=dy.dtype, device="cuda")
-    dW = torch.empty((K, N), dtype=dy.dtype, device="cuda") if "dW" in want else None
-    db = torch.empty((N,), dtype=dy.dtype, device="cuda") if "db" in want else None
+        dx = dy.new_empty((M, K))
+    dW = dy.new_empty((K, N)) if "dW" in want else None
+    db = dy.new_empty((N,)) if "db" in want else None
     if ws is None:
         ws = workspace(dense_workspace_size(M, K, N, dt)[1])
     xp, ldx, xq, xc = (None, K, None, None) if x is None else _kept(x, "x", (M, K), dt)
