@@ -10,7 +10,6 @@ struct DenseArgs {
   Side a, b;  // rows of A by columns of B over the reduction
   int64_t rows, red;
   int cols;
-  int width;      // columns of a packed A
   int64_t chunk;  // reduction indexes per split
   int splits;
   float* part;    // partial sums [splits][rows][cols], instead of the epilogue
@@ -38,9 +37,7 @@ __device__ __forceinline__ void dense_tail(const DenseArgs& a, int64_t row, bool
   }
   if (a.z) st_piece<T>(static_cast<T*>(a.z) + row * a.ldz + col, n, v);
   if (a.zq) pack8_piece<V>(v, col, n, a.zq + row * a.cols, a.zc + row * groups);
-  if (a.act != E3_ACT_NONE)
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = act_of(a.act, v[i]);
+  act_piece(a.act, v);
   if (a.res) {
     ld_piece<T>(static_cast<const T*>(a.res) + row * a.ldr + col, n, u);
 #pragma unroll
@@ -55,12 +52,11 @@ __device__ __forceinline__ void dense_tail(const DenseArgs& a, int64_t row, bool
 // A sum again from memory, in float32.
 template <class T, Form FA, Form FB, bool QA>
 __device__ __attribute__((noinline)) float dense_again(const Side& a, const Side& b, int64_t row, int col, int64_t k0,
-                                                       int64_t end, int width) {
+                                                       int64_t end) {
   float sum = 0.0f;
-  const int groups = (width + kGroup - 1) / kGroup;
   for (int64_t k = k0; k < end; ++k) {
     const int64_t m = FA == kAlong ? row : k, c = FA == kAlong ? k : row;
-    const float u = QA ? (float)a.q[m * width + c] * step8(a.c[m * groups + c / kGroup])
+    const float u = QA ? (float)a.q[m * a.ld + c] * step8(a.c[m * a.ldc + c / kGroup])
                        : Elem<T>::one(static_cast<const T*>(a.p)[m * a.ld + c]);
     const float w = Elem<T>::one(static_cast<const T*>(b.p)[FB == kAlong ? col * b.ld + k : k * b.ld + col]);
     sum = fmaf(u, w, sum);
@@ -83,7 +79,7 @@ __global__ __launch_bounds__(WM* WN* kWave, OCC) void k_dense(DenseArgs a) {
   const int c0 = (int)(u % tn) * BN;
   const int64_t k0 = split * a.chunk, end = k0 + a.chunk < a.red ? k0 + a.chunk : a.red;
   Tl t;
-  t.run(sh, a.a, a.b, r0, a.rows, c0, a.cols, k0, end, a.width);
+  t.run(sh, a.a, a.b, r0, a.rows, c0, a.cols, k0, end);
   t.finish(sh, [&](int r, int c, float(&v)[V]) {
     const int64_t row = r0 + r;
     const int col = c0 + c;
@@ -95,7 +91,7 @@ __global__ __launch_bounds__(WM* WN* kWave, OCC) void k_dense(DenseArgs a) {
       if (z != 0.0f)
 #pragma unroll
         for (int e = 0; e < V; ++e)
-          if (e < n && v[e] * 0.0f != 0.0f) v[e] = dense_again<T, FA, FB, QA>(a.a, a.b, row, col + e, k0, end, a.width);
+          if (e < n && v[e] * 0.0f != 0.0f) v[e] = dense_again<T, FA, FB, QA>(a.a, a.b, row, col + e, k0, end);
     }
     if (a.part) {
       float* p = a.part + ((int64_t)split * a.rows + row) * a.cols + col;
@@ -142,8 +138,7 @@ __global__ __launch_bounds__(256) void k_dense_dz(RowsIn<T> z, int act, const T*
     if (act != E3_ACT_NONE) {
       float w[V];
       z.load(row, col, cols, w);
-#pragma unroll
-      for (int i = 0; i < V; ++i) u[i] *= act_grad(act, w[i]);
+      act_grad_piece(act, w, u);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) sum[i] += u[i];
@@ -261,14 +256,14 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
   const int64_t ldd = own ? N : lddy;
   if (dx) {
     DenseArgs a{};
-    a.a = {d, ldd, nullptr, nullptr}, a.b = {W, N, nullptr, nullptr}, a.rows = M, a.cols = (int)K, a.red = N;
+    a.a = {d, ldd}, a.b = {W, N}, a.rows = M, a.cols = (int)K, a.red = N;
     a.y = dx, a.ldy = lddx;
     const e3_status s = dense_product<T, kAlong, kAlong, false>(a, part, "dense_bwd_dx", st);
     if (s != E3_OK) return s;
   }
   if (dW) {
     DenseArgs a{};
-    a.a = {x.x, x.ld, x.q, x.c}, a.width = (int)K, a.b = {d, ldd, nullptr, nullptr};
+    a.a = {x.x, x.x ? x.ld : K, x.q, x.c, (K + kGroup - 1) / kGroup}, a.b = {d, ldd};
     a.rows = K, a.cols = (int)N, a.red = M, a.y = dW, a.ldy = N;
     return x.x ? dense_product<T, kAcross, kAcross, false>(a, part, "dense_bwd_dw", st)
                : dense_product<T, kAcross, kAcross, true>(a, part, "dense_bwd_dw", st);
@@ -319,7 +314,7 @@ e3_status e3_dense_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* W
   if (ws_bytes < need) return E3_ERR_WORKSPACE_TOO_SMALL;
   if (need && (!ws || misaligned(E3_F32, ws))) return E3_ERR_INVALID_ARG;
   DenseArgs a{};
-  a.a = {x, ldx, nullptr, nullptr}, a.b = {W, N, nullptr, nullptr}, a.rows = M, a.cols = (int)N, a.red = K;
+  a.a = {x, ldx}, a.b = {W, N}, a.rows = M, a.cols = (int)N, a.red = K;
   a.bias = bias, a.res = res, a.ldr = ldr, a.act = act, a.y = y, a.ldy = ldy, a.z = z, a.ldz = ldz, a.zq = zq;
   a.zc = zc, a.yq = yq, a.yc = yc;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);

@@ -49,8 +49,9 @@ __device__ __forceinline__ unsigned term2(float& a, float& b) {
 struct Side {
   const void* p;      // full: rows (kAlong: output index, kAcross: reduction index) at p + i ld
   int64_t ld;
-  const int8_t* q;    // packed (p null)
+  const int8_t* q;    // packed (p null): ld values and ldc exponents a row
   const uint8_t* c;
+  int64_t ldc;
 };
 
 // LDS planes of R rows (or columns) by BK reduction indexes.  16-byte slots are
@@ -86,70 +87,98 @@ struct Plane {
   }
 };
 
+// The 16 (8) bytes r moved down by `bits`, zeros from above.
+__device__ __forceinline__ u4v shift_down(u4v r, unsigned bits) {
+  uint64_t lo = (uint64_t)r.y << 32 | r.x, hi = (uint64_t)r.w << 32 | r.z;
+  if (bits & 64) lo = hi, hi = 0;
+  const unsigned b = bits & 63;
+  lo = b ? lo >> b | hi << (64 - b) : lo;
+  hi >>= b;
+  if (bits >= 128) lo = hi = 0;
+  return u4v{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+__device__ __forceinline__ u2v shift_down(u2v r, unsigned bits) {
+  const uint64_t v = bits < 64 ? ((uint64_t)r.y << 32 | r.x) >> bits : 0;
+  return u2v{(unsigned)v, (unsigned)(v >> 32)};
+}
+__device__ __forceinline__ unsigned shift_down(unsigned r, unsigned bits) { return bits < 32 ? r >> bits : 0u; }
+
 // Loads of one operand's tile: N pieces a thread, of V values of memory rows.
 template <class T, Form F, int R, int BK, int THREADS, bool Q>
 struct Loader {
   static constexpr int V = Elem<T>::V;
   static constexpr int P = sizeof(T) == 2 || Q ? 1 : 3;   // planes
+  static constexpr int BITS = Q ? 8 : 8 * sizeof(T);      // of a value
   using Lds = Plane<F, R, BK, P>;
+  using E = typename std::conditional<Q, int8_t, T>::type;
+  using Raw = typename std::conditional<Q, typename std::conditional<V == 4, unsigned, u2v>::type, u4v>::type;
+  typedef Raw Any __attribute__((aligned(sizeof(E))));
   static constexpr int PER = Lds::W / V;                  // pieces of a memory row
   static constexpr int N = R * BK / V / THREADS;
   static_assert(N * V * THREADS == R * BK && THREADS % PER == 0);
-  typename std::conditional<Q, typename std::conditional<V == 4, unsigned, u2v>::type, typename Elem<T>::vec>::type raw[N];
+  static_assert(!Q || F == kAcross);
+  Raw raw[N];
   unsigned char exps[Q ? N : 1];
 
   static __device__ __forceinline__ int row_of(int i) { return threadIdx.x / PER + i * (THREADS / PER); }
   static __device__ __forceinline__ int col_of() { return threadIdx.x % PER * V; }
 
   // The tile at output index r0 and reduction index k0 of an operand with `rows`
-  // output indexes; reduction indexes from `end` on are zero, output indexes
+  // output indexes; reduction indexes from `end` on are zero; output indexes
   // past the end read as the last row (along) or zero (across): their results
-  // are not stored.
-  __device__ __forceinline__ void load(const Side& s, int64_t r0, int64_t rows, int64_t k0, int64_t end, int width) {
+  // are not stored.  WHOLE: no piece crosses a row's end and all reduction
+  // indexes are inside (a tile's own loop: with both ways in one loop, the loaded
+  // registers were copied where the ways meet, which waits for the loads).
+  // Otherwise a piece that crosses a row's end is loaded from where it still
+  // fits and moved down; only rows shorter than a piece go by values.
+  static __device__ __forceinline__ bool whole_cols(int64_t r0, int64_t rows) {
+    return F == kAlong || r0 + Lds::W <= rows;
+  }
+  template <bool WHOLE>
+  __device__ __forceinline__ void load(const Side& s, int64_t r0, int64_t rows, int64_t k0, int64_t end) {
     const int64_t m0 = F == kAlong ? r0 : k0;              // memory row and column of the tile
-    const int64_t c0 = (F == kAlong ? k0 : r0) + col_of();
+    int64_t c0 = (F == kAlong ? k0 : r0) + col_of();
     const int64_t mend = F == kAlong ? rows : end, cend = F == kAlong ? end : rows;
-    const bool whole = (F == kAlong || k0 + BK <= end) && (F == kAlong ? k0 : r0) + Lds::W <= cend;
-    if constexpr (Q) {
-      const int groups = (width + kGroup - 1) / kGroup;
+    const E* p = Q ? reinterpret_cast<const E*>(s.q) : static_cast<const E*>(s.p);
+    if constexpr (WHOLE) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         int64_t m = m0 + row_of(i);
-        const bool in = m < mend && c0 < cend;
         if (F == kAlong && m >= mend) m = mend - 1;
-        if constexpr (V == 4) raw[i] = 0u; else raw[i] = u2v{0u, 0u};
-        exps[i] = 0;
-        if (!whole && !in) continue;
-        const int8_t* q = s.q + m * width + c0;
-        exps[i] = s.c[m * groups + c0 / kGroup];
-        if (whole || c0 + V <= cend) {
-          raw[i] = *reinterpret_cast<const typename Bytes<V>::vec*>(q);
-        } else {
-          unsigned w[2] = {0, 0};
-          for (int e = 0; e < (int)(cend - c0); ++e) w[e / 4] |= (unsigned)(uint8_t)q[e] << (8 * (e % 4));
-          if constexpr (V == 4) raw[i] = w[0]; else raw[i] = u2v{w[0], w[1]};
-        }
+        raw[i] = *reinterpret_cast<const Any*>(p + m * s.ld + c0);
+        if constexpr (Q) exps[i] = s.c[m * s.ldc + c0 / kGroup];
       }
-    } else {
-      const T* p = static_cast<const T*>(s.p);
-      if (whole) {
+      return;
+    }
+    const bool fits = cend >= V;
+    const int64_t over = c0 > cend - V ? c0 - (cend - V) : 0;
+    const unsigned bits = over >= V ? 8 * sizeof(Raw) : (unsigned)over * BITS;
+    if (over >= V) c0 = cend - 1;                          // an address in the row; nothing of it is used
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          int64_t m = m0 + row_of(i);
-          if (F == kAlong && m >= mend) m = mend - 1;
-          raw[i] = *reinterpret_cast<const typename Elem<T>::vec*>(p + m * s.ld + c0);
-        }
+    for (int i = 0; i < N; ++i) {
+      int64_t m = m0 + row_of(i);
+      const bool in = F == kAlong || m < mend;
+      if (m >= mend) m = mend - 1;
+      const E* q = p + m * s.ld;
+      if (fits) {
+        raw[i] = shift_down(*reinterpret_cast<const Any*>(q + (over >= V ? cend - V : c0 - over)), in ? bits : 8 * sizeof(Raw));
       } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          int64_t m = m0 + row_of(i);
-          int64_t n = m < mend ? cend - c0 : F == kAlong ? cend - c0 : 0;
-          if (F == kAlong && m >= mend) m = mend - 1;
-          float v[V];
-          ld_piece<T>(p + m * s.ld + c0, n < V ? (int)(n < 0 ? 0 : n) : V, v);
-          raw[i] = Elem<T>::put(v);
-        }
+        unsigned w[sizeof(Raw) / 4] = {};
+        const int n = in && over < V ? (int)(cend - c0) : 0;
+        for (int e = 0; e < V; ++e)
+          if (e < n) {
+            unsigned u;
+            if constexpr (Q) u = (uint8_t)q[c0 + e];
+            else if constexpr (sizeof(E) == 2) u = __builtin_bit_cast(unsigned short, q[c0 + e]);
+            else u = __builtin_bit_cast(unsigned, q[c0 + e]);
+            w[e * BITS / 32] |= u << (e * BITS % 32);
+          }
+        if constexpr (sizeof(Raw) == 16) raw[i] = u4v{w[0], w[1], w[2], w[3]};
+        else if constexpr (sizeof(Raw) == 8) raw[i] = u2v{w[0], w[1]};
+        else raw[i] = w[0];
       }
+      // a step's exponent only where something was read: a NaN step times a zero is NaN
+      if constexpr (Q) exps[i] = in && over < V ? s.c[m * s.ldc + c0 / kGroup] : 0;
     }
   }
   __device__ __forceinline__ void store(Lds& l) const {
@@ -172,8 +201,8 @@ struct Loader {
         if constexpr (V == 4) *reinterpret_cast<u2v*>(&l.v[0][o]) = u2v{b[0], b[1]};
         else *reinterpret_cast<u4v*>(&l.v[0][o]) = u4v{b[0], b[1], b[2], b[3]};
       } else {
-        float a = raw[i][0] * kTermScale, b = raw[i][1] * kTermScale;
-        float c = raw[i][2] * kTermScale, d = raw[i][3] * kTermScale;
+        const f4v r = __builtin_bit_cast(f4v, raw[i]);
+        float a = r.x * kTermScale, b = r.y * kTermScale, c = r.z * kTermScale, d = r.w * kTermScale;
 #pragma unroll
         for (int t = 0; t < 3; ++t) {
           const unsigned x = term2(a, b), y = term2(c, d);
@@ -235,7 +264,7 @@ struct Tile {
 
   // Sums over reduction indexes [k0, end) of the tile at (r0, c0) of rows x cols.
   __device__ __forceinline__ void run(Shared& sh, const Side& sa, const Side& sb, int64_t r0, int64_t rows, int c0,
-                                      int cols, int64_t k0, int64_t end, int width) {
+                                      int cols, int64_t k0, int64_t end) {
     const int w = uniform(threadIdx.x / kWave), row0 = w / WN * TM, col0 = w % WN * TN;
 #pragma unroll
     for (int i = 0; i < RM; ++i)
@@ -243,34 +272,35 @@ struct Tile {
       for (int j = 0; j < RN; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    const int64_t whole = LA::whole_cols(r0, rows) && LB::whole_cols(c0, cols) ? k0 + (end - k0) / BK * BK : k0;
+    steps<true>(sh, sa, sb, r0, rows, c0, cols, k0, whole, row0, col0);
+    steps<false>(sh, sa, sb, r0, rows, c0, cols, whole, end, row0, col0);
+  }
+  template <bool WHOLE>
+  __device__ __forceinline__ void steps(Shared& sh, const Side& sa, const Side& sb, int64_t r0, int64_t rows, int c0,
+                                        int cols, int64_t k, int64_t end, int row0, int col0) {
+    if (k >= end) return;
     LA la;
     LB lb;
-    la.load(sa, r0, rows, k0, end, width);
-    lb.load(sb, c0, cols, k0, end, 0);
-    if constexpr (BUFS == 2) {
-      la.store(sh.in[0].a), lb.store(sh.in[0].b);
-      int cur = 0;
-      for (int64_t k = k0; k < end; k += BK) {
+    la.template load<WHOLE>(sa, r0, rows, k, end);
+    lb.template load<WHOLE>(sb, c0, cols, k, end);
+    __syncthreads();
+    int cur = 0;
+    if constexpr (BUFS == 2) la.store(sh.in[0].a), lb.store(sh.in[0].b);
+    for (; k < end; k += BK) {
+      if constexpr (BUFS == 1) la.store(sh.in[0].a), lb.store(sh.in[0].b);
+      __syncthreads();
+      const bool more = k + BK < end;
+      if (more) {
+        la.template load<WHOLE>(sa, r0, rows, k + BK, end);
+        lb.template load<WHOLE>(sb, c0, cols, k + BK, end);
+      }
+      step(sh.in[cur].a, sh.in[cur].b, row0, col0);
+      if constexpr (BUFS == 1) {
         __syncthreads();
-        const bool more = k + BK < end;
-        if (more) {
-          la.load(sa, r0, rows, k + BK, end, width);
-          lb.load(sb, c0, cols, k + BK, end, 0);
-        }
-        step(sh.in[cur].a, sh.in[cur].b, row0, col0);
+      } else {
         if (more) la.store(sh.in[cur ^ 1].a), lb.store(sh.in[cur ^ 1].b);
         cur ^= 1;
-      }
-    } else {
-      for (int64_t k = k0; k < end; k += BK) {
-        la.store(sh.in[0].a), lb.store(sh.in[0].b);
-        __syncthreads();
-        if (k + BK < end) {
-          la.load(sa, r0, rows, k + BK, end, width);
-          lb.load(sb, c0, cols, k + BK, end, 0);
-        }
-        step(sh.in[0].a, sh.in[0].b, row0, col0);
-        __syncthreads();
       }
     }
   }
