@@ -103,6 +103,108 @@ __global__ __launch_bounds__(WM* WN* kWave, OCC) void k_dense(DenseArgs a) {
   });
 }
 
+// Reductions of at most KC <= 16 (a radial basis): the weights of a thread's V
+// columns stay in registers, rows go by with the next one's x in flight, and no
+// LDS is used; L lanes share a row.  Bound by the write of y: 1,248,000 x 8 x 64
+// float32 @THIN@ us, where the tile product took 156 (its steps are of 32).
+template <class T, int L, int KC>
+__global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {
+  constexpr int V = Elem<T>::V, R = 256 / L, P = KC / V > 0 ? KC / V : 1;
+  const int K = (int)a.red, col = ((int)blockIdx.y * L + (int)threadIdx.x % L) * V, n = a.cols - col;
+  const T* W = static_cast<const T*>(a.b.p);
+  const T* x = static_cast<const T*>(a.a.p);
+  float w[KC][V], bias[V] = {};
+#pragma unroll
+  for (int k = 0; k < KC; ++k) {
+    if (k < K) {
+      ld_piece<T>(W + (int64_t)k * a.cols + col, n, w[k]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) w[k][i] = 0.0f;
+    }
+  }
+  if (a.bias) ld_piece<T>(static_cast<const T*>(a.bias) + col, n, bias);
+  a.bias = nullptr;
+  const int64_t stride = (int64_t)gridDim.x * R;
+  typename Elem<T>::vec raw[P];
+  auto load = [&](int64_t row) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) raw[p] = ld_raw<T>(x + row * a.a.ld + p * V, K - p * V);
+  };
+  int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L;
+  if (row < a.rows) load(row);
+  for (; row < a.rows; row += stride) {
+    float u[P][V], v[V];
+#pragma unroll
+    for (int p = 0; p < P; ++p) Elem<T>::get(raw[p], u[p]);
+    if (row + stride < a.rows) load(row + stride);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KC; ++k) {
+      if (k < K)  // uniform; an infinity of x times a missing weight would be NaN
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = fmaf(u[k / V][k % V], w[k][i], v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] += bias[i];
+    dense_tail<T, V>(a, row, true, col, v);
+  }
+}
+
+// At most MR <= 8 rows: W is read once, straight to registers, and that is what
+// bounds it.  A workgroup takes 32 columns; its lanes of a column piece take
+// every G-th reduction index, and their sums are added over the wave and then
+// over the waves in order.
+template <class T, int MR>
+__global__ __launch_bounds__(512) void k_dense_few(DenseArgs a) {
+  constexpr int V = Elem<T>::V, C = 32 / V, G = 512 / C, WAVES = 512 / kWave;
+  __shared__ float s[WAVES][MR][32];
+  const int cl = threadIdx.x % C, g = threadIdx.x / C, col = (int)blockIdx.x * 32 + cl * V, n = a.cols - col;
+  const int K = (int)a.red;
+  const T* W = static_cast<const T*>(a.b.p);
+  const T* x = static_cast<const T*>(a.a.p);
+  float v[MR][V] = {};
+  constexpr int U = 8;  // loads in flight
+  for (int k0 = g; k0 < K; k0 += G * U) {
+    typename Elem<T>::vec w[U];
+    float u[U][MR];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int k = k0 + j * G;
+      if (k < K) {
+        w[j] = ld_raw<T>(W + (int64_t)k * a.cols + col, n);
+#pragma unroll
+        for (int m = 0; m < MR; ++m) u[j][m] = m < a.rows ? Elem<T>::one(x[m * a.a.ld + k]) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (k0 + j * G < K) {
+        float t[V];
+        Elem<T>::get(w[j], t);
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[m][i] = fmaf(u[j][m], t[i], v[m][i]);
+      }
+  }
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float t = sum_strided<C>(v[m][i]);
+      if (threadIdx.x % kWave < C) s[threadIdx.x / kWave][m][cl * V + i] = t;
+    }
+  __syncthreads();
+  if (threadIdx.x >= MR * C) return;
+  float t[V] = {};
+  for (int q = 0; q < WAVES; ++q)
+#pragma unroll
+    for (int i = 0; i < V; ++i) t[i] += s[q][g][cl * V + i];
+  dense_tail<T, V>(a, g, g < a.rows, col, t);
+}
+
 // The partial sums of the splits, in order, and the epilogue.
 template <class T>
 __global__ __launch_bounds__(256) void k_dense_join(DenseArgs a, int splits) {
@@ -204,6 +306,29 @@ DenseBwdWs dense_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   return w;
 }
 
+constexpr int kThin = 16, kFew = 8;
+
+template <class T, int L, int KC>
+e3_status dense_thin(const DenseArgs& a, hipStream_t st) {
+  constexpr int R = 256 / L, V = Elem<T>::V;
+  // at least two rows a thread where that still fills the card, for the weights it loads first
+  const int64_t tiles = (a.rows + R - 1) / R, cols = (a.cols + L * V - 1) / (L * V);
+  const int64_t blocks = std::min<int64_t>(tiles, std::max<int64_t>(1, 4096 / cols));
+  TimedLaunch t_("dense_thin", st);
+  hipLaunchKernelGGL((k_dense_thin<T, L, KC>), dim3((unsigned)blocks, (unsigned)cols), dim3(256), 0, st, a);
+  E3_HIP(hipGetLastError());
+  return E3_OK;
+}
+template <class T>
+e3_status dense_few(const DenseArgs& a, hipStream_t st) {
+  TimedLaunch t_("dense_few", st);
+  auto* k = a.rows == 1 ? k_dense_few<T, 1> : a.rows == 2 ? k_dense_few<T, 2> : a.rows <= 4 ? k_dense_few<T, 4>
+                                                                                        : k_dense_few<T, kFew>;
+  hipLaunchKernelGGL(k, dim3((unsigned)((a.cols + 31) / 32)), dim3(512), 0, st, a);
+  E3_HIP(hipGetLastError());
+  return E3_OK;
+}
+
 template <class T, Form FA, Form FB, bool QA>
 e3_status dense_product(DenseArgs a, float* part, const char* name, hipStream_t st) {
   const Cut c = dense_cut(a.rows, a.cols, a.red);
@@ -226,7 +351,24 @@ e3_status dense_product(DenseArgs a, float* part, const char* name, hipStream_t 
   return E3_OK;
 }
 
-size_t dense_fwd_ws(int64_t M, int64_t K, int64_t N) { return M == 0 ? 0 : cut_bytes(dense_cut(M, N, K), M, N); }
+size_t dense_fwd_ws(int64_t M, int64_t K, int64_t N) {
+  return M <= kFew || K <= kThin ? 0 : cut_bytes(dense_cut(M, N, K), M, N);
+}
+template <class T>
+e3_status dense_fwd(const DenseArgs& a, float* part, hipStream_t st) {
+  if (a.rows <= kFew) return dense_few<T>(a, st);
+  if (a.red <= kThin) {
+    constexpr int V = Elem<T>::V;
+    const int pieces = (a.cols + V - 1) / V;
+    auto with = [&](auto KC) {
+      constexpr int kc = decltype(KC)::value;
+      return pieces <= 8 ? dense_thin<T, 8, kc>(a, st) : pieces <= 16 ? dense_thin<T, 16, kc>(a, st)
+                                                                      : dense_thin<T, 64, kc>(a, st);
+    };
+    return a.red <= 8 ? with(std::integral_constant<int, 8>{}) : with(std::integral_constant<int, kThin>{});
+  }
+  return dense_product<T, kAlong, kAcross, false>(a, part, "dense_fwd", st);
+}
 
 bool good_dims(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   return good_rows(t, M, K) && N >= 1 && N <= kMaxCols;
@@ -319,8 +461,7 @@ e3_status e3_dense_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* W
   a.zc = zc, a.yq = yq, a.yc = yc;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   float* part = static_cast<float*>(ws);
-  return dtype == E3_F32 ? dense_product<float, kAlong, kAcross, false>(a, part, "dense_fwd", st)
-                         : dense_product<__bf16, kAlong, kAcross, false>(a, part, "dense_fwd", st);
+  return dtype == E3_F32 ? dense_fwd<float>(a, part, st) : dense_fwd<__bf16>(a, part, st);
 }
 
 e3_status e3_dense_bwd(e3_dtype dtype, const void* x, int64_t ldx, const int8_t* xq, const uint8_t* xc, const void* W,

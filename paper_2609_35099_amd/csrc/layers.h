@@ -113,6 +113,19 @@ __device__ __forceinline__ float sum_lanes(float v) {
     return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
   }));
 }
+// Over the lanes of the wave that are congruent modulo C (4 or 8).
+template <int C>
+__device__ __forceinline__ float sum_strided(float v) {
+  static_assert(C == 4 || C == 8);
+  auto add = [](unsigned a, unsigned b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); };
+  unsigned u = __float_as_uint(v);
+  if constexpr (C == 4) u = add(u, dpp_u<0x124>(u));  // row_ror:4
+  u = add(u, dpp_u<0x128>(u));                        // row_ror:8
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  u = add(r[0], r[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(add(q[0], q[1]));
+}
 template <int L>
 __device__ __forceinline__ unsigned max_lanes(unsigned v) {
   return fold_lanes<L>(v, [](unsigned a, unsigned b) { return a > b ? a : b; });
