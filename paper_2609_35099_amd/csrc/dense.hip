@@ -20,33 +20,39 @@ struct DenseArgs {
   uint8_t *zc, *yc;
   int64_t ldr, ldy, ldz;
   int act;
+  bool nt;  // y (and z) streams
 };
 
-// What follows the sums of one piece of a row; the lanes of a group of 32
-// columns take part together, also where the row (row_ok) or columns end.
+// What follows the sums of one piece of a row, row0 + lr with row0 uniform (so
+// that a thread multiplies by a row stride once, not per piece); the lanes of a
+// group of 32 columns take part together, also where rows (ok) or columns end.
 template <class T, int V>
-__device__ __forceinline__ void dense_tail(const DenseArgs& a, int64_t row, bool row_ok, int col, float (&v)[V]) {
+__device__ __forceinline__ void dense_tail(const DenseArgs& a, int64_t row0, int lr, bool ok, int col, float (&v)[V]) {
   static_assert(V == Elem<T>::V);
-  const int n = row_ok ? a.cols - col : 0;
-  const int64_t groups = (a.cols + kGroup - 1) / kGroup;
+  const int n = ok ? a.cols - col : 0;
+  auto at = [&](int64_t ld) { return row0 * ld + (lr * ld + col); };
+  auto pack = [&](int8_t* q, uint8_t* c) {
+    const int64_t groups = (a.cols + kGroup - 1) / kGroup;
+    pack8_piece<V>(v, col, n, q + (row0 * a.cols + (int64_t)lr * a.cols), c + (row0 * groups + lr * groups));
+  };
   float u[V];
   if (a.bias) {
     ld_piece<T>(static_cast<const T*>(a.bias) + col, n, u);
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] += u[i];
   }
-  if (a.z) st_piece<T>(static_cast<T*>(a.z) + row * a.ldz + col, n, v);
-  if (a.zq) pack8_piece<V>(v, col, n, a.zq + row * a.cols, a.zc + row * groups);
+  if (a.z) st_piece<T>(static_cast<T*>(a.z) + at(a.ldz), n, v, a.nt);
+  if (a.zq) pack(a.zq, a.zc);
   act_piece(a.act, v);
   if (a.res) {
-    ld_piece<T>(static_cast<const T*>(a.res) + row * a.ldr + col, n, u);
+    ld_piece<T>(static_cast<const T*>(a.res) + at(a.ldr), n, u);
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] += u[i];
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = Elem<T>::round(v[i]);
-  st_piece<T>(static_cast<T*>(a.y) + row * a.ldy + col, n, v);
-  if (a.yq) pack8_piece<V>(v, col, n, a.yq + row * a.cols, a.yc + row * groups);
+  st_piece<T>(static_cast<T*>(a.y) + at(a.ldy), n, v, a.nt);
+  if (a.yq) pack(a.yq, a.yc);
 }
 
 // A sum again from memory, in float32.
@@ -80,8 +86,8 @@ __global__ __launch_bounds__(WM* WN* kWave, OCC) void k_dense(DenseArgs a) {
   const int64_t k0 = split * a.chunk, end = k0 + a.chunk < a.red ? k0 + a.chunk : a.red;
   Tl t;
   t.run(sh, a.a, a.b, r0, a.rows, c0, a.cols, k0, end);
-  t.finish(sh, [&](int r, int c, float(&v)[V]) {
-    const int64_t row = r0 + r;
+  t.finish(sh, [&](int r, int lr, int c, float(&v)[V]) {
+    const int64_t rowu = r0 + r, row = rowu + lr;
     const int col = c0 + c;
     const int n = row < a.rows ? a.cols - col : 0;
     if constexpr (sizeof(T) == 4) {
@@ -94,11 +100,11 @@ __global__ __launch_bounds__(WM* WN* kWave, OCC) void k_dense(DenseArgs a) {
           if (e < n && v[e] * 0.0f != 0.0f) v[e] = dense_again<T, FA, FB, QA>(a.a, a.b, row, col + e, k0, end);
     }
     if (a.part) {
-      float* p = a.part + ((int64_t)split * a.rows + row) * a.cols + col;
+      float* p = a.part + ((int64_t)split * a.rows + rowu) * a.cols + ((int64_t)lr * a.cols + col);
 #pragma unroll
       for (int e = 0; e < V; e += 4) st_piece<float>(p + e, n - e, reinterpret_cast<float(&)[4]>(v[e]));
     } else {
-      dense_tail<T, V>(a, row, row < a.rows, col, v);
+      dense_tail<T, V>(a, rowu, lr, row < a.rows, col, v);
     }
   });
 }
@@ -125,30 +131,44 @@ __global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {
   }
   if (a.bias) ld_piece<T>(static_cast<const T*>(a.bias) + col, n, bias);
   a.bias = nullptr;
-  const int64_t stride = (int64_t)gridDim.x * R;
-  typename Elem<T>::vec raw[P];
-  auto load = [&](int64_t row) {
+  // U rows a thread and round, the next round's x in flight: with one, the rows'
+  // latency was most of the time (@ONE@ us)
+  constexpr int U = 4;
+  constexpr int TR = R * U;  // rows of a round
+  const int lr = threadIdx.x / L;
+  typename Elem<T>::vec raw[U][P];
+  auto load = [&](int64_t tile) {
+    const T* xt = x + tile * TR * a.a.ld;
+    const int last = a.rows - tile * TR < TR ? (int)(a.rows - tile * TR) - 1 : TR - 1;
 #pragma unroll
-    for (int p = 0; p < P; ++p) raw[p] = ld_raw<T>(x + row * a.a.ld + p * V, K - p * V);
-  };
-  int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L;
-  if (row < a.rows) load(row);
-  for (; row < a.rows; row += stride) {
-    float u[P][V], v[V];
+    for (int j = 0; j < U; ++j) {
+      const int64_t at = imin(lr + j * R, last) * a.a.ld;
 #pragma unroll
-    for (int p = 0; p < P; ++p) Elem<T>::get(raw[p], u[p]);
-    if (row + stride < a.rows) load(row + stride);
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < KC; ++k) {
-      if (k < K)  // uniform; an infinity of x times a missing weight would be NaN
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = fmaf(u[k / V][k % V], w[k][i], v[i]);
+      for (int p = 0; p < P; ++p) raw[j][p] = ld_raw<T>(xt + at + p * V, K - p * V);
     }
+  };
+  int64_t tile = blockIdx.x;
+  if (tile * TR < a.rows) load(tile);
+  for (; tile * TR < a.rows; tile += gridDim.x) {
+    float v[U][V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] += bias[i];
-    dense_tail<T, V>(a, row, true, col, v);
+    for (int j = 0; j < U; ++j) {
+      float u[P][V];
+#pragma unroll
+      for (int p = 0; p < P; ++p) Elem<T>::get(raw[j][p], u[p]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[j][i] = bias[i];
+#pragma unroll
+      for (int k = 0; k < KC; ++k)  // past K both are zero
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[j][i] = fmaf(u[k / V][k % V], w[k][i], v[j][i]);
+    }
+    if ((tile + gridDim.x) * TR < a.rows) load(tile + gridDim.x);
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int64_t row0 = tile * TR + j * R;
+      dense_tail<T, V>(a, row0, lr, row0 + lr < a.rows, col, v[j]);
+    }
   }
 }
 
@@ -202,7 +222,7 @@ __global__ __launch_bounds__(512) void k_dense_few(DenseArgs a) {
   for (int q = 0; q < WAVES; ++q)
 #pragma unroll
     for (int i = 0; i < V; ++i) t[i] += s[q][g][cl * V + i];
-  dense_tail<T, V>(a, g, g < a.rows, col, t);
+  dense_tail<T, V>(a, 0, g, g < a.rows, col, t);
 }
 
 // The partial sums of the splits, in order, and the epilogue.
@@ -219,7 +239,7 @@ __global__ __launch_bounds__(256) void k_dense_join(DenseArgs a, int splits) {
 #pragma unroll
       for (int e = 0; e < V; ++e)
         if (col + e < a.cols) v[e] += a.part[((int64_t)s * a.rows + row) * a.cols + col + e];
-  dense_tail<T, V>(a, row, ok, col, v);
+  dense_tail<T, V>(a, row, 0, ok, col, v);
 }
 
 // dz = dy act'(z) in the type of dy (a bfloat16 dz is an operand of the matrix
@@ -310,10 +330,9 @@ constexpr int kThin = 16, kFew = 8;
 
 template <class T, int L, int KC>
 e3_status dense_thin(const DenseArgs& a, hipStream_t st) {
-  constexpr int R = 256 / L, V = Elem<T>::V;
-  // at least two rows a thread where that still fills the card, for the weights it loads first
+  constexpr int R = 256 / L * 4, V = Elem<T>::V;
   const int64_t tiles = (a.rows + R - 1) / R, cols = (a.cols + L * V - 1) / (L * V);
-  const int64_t blocks = std::min<int64_t>(tiles, std::max<int64_t>(1, 4096 / cols));
+  const int64_t blocks = std::min<int64_t>(tiles, std::max<int64_t>(1, 1536 / cols));
   TimedLaunch t_("dense_thin", st);
   hipLaunchKernelGGL((k_dense_thin<T, L, KC>), dim3((unsigned)blocks, (unsigned)cols), dim3(256), 0, st, a);
   E3_HIP(hipGetLastError());
@@ -362,8 +381,11 @@ e3_status dense_fwd(const DenseArgs& a, float* part, hipStream_t st) {
     const int pieces = (a.cols + V - 1) / V;
     auto with = [&](auto KC) {
       constexpr int kc = decltype(KC)::value;
-      return pieces <= 8 ? dense_thin<T, 8, kc>(a, st) : pieces <= 16 ? dense_thin<T, 16, kc>(a, st)
-                                                                      : dense_thin<T, 64, kc>(a, st);
+      const int last = pieces % 64;  // lanes of a row's last column tile
+      return pieces <= 8    ? dense_thin<T, 8, kc>(a, st)
+             : pieces <= 16 ? dense_thin<T, 16, kc>(a, st)
+             : pieces <= 32 || (last && last <= 32) ? dense_thin<T, 32, kc>(a, st)
+                                                    : dense_thin<T, 64, kc>(a, st);
     };
     return a.red <= 8 ? with(std::integral_constant<int, 8>{}) : with(std::integral_constant<int, kThin>{});
   }
@@ -399,7 +421,7 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
   if (dx) {
     DenseArgs a{};
     a.a = {d, ldd}, a.b = {W, N}, a.rows = M, a.cols = (int)K, a.red = N;
-    a.y = dx, a.ldy = lddx;
+    a.y = dx, a.ldy = lddx, a.nt = streams(t, M, K);
     const e3_status s = dense_product<T, kAlong, kAlong, false>(a, part, "dense_bwd_dx", st);
     if (s != E3_OK) return s;
   }
@@ -458,7 +480,7 @@ e3_status e3_dense_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* W
   DenseArgs a{};
   a.a = {x, ldx}, a.b = {W, N}, a.rows = M, a.cols = (int)N, a.red = K;
   a.bias = bias, a.res = res, a.ldr = ldr, a.act = act, a.y = y, a.ldy = ldy, a.z = z, a.ldz = ldz, a.zq = zq;
-  a.zc = zc, a.yq = yq, a.yc = yc;
+  a.zc = zc, a.yq = yq, a.yc = yc, a.nt = streams(dtype, M, N);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   float* part = static_cast<float*>(ws);
   return dtype == E3_F32 ? dense_fwd<float>(a, part, st) : dense_fwd<__bf16>(a, part, st);

@@ -136,41 +136,42 @@ struct Loader {
   }
   template <bool WHOLE>
   __device__ __forceinline__ void load(const Side& s, int64_t r0, int64_t rows, int64_t k0, int64_t end) {
-    const int64_t m0 = F == kAlong ? r0 : k0;              // memory row and column of the tile
-    int64_t c0 = (F == kAlong ? k0 : r0) + col_of();
+    // memory row m0 + row_of(i), column c0 + col_of(): the uniform part in the base
+    const int64_t m0 = F == kAlong ? r0 : k0, c0 = F == kAlong ? k0 : r0;
     const int64_t mend = F == kAlong ? rows : end, cend = F == kAlong ? end : rows;
-    const E* p = Q ? reinterpret_cast<const E*>(s.q) : static_cast<const E*>(s.p);
+    const E* p = (Q ? reinterpret_cast<const E*>(s.q) : static_cast<const E*>(s.p)) + (m0 * s.ld + c0);
+    const uint8_t* pc = Q ? s.c + (m0 * s.ldc + c0 / kGroup) : nullptr;
+    const int mlast = mend - m0 < 1024 ? (int)(mend - m0) - 1 : 1023;
+    const int lc = col_of();
     if constexpr (WHOLE) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        int64_t m = m0 + row_of(i);
-        if (F == kAlong && m >= mend) m = mend - 1;
-        raw[i] = *reinterpret_cast<const Any*>(p + m * s.ld + c0);
-        if constexpr (Q) exps[i] = s.c[m * s.ldc + c0 / kGroup];
+        const int64_t m = F == kAlong ? imin(row_of(i), mlast) : row_of(i);
+        raw[i] = *reinterpret_cast<const Any*>(p + (m * s.ld + lc));
+        if constexpr (Q) exps[i] = pc[m * s.ldc + lc / kGroup];
       }
       return;
     }
     const bool fits = cend >= V;
-    const int64_t over = c0 > cend - V ? c0 - (cend - V) : 0;
+    const int left = cend - c0 < 1024 ? (int)(cend - c0) : 1024;  // columns from c0 on
+    const int over = lc > left - V ? lc - (left - V) : 0;          // how far the piece reaches out
     const unsigned bits = over >= V ? 8 * sizeof(Raw) : (unsigned)over * BITS;
-    if (over >= V) c0 = cend - 1;                          // an address in the row; nothing of it is used
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      int64_t m = m0 + row_of(i);
-      const bool in = F == kAlong || m < mend;
-      if (m >= mend) m = mend - 1;
+      const bool in = F == kAlong || row_of(i) <= mlast;
+      const int64_t m = imin(row_of(i), mlast);
       const E* q = p + m * s.ld;
       if (fits) {
-        raw[i] = shift_down(*reinterpret_cast<const Any*>(q + (over >= V ? cend - V : c0 - over)), in ? bits : 8 * sizeof(Raw));
+        raw[i] = shift_down(*reinterpret_cast<const Any*>(q + (over ? left - V : lc)), in ? bits : 8 * sizeof(Raw));
       } else {
         unsigned w[sizeof(Raw) / 4] = {};
-        const int n = in && over < V ? (int)(cend - c0) : 0;
+        const int n = in && over < V ? left - lc : 0;
         for (int e = 0; e < V; ++e)
           if (e < n) {
             unsigned u;
-            if constexpr (Q) u = (uint8_t)q[c0 + e];
-            else if constexpr (sizeof(E) == 2) u = __builtin_bit_cast(unsigned short, q[c0 + e]);
-            else u = __builtin_bit_cast(unsigned, q[c0 + e]);
+            if constexpr (Q) u = (uint8_t)q[lc + e];
+            else if constexpr (sizeof(E) == 2) u = __builtin_bit_cast(unsigned short, q[lc + e]);
+            else u = __builtin_bit_cast(unsigned, q[lc + e]);
             w[e * BITS / 32] |= u << (e * BITS % 32);
           }
         if constexpr (sizeof(Raw) == 16) raw[i] = u4v{w[0], w[1], w[2], w[3]};
@@ -178,7 +179,10 @@ struct Loader {
         else raw[i] = w[0];
       }
       // a step's exponent only where something was read: a NaN step times a zero is NaN
-      if constexpr (Q) exps[i] = in && over < V ? s.c[m * s.ldc + c0 / kGroup] : 0;
+      if constexpr (Q) {
+        exps[i] = 0;
+        if (in && over < V) exps[i] = pc[m * s.ldc + lc / kGroup];
+      }
     }
   }
   __device__ __forceinline__ void store(Lds& l) const {
@@ -305,9 +309,9 @@ struct Tile {
     }
   }
 
-  // Hands the results out as pieces of V values of a row, f(row, col, v) with row
-  // and col within the tile; the lanes of a wave hold consecutive pieces.  Every
-  // wave goes through memory of its own.
+  // Hands the results out as pieces of V values of a row, f(row, lr, col, v) with
+  // row + lr and col within the tile and row uniform; the lanes of a wave hold
+  // consecutive pieces.  Every wave goes through memory of its own.
   template <class Fn>
   __device__ __forceinline__ void finish(Shared& sh, Fn&& f) {
     constexpr int V = Elem<T>::V, PER = TN / V, PASS = kWave / PER;
@@ -328,14 +332,14 @@ struct Tile {
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int r = 0; r < 32; r += PASS) {
-        const int row = r + l / PER, col = l % PER * V;
+        const int col = l % PER * V;
         float v[V];
 #pragma unroll
         for (int e = 0; e < V; e += 4) {
-          const f4v t = *reinterpret_cast<const f4v*>(&sh.out[w][row][col + e]);
+          const f4v t = *reinterpret_cast<const f4v*>(&sh.out[w][r + l / PER][col + e]);
           v[e] = t.x * kBack, v[e + 1] = t.y * kBack, v[e + 2] = t.z * kBack, v[e + 3] = t.w * kBack;
         }
-        f(row0 + 32 * i + row, col0 + col, v);
+        f(row0 + 32 * i + r, l / PER, col0 + col, v);
       }
       __builtin_amdgcn_wave_barrier();
     }

@@ -29,6 +29,7 @@ struct NormArgs {
   int64_t ldx, ldy, lddx, rows;
   int cols, blocks;
   float eps;
+  bool nt;  // y or dx streams
 };
 
 // Sums over the L lanes of a row: part of a wave, or the whole workgroup (then
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(kNormFwdThreads<L>) void k_norm_fwd(NormArgs a) {
       const float t = gamma ? w * g[i] : w;
       u[i] = Elem<T>::round(beta ? t + b[i] : t);
     }
-    st_piece<T>(static_cast<T*>(a.y) + row * a.ldy + col, n, u);
+    st_piece<T>(static_cast<T*>(a.y) + row * a.ldy + col, n, u, a.nt);
     if (a.yq) pack8_piece<V>(u, col, n, a.yq + row * cols, a.yc + row * groups);
   }
 }
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(kNormBwdThreads<L>) void k_norm_bwd(NormArgs a) {
         const int col = (j * L + lane) * V;
 #pragma unroll
         for (int i = 0; i < V; ++i) dy[j][i] = rs * (dy[j][i] - c0 - x[j][i] * c1);
-        st_piece<T>(static_cast<T*>(a.dx) + row * a.lddx + col, cols - col, dy[j]);
+        st_piece<T>(static_cast<T*>(a.dx) + row * a.lddx + col, cols - col, dy[j], a.nt);
       }
     }
   }
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_bwd_wide(NormArgs a) {
     load(col, x, u);
 #pragma unroll
     for (int i = 0; i < V; ++i) u[i] = rstd * (u[i] - c0 - x[i] * c1);
-    st_piece<T>(static_cast<T*>(a.dx) + row * a.lddx + col, cols - col, u);
+    st_piece<T>(static_cast<T*>(a.dx) + row * a.lddx + col, cols - col, u, a.nt);
   }
 }
 // Their weight gradients: a thread's V columns over the rows of the block's
@@ -308,7 +309,7 @@ __global__ __launch_bounds__(256) void k_pack8(const T* x, int64_t ldx, int8_t* 
 }
 template <class T>
 __global__ __launch_bounds__(256) void k_unpack8(const int8_t* q, const uint8_t* c, T* x, int64_t ldx, int64_t rows,
-                                                 int cols) {
+                                                 int cols, bool nt) {
   constexpr int V = Elem<T>::V;
   const int groups = (cols + kGroup - 1) / kGroup;
   const int64_t per = (cols + V - 1) / V;
@@ -317,7 +318,7 @@ __global__ __launch_bounds__(256) void k_unpack8(const int8_t* q, const uint8_t*
   const int col = (int)(i - row * per) * V, n = cols - col;
   float v[V];
   get8(ld_raw8<V>(q + row * cols, c + row * groups, col, n), v);
-  st_piece<T>(x + row * ldx + col, n, v);
+  st_piece<T>(x + row * ldx + col, n, v, nt);
 }
 
 // ------------------------------------------------------------ host
@@ -421,10 +422,10 @@ e3_status e3_unpack8(e3_dtype dtype, const int8_t* q, const uint8_t* c, void* x,
   TimedLaunch t_("unpack8", st);
   if (dtype == E3_F32)
     hipLaunchKernelGGL(k_unpack8<float>, grid_of((rows * ((cols + 3) / 4) + 255) / 256), dim3(256), 0, st, q, c,
-                       static_cast<float*>(x), ldx, rows, (int)cols);
+                       static_cast<float*>(x), ldx, rows, (int)cols, streams(dtype, rows, cols));
   else
     hipLaunchKernelGGL(k_unpack8<__bf16>, grid_of((rows * ((cols + 7) / 8) + 255) / 256), dim3(256), 0, st, q, c,
-                       static_cast<__bf16*>(x), ldx, rows, (int)cols);
+                       static_cast<__bf16*>(x), ldx, rows, (int)cols, streams(dtype, rows, cols));
   E3_HIP(hipGetLastError());
   return E3_OK;
 }
@@ -441,6 +442,7 @@ e3_status e3_layer_norm_fwd(e3_dtype dtype, const void* x, int64_t ldx, const vo
   NormArgs a{};
   a.x = x, a.ldx = ldx, a.gamma = gamma, a.beta = beta, a.eps = eps, a.y = y, a.ldy = ldy, a.mean = mean;
   a.rstd = rstd, a.xq = xq, a.xc = xc, a.yq = yq, a.yc = yc, a.rows = rows, a.cols = (int)cols;
+  a.nt = streams(dtype, rows, cols);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   return dtype == E3_F32 ? norm_fwd<float>(a, st) : norm_fwd<__bf16>(a, st);
 }
@@ -473,6 +475,7 @@ e3_status e3_layer_norm_bwd(e3_dtype dtype, const void* x, int64_t ldx, const in
   a.x = x, a.ldx = ldx, a.xq_in = xq, a.xc_in = xc, a.gamma = gamma, a.dy = dy, a.ldy = lddy, a.dx = dx;
   a.lddx = lddx, a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd);
   a.part = sums && rows ? static_cast<float*>(ws) : nullptr, a.rows = rows, a.cols = (int)cols;
+  a.nt = streams(dtype, rows, cols);
   a.blocks = rows ? norm_blocks(dtype, rows, (int)cols) : 0;
   if (rows) {
     const e3_status s = dtype == E3_F32 ? norm_bwd<float>(a, st) : norm_bwd<__bf16>(a, st);
