@@ -45,9 +45,9 @@ __device__ __forceinline__ unsigned term2(float& a, float& b) {
   return t;
 }
 
-// One operand of a tile product.
+// One operand of a tile product, or the pre-activation beside it.
 struct Side {
-  const void* p;      // full: rows (kAlong: output index, kAcross: reduction index) at p + i ld
+  const void* p;      // full: memory rows (kAlong: of an output index, kAcross: of a reduction index) at p + i ld
   int64_t ld;
   const int8_t* q;    // packed (p null): ld values and ldc exponents a row
   const uint8_t* c;
@@ -103,25 +103,22 @@ __device__ __forceinline__ u2v shift_down(u2v r, unsigned bits) {
 }
 __device__ __forceinline__ unsigned shift_down(unsigned r, unsigned bits) { return bits < 32 ? r >> bits : 0u; }
 
-// Loads of one operand's tile: N pieces a thread, of V values of memory rows.
+// A thread's N pieces of V values of a tile of memory rows of W values, as they
+// lie in memory; R and BK are the tile's output and reduction indexes.
 template <class T, Form F, int R, int BK, int THREADS, bool Q>
-struct Loader {
-  static constexpr int V = Elem<T>::V;
-  static constexpr int P = sizeof(T) == 2 || Q ? 1 : 3;   // planes
+struct Fetch {
+  static constexpr int V = Elem<T>::V, W = F == kAlong ? BK : R, PER = W / V, N = R * BK / V / THREADS;
   static constexpr int BITS = Q ? 8 : 8 * sizeof(T);      // of a value
-  using Lds = Plane<F, R, BK, P>;
+  static_assert(N * V * THREADS == R * BK && THREADS % PER == 0);
   using E = typename std::conditional<Q, int8_t, T>::type;
   using Raw = typename std::conditional<Q, typename std::conditional<V == 4, unsigned, u2v>::type, u4v>::type;
   typedef Raw Any __attribute__((aligned(sizeof(E))));
-  static constexpr int PER = Lds::W / V;                  // pieces of a memory row
-  static constexpr int N = R * BK / V / THREADS;
-  static_assert(N * V * THREADS == R * BK && THREADS % PER == 0);
-  static_assert(!Q || F == kAcross);
   Raw raw[N];
   unsigned char exps[Q ? N : 1];
 
   static __device__ __forceinline__ int row_of(int i) { return threadIdx.x / PER + i * (THREADS / PER); }
   static __device__ __forceinline__ int col_of() { return threadIdx.x % PER * V; }
+  static __device__ __forceinline__ bool whole_cols(int64_t r0, int64_t rows) { return F == kAlong || r0 + W <= rows; }
 
   // The tile at output index r0 and reduction index k0 of an operand with `rows`
   // output indexes; reduction indexes from `end` on are zero; output indexes
@@ -131,9 +128,6 @@ struct Loader {
   // registers were copied where the ways meet, which waits for the loads).
   // Otherwise a piece that crosses a row's end is loaded from where it still
   // fits and moved down; only rows shorter than a piece go by values.
-  static __device__ __forceinline__ bool whole_cols(int64_t r0, int64_t rows) {
-    return F == kAlong || r0 + Lds::W <= rows;
-  }
   template <bool WHOLE>
   __device__ __forceinline__ void load(const Side& s, int64_t r0, int64_t rows, int64_t k0, int64_t end) {
     // memory row m0 + row_of(i), column c0 + col_of(): the uniform part in the base
@@ -185,32 +179,80 @@ struct Loader {
       }
     }
   }
-  __device__ __forceinline__ void store(Lds& l) const {
+  // The values of piece i.
+  __device__ __forceinline__ void get(int i, float (&v)[V]) const {
+    if constexpr (Q) {
+      Raw8<V> r;
+      r.e = exps[i];
+      if constexpr (V == 4) r.w[0] = raw[i]; else r.w[0] = raw[i].x, r.w[1] = raw[i].y;
+      get8(r, v);
+    } else {
+      Elem<T>::get(__builtin_bit_cast(typename Elem<T>::vec, raw[i]), v);
+    }
+  }
+};
+
+// What an operand is: as it is, packed, or dy act'(z) from dy and z in full or
+// packed (the last two never exist in memory; in bfloat16 they are rounded here,
+// as operands of the instruction).
+enum Kind { kFull, kPacked, kGradFull, kGradPacked };
+
+// One operand's way from memory to LDS.
+template <class T, Form F, int R, int BK, int THREADS, Kind KD>
+struct Loader {
+  static constexpr int V = Elem<T>::V;
+  static constexpr bool Q = KD == kPacked, G = KD >= kGradFull;
+  static constexpr int P = sizeof(T) == 2 || Q ? 1 : 3;   // planes
+  using Lds = Plane<F, R, BK, P>;
+  using Main = Fetch<T, F, R, BK, THREADS, Q>;
+  using Pre = Fetch<T, F, R, BK, THREADS, KD == kGradPacked>;
+  static constexpr int N = Main::N;
+  struct None {};
+  Main x;
+  typename std::conditional<G, Pre, None>::type z;
+
+  static __device__ __forceinline__ bool whole_cols(int64_t r0, int64_t rows) { return Main::whole_cols(r0, rows); }
+  template <bool WHOLE>
+  __device__ __forceinline__ void load(const Side& s, const Side& pre, int64_t r0, int64_t rows, int64_t k0,
+                                       int64_t end) {
+    x.template load<WHOLE>(s, r0, rows, k0, end);
+    if constexpr (G) z.template load<WHOLE>(pre, r0, rows, k0, end);
+  }
+  // To LDS; `sum` (where wanted) grows by the values of the thread's columns.
+  template <bool SUM>
+  __device__ __forceinline__ void store(Lds& l, int act, float (&sum)[V]) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int row = row_of(i), col = col_of();
+      const int row = Main::row_of(i), col = Main::col_of();
       const int o = Lds::off(row, col / 8) + col % 8;
-      if constexpr (!Q && sizeof(T) == 2) {
-        *reinterpret_cast<u4v*>(&l.v[0][o]) = raw[i];
-      } else if constexpr (Q) {
-        // q and the step are exact in bf16; float32 tiles are scaled
-        const float st = step8(exps[i]) * (sizeof(T) == 4 ? kTermScale : 1.0f);
-        unsigned w[V / 4], b[V / 2];
-        if constexpr (V == 4) w[0] = raw[i]; else w[0] = raw[i].x, w[1] = raw[i].y;
-#pragma unroll
-        for (int e = 0; e < V / 2; ++e) {
-          const unsigned t = w[e / 2] >> (16 * (e % 2));
-          b[e] = pack2((float)(int)(int8_t)t * st, (float)(int)(int8_t)(t >> 8) * st);
-        }
-        if constexpr (V == 4) *reinterpret_cast<u2v*>(&l.v[0][o]) = u2v{b[0], b[1]};
-        else *reinterpret_cast<u4v*>(&l.v[0][o]) = u4v{b[0], b[1], b[2], b[3]};
+      if constexpr (KD == kFull && sizeof(T) == 2 && !SUM) {
+        *reinterpret_cast<u4v*>(&l.v[0][o]) = x.raw[i];
       } else {
-        const f4v r = __builtin_bit_cast(f4v, raw[i]);
-        float a = r.x * kTermScale, b = r.y * kTermScale, c = r.z * kTermScale, d = r.w * kTermScale;
+        float v[V];
+        x.get(i, v);
+        if constexpr (G) {
+          float w[V];
+          z.get(i, w);
+          act_grad_piece(act, w, v);
+        }
+        if constexpr (SUM)
 #pragma unroll
-        for (int t = 0; t < 3; ++t) {
-          const unsigned x = term2(a, b), y = term2(c, d);
-          *reinterpret_cast<u2v*>(&l.v[t][o]) = u2v{x, y};
+          for (int e = 0; e < V; ++e) sum[e] += v[e];
+        if constexpr (P == 1) {
+          // packed values are exact; those of float32 tiles are scaled
+          unsigned b[V / 2];
+#pragma unroll
+          for (int e = 0; e < V / 2; ++e)
+            b[e] = sizeof(T) == 4 ? pack2(v[2 * e] * kTermScale, v[2 * e + 1] * kTermScale) : pack2(v[2 * e], v[2 * e + 1]);
+          if constexpr (V == 4) *reinterpret_cast<u2v*>(&l.v[0][o]) = u2v{b[0], b[1]};
+          else *reinterpret_cast<u4v*>(&l.v[0][o]) = u4v{b[0], b[1], b[2], b[3]};
+        } else {
+          float a = v[0] * kTermScale, b = v[1] * kTermScale, c = v[2] * kTermScale, d = v[3] * kTermScale;
+#pragma unroll
+          for (int t = 0; t < 3; ++t) {
+            const unsigned x = term2(a, b), y = term2(c, d);
+            *reinterpret_cast<u2v*>(&l.v[t][o]) = u2v{x, y};
+          }
         }
       }
     }
@@ -220,11 +262,11 @@ struct Loader {
 // The tile and its reduction.  WM x WN waves; acc[i][j]: rows 32 i on and
 // columns 32 j on of the wave's part; the columns take the instruction's A side,
 // so that a lane holds row l % 32 and columns 8 (e / 4) + 4 (l / 32) + e % 4.
-template <class T, Form FA, Form FB, int BM, int BN, int BK, int WM, int WN, bool QA, int BUFS>
+template <class T, Form FA, Form FB, int BM, int BN, int BK, int WM, int WN, Kind KA, Kind KB, bool SUM, int BUFS>
 struct Tile {
   static constexpr int THREADS = WM * WN * kWave, TM = BM / WM, TN = BN / WN, RM = TM / 32, RN = TN / 32;
-  using LA = Loader<T, FA, BM, BK, THREADS, QA>;
-  using LB = Loader<T, FB, BN, BK, THREADS, false>;
+  using LA = Loader<T, FA, BM, BK, THREADS, KA>;
+  using LB = Loader<T, FB, BN, BK, THREADS, KB>;
   static constexpr int PITCH = TN + 4;                    // floats of a row of the results' staging
   union Shared {
     struct {
@@ -232,10 +274,12 @@ struct Tile {
       typename LB::Lds b;
     } in[BUFS];
     float out[WM * WN][32][PITCH];
+    float sums[SUM ? THREADS / LB::Main::PER : 1][SUM ? BN : 1];
   };
   static constexpr float kBack = sizeof(T) == 2 ? 1.0f : kTermBack;
 
   f16v acc[RM][RN];
+  float sum[LB::V];  // SUM: of this thread's columns of B
 
   __device__ __forceinline__ void step(const typename LA::Lds& a, const typename LB::Lds& b, int row0, int col0) {
     constexpr int PA = LA::P, PB = LB::P;
@@ -266,8 +310,14 @@ struct Tile {
     }
   }
 
-  // Sums over reduction indexes [k0, end) of the tile at (r0, c0) of rows x cols.
-  __device__ __forceinline__ void run(Shared& sh, const Side& sa, const Side& sb, int64_t r0, int64_t rows, int c0,
+  struct Args {
+    Side a, b, z;      // z: beside the operand that is a gradient
+    int act;
+  };
+  // Sums over reduction indexes [k0, end) of the tile at (r0, c0) of rows x cols
+  // (ONLY: the column sums of B alone).
+  template <bool ONLY>
+  __device__ __forceinline__ void run(Shared& sh, const Args& g, int64_t r0, int64_t rows, int c0,
                                       int cols, int64_t k0, int64_t end) {
     const int w = uniform(threadIdx.x / kWave), row0 = w / WN * TM, col0 = w % WN * TN;
 #pragma unroll
@@ -276,36 +326,60 @@ struct Tile {
       for (int j = 0; j < RN; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    if constexpr (SUM)
+#pragma unroll
+      for (int e = 0; e < LB::V; ++e) sum[e] = 0.0f;
     const int64_t whole = LA::whole_cols(r0, rows) && LB::whole_cols(c0, cols) ? k0 + (end - k0) / BK * BK : k0;
-    steps<true>(sh, sa, sb, r0, rows, c0, cols, k0, whole, row0, col0);
-    steps<false>(sh, sa, sb, r0, rows, c0, cols, whole, end, row0, col0);
+    steps<true, ONLY>(sh, g, r0, rows, c0, cols, k0, whole, row0, col0);
+    steps<false, ONLY>(sh, g, r0, rows, c0, cols, whole, end, row0, col0);
   }
-  template <bool WHOLE>
-  __device__ __forceinline__ void steps(Shared& sh, const Side& sa, const Side& sb, int64_t r0, int64_t rows, int c0,
-                                        int cols, int64_t k, int64_t end, int row0, int col0) {
+  template <bool WHOLE, bool ONLY>
+  __device__ __forceinline__ void steps(Shared& sh, const Args& g, int64_t r0, int64_t rows, int c0, int cols, int64_t k,
+                                        int64_t end, int row0, int col0) {
     if (k >= end) return;
     LA la;
     LB lb;
-    la.template load<WHOLE>(sa, r0, rows, k, end);
-    lb.template load<WHOLE>(sb, c0, cols, k, end);
+    auto load = [&](int64_t at) {
+      if constexpr (!ONLY) la.template load<WHOLE>(g.a, g.z, r0, rows, at, end);
+      lb.template load<WHOLE>(g.b, g.z, c0, cols, at, end);
+    };
+    auto store = [&](int buf) {
+      float none[LA::V];
+      if constexpr (!ONLY) la.template store<false>(sh.in[buf].a, g.act, none);
+      lb.template store<SUM>(sh.in[buf].b, g.act, sum);
+    };
+    load(k);
     __syncthreads();
     int cur = 0;
-    if constexpr (BUFS == 2) la.store(sh.in[0].a), lb.store(sh.in[0].b);
+    if constexpr (BUFS == 2) store(0);
     for (; k < end; k += BK) {
-      if constexpr (BUFS == 1) la.store(sh.in[0].a), lb.store(sh.in[0].b);
+      if constexpr (BUFS == 1) store(0);
       __syncthreads();
       const bool more = k + BK < end;
-      if (more) {
-        la.template load<WHOLE>(sa, r0, rows, k + BK, end);
-        lb.template load<WHOLE>(sb, c0, cols, k + BK, end);
-      }
-      step(sh.in[cur].a, sh.in[cur].b, row0, col0);
+      if (more) load(k + BK);
+      if constexpr (!ONLY) step(sh.in[cur].a, sh.in[cur].b, row0, col0);
       if constexpr (BUFS == 1) {
         __syncthreads();
       } else {
-        if (more) la.store(sh.in[cur ^ 1].a), lb.store(sh.in[cur ^ 1].b);
+        if (more) store(cur ^ 1);
         cur ^= 1;
       }
+    }
+  }
+  // The column sums of B over the tile's reduction, f(col, value), col within the
+  // tile: the threads of a column in order.
+  template <class Fn>
+  __device__ __forceinline__ void finish_sums(Shared& sh, Fn&& f) {
+    using M = typename LB::Main;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < LB::V; ++e) sh.sums[threadIdx.x / M::PER][M::col_of() + e] = sum[e];
+    __syncthreads();
+    if (threadIdx.x < BN) {
+      float v = 0.0f;
+#pragma unroll
+      for (int r = 0; r < THREADS / M::PER; ++r) v += sh.sums[r][threadIdx.x];
+      f((int)threadIdx.x, v);
     }
   }
 

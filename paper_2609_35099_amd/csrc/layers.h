@@ -338,41 +338,42 @@ __device__ __forceinline__ void act_grad_piece(int act, const float (&z)[V], flo
 }
 
 // ------------------------------------------------------------ column sums
-// out_s[col] = sum over p of part[p][s][col], s = 0, 1 (either output may be
-// null), in a fixed order: 32 threads of a column take every 32nd partial in
-// eight running sums (loads of 16 columns are in flight together: latency is all
-// there is to it), then their sums are added in order.
+// Sums over p of part[p pitch + c], c < n0 to out0 and n0 <= c < n to out1
+// (either may be null), in a fixed order: 32 threads of a column take every 32nd
+// partial in eight running sums (16 columns' loads are in flight together:
+// latency is all there is to it), then their sums are added in order.
 template <class T>
-__global__ __launch_bounds__(512) void k_column_sums(const float* part, int parts, int sets, int cols, T* out0,
-                                                     T* out1) {
+__global__ __launch_bounds__(512) void k_column_sums(const float* part, int parts, int64_t pitch, int64_t n0, int64_t n,
+                                                     T* out0, T* out1) {
   __shared__ float s[32][17];
-  const int c = threadIdx.x % 16, p0 = threadIdx.x / 16, col = (int)blockIdx.x * 16 + c, set = blockIdx.y;
-  T* out = set ? out1 : out0;
-  if (!out) return;
+  const int c = threadIdx.x % 16, p0 = threadIdx.x / 16;
+  const int64_t first = block_id() * 16, col = first + c;
+  if (first >= n || (!out0 && first + 16 <= n0) || (!out1 && first >= n0)) return;
   float t[8] = {};
-  if (col < cols)
+  if (col < n)
     for (int p = p0; p < parts; p += 256)
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (p + 32 * i < parts) t[i] += part[((int64_t)(p + 32 * i) * sets + set) * cols + col];
+        if (p + 32 * i < parts) t[i] += part[(p + 32 * i) * pitch + col];
   s[p0][c] = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
   __syncthreads();
-  if (p0 != 0 || col >= cols) return;
+  if (p0 != 0 || col >= n) return;
   float v = 0.0f;
 #pragma unroll
   for (int p = 0; p < 32; ++p) v += s[p][c];
-  out[col] = (T)v;
+  T* out = col < n0 ? out0 + col : out1 + (col - n0);
+  if (col < n0 ? out0 != nullptr : out1 != nullptr) *out = (T)v;
 }
 
-inline e3_status column_sums(e3_dtype dtype, const float* part, int parts, int sets, int cols, void* out0, void* out1,
-                             hipStream_t st) {
+inline e3_status column_sums(e3_dtype dtype, const float* part, int parts, int64_t pitch, int64_t n0, int64_t n,
+                             void* out0, void* out1, hipStream_t st) {
   TimedLaunch t_("column_sums", st);
-  const dim3 grid((cols + 15) / 16, sets);
+  const dim3 grid = grid_of((n + 15) / 16);
   if (dtype == E3_F32)
-    hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(512), 0, st, part, parts, sets, cols,
+    hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(512), 0, st, part, parts, pitch, n0, n,
                        static_cast<float*>(out0), static_cast<float*>(out1));
   else
-    hipLaunchKernelGGL(k_column_sums<__bf16>, grid, dim3(512), 0, st, part, parts, sets, cols,
+    hipLaunchKernelGGL(k_column_sums<__bf16>, grid, dim3(512), 0, st, part, parts, pitch, n0, n,
                        static_cast<__bf16*>(out0), static_cast<__bf16*>(out1));
   E3_HIP(hipGetLastError());
   return E3_OK;

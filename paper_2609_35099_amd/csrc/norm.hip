@@ -482,7 +482,7 @@ e3_status e3_layer_norm_bwd(e3_dtype dtype, const void* x, int64_t ldx, const in
     if (s != E3_OK) return s;
   }
   if (!sums) return E3_OK;
-  return column_sums(dtype, static_cast<const float*>(ws), a.blocks, 2, (int)cols, dgamma, dbeta, st);
+  return column_sums(dtype, static_cast<const float*>(ws), a.blocks, 2 * cols, cols, 2 * cols, dgamma, dbeta, st);
 }
 
 }  // extern "C"
