@@ -8,7 +8,7 @@
    and their table.
 2. hipcc compiles the core unit (csrc/e3mi.hip: C ABI, graph, linear mixing,
    record tensor product, probes), the record convolution (csrc/convr.hip:
-   layouts without a compiled unit), the invariant layers (csrc/dense.hip,
+   layouts without a compiled unit), the invariant layers (csrc/dense*.hip,
    csrc/norm.hip), every layout unit and the builder for gfx950, in parallel,
    and links libe3mi.so next to this file.
 
@@ -94,7 +94,7 @@ def build(verbose: bool = True, extra=None) -> str:
     objdir = os.path.join(BUILD, "obj")
     os.makedirs(objdir, exist_ok=True)
     sources = [os.path.join(CSRC, "e3mi.hip"), os.path.join(CSRC, "convr.hip"),
-               os.path.join(CSRC, "dense.hip"), os.path.join(CSRC, "norm.hip"),
+               *(os.path.join(CSRC, f) for f in ("dense.hip", "dense_bwd_f32.hip", "dense_bwd_bf16.hip", "norm.hip")),
                os.path.join(CSRC, "builder.cpp")] + \
               [os.path.join(GEN, u) for u in units]
     objs = []

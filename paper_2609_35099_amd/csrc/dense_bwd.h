@@ -1,0 +1,159 @@
+// Dense layers: the backward, for the type of the including unit.
+#pragma once
+#include "dense.h"
+
+namespace {
+
+// The column sums of B alone, in the order in which the product sums them.
+template <class J, int B>
+__global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void k_dense_sums(DenseArgs a) {
+  using Tl = typename TileOf<J, B>::type;
+  __shared__ __align__(16) typename Tl::Shared sh;
+  dense_block<J, Tl, B, B, true>(a, sh, block_id());
+}
+// Two products in one launch: the first `first` blocks take the first.
+template <class J, class K, int B>
+__global__ __launch_bounds__((TileOf<J, B>::THREADS), 2) void k_dense_two(DenseArgs a, DenseArgs b, int64_t first) {
+  using Ta = typename TileOf<J, B>::type;
+  using Tb = typename TileOf<K, B>::type;
+  static_assert(Ta::THREADS == Tb::THREADS);
+  __shared__ __align__(16) union {
+    typename Ta::Shared a;
+    typename Tb::Shared b;
+  } sh;
+  const int64_t u = block_id();
+  if (u < first) dense_block<J, Ta, B, B>(a, sh.a, u);
+  else dense_block<K, Tb, B, B>(b, sh.b, u - first);
+}
+
+// dz = dy act'(z) in the type of dy (a bfloat16 dz is an operand of the matrix
+// instructions, which take no more bits), and the column sums of its unrounded
+// values over the block's rows, for layers whose products would form dz too often
+// themselves (kOnTheFly).  Either output may be null.
+template <class T>
+__global__ __launch_bounds__(256) void k_dense_dz(RowsIn<T> z, int act, const T* dy, int64_t lddy, T* dz, float* part,
+                                                  int64_t rows, int cols, int64_t per) {
+  constexpr int V = Elem<T>::V, CL = 16, RL = 256 / CL;
+  __shared__ float s[RL][CL * V];
+  const int cl = threadIdx.x % CL, rl = threadIdx.x / CL;
+  const int col = ((int)blockIdx.y * CL + cl) * V, n = cols - col;
+  const int64_t row0 = blockIdx.x * per, row1 = row0 + per < rows ? row0 + per : rows;
+  float sum[V] = {};
+  for (int64_t row = row0 + rl; row < row1; row += RL) {
+    float u[V];
+    ld_piece<T>(dy + row * lddy + col, n, u);
+    if (act != E3_ACT_NONE) {
+      float w[V];
+      z.load(row, col, cols, w);
+      act_grad_piece(act, w, u);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[i] += u[i];
+    if (dz) st_piece<T>(dz + row * cols + col, n, u);
+  }
+  if (!part) return;
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[rl][cl * V + i] = sum[i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < CL * V; i += 256) {
+    const int c = (int)blockIdx.y * CL * V + i;
+    if (c >= cols) continue;
+    float v = 0.0f;
+#pragma unroll
+    for (int r = 0; r < RL; ++r) v += s[r][i];
+    part[(int64_t)blockIdx.x * cols + c] = v;
+  }
+}
+
+// ------------------------------------------------------------ host
+// dx and dW (FLY: and db) of a layer whose operand dz is of kind KD and x of KX.
+template <class T, Kind KD, Kind KX, bool FLY>
+e3_status dense_bwd_products(DenseArgs x, DenseArgs w, float* part, hipStream_t st) {
+  constexpr e3_dtype t = std::is_same_v<T, float> ? E3_F32 : E3_BF16;
+  using JX = Job<T, kAlong, kAlong, KD, kFull, false>;
+  using JW = Job<T, kAcross, kAcross, KX, KD, FLY>;
+  const bool dx = x.y, dw = w.y, db = w.sums;
+  const Cut cx = dense_cut(t, x.rows, x.cols, x.red), cw = dense_cut(t, w.rows, w.cols, w.red);
+  set_cut(x, cx, part);
+  set_cut(w, cw, part + cut_bytes(cx, x.rows, x.cols) / sizeof(float), w.cols);
+  e3_status s = E3_OK;
+  if (dx && dw && cx.tile == 64 && cw.tile == 64) {
+    TimedLaunch t_("dense_bwd_both", st);
+    const int64_t first = cx.tiles * cx.splits;
+    hipLaunchKernelGGL((k_dense_two<JX, JW, 64>), grid_of(first + cw.tiles * cw.splits), dim3(256), 0, st, x, w, first);
+    E3_HIP(hipGetLastError());
+  } else {
+    if (dx) s = dense_launch<JX>(x, cx, "dense_bwd_dx", st);
+    if (s == E3_OK && dw) s = dense_launch<JW>(w, cw, "dense_bwd_dw", st);
+  }
+  if constexpr (FLY && KX == kFull) {
+    if (s == E3_OK && db && !dw) {
+      TimedLaunch t_("dense_bwd_db", st);
+      const dim3 grid = grid_of((w.cols + cw.tile - 1) / cw.tile * (int64_t)cw.splits);
+      auto go = [&](auto B) {
+        constexpr int b = decltype(B)::value;
+        hipLaunchKernelGGL((k_dense_sums<JW, b>), grid, dim3(TileOf<JW, b>::THREADS), 0, st, w);
+      };
+      if (cw.tile == 64) go(std::integral_constant<int, 64>{});
+      else if (cw.tile == 128) go(std::integral_constant<int, 128>{});
+      else if constexpr (sizeof(T) == 2) go(std::integral_constant<int, 256>{});
+      E3_HIP(hipGetLastError());
+    }
+  }
+  if (s == E3_OK && dx && cx.splits > 1) s = dense_join<T>(x, st);
+  // many partial sums of few columns take threads of their own (252 of 128 x 256: 6 us against 34)
+  if (s == E3_OK && (dw || db) && cw.splits > 1 && cw.splits <= 16) s = dense_join<T>(w, st);
+  if (s == E3_OK && (dw || db) && cw.splits > 16)
+    s = column_sums(t, w.part, cw.splits, w.pitch, w.rows * w.cols, w.pitch, w.y, w.sums, st);
+  return s;
+}
+
+template <class T>
+e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, int64_t lddy, T* dx, int64_t lddx, T* dW,
+                    T* db, char* ws, int64_t M, int64_t K, int64_t N, hipStream_t st) {
+  constexpr e3_dtype t = std::is_same_v<T, float> ? E3_F32 : E3_BF16;
+  const DenseBwdWs w = dense_bwd_ws(t, M, K, N);
+  const bool fly = K <= kOnTheFly;
+  T* dz = reinterpret_cast<T*>(ws);
+  float* dbp = reinterpret_cast<float*>(ws + w.dz);
+  float* part = reinterpret_cast<float*>(ws + w.dz + w.db);
+  const bool own = !fly && act != E3_ACT_NONE && (dx || dW);  // else dz is dy, or formed by the products
+  if (own || (db && !fly)) {
+    TimedLaunch t_("dense_dz", st);
+    const int per = 16 * Elem<T>::V;
+    hipLaunchKernelGGL(k_dense_dz<T>, dim3((unsigned)w.db_blocks, (unsigned)((N + per - 1) / per)), dim3(256), 0, st, z,
+                       act, dy, lddy, own ? dz : nullptr, db ? dbp : nullptr, M, (int)N, w.db_rows);
+    E3_HIP(hipGetLastError());
+  }
+  if (db && !fly) {
+    const e3_status s = column_sums(t, dbp, (int)w.db_blocks, N, N, N, db, nullptr, st);
+    if (s != E3_OK) return s;
+  }
+  DenseArgs ax{}, aw{};
+  const Side d{own ? dz : dy, own ? N : lddy}, pre{z.x, z.x ? z.ld : N, z.q, z.c, (N + kGroup - 1) / kGroup};
+  ax.a = d, ax.b = {W, N}, ax.pre = pre, ax.grad_act = act, ax.rows = M, ax.cols = (int)K, ax.red = N;
+  ax.y = dx, ax.ldy = lddx, ax.nt = streams(t, M, K);
+  aw.a = {x.x, x.x ? x.ld : K, x.q, x.c, (K + kGroup - 1) / kGroup}, aw.b = d, aw.pre = pre, aw.grad_act = act;
+  aw.rows = K, aw.cols = (int)N, aw.red = M, aw.y = dW, aw.ldy = N, aw.sums = fly ? db : nullptr;
+  auto run = [&](auto KD, auto FLY) {
+    constexpr Kind kd = decltype(KD)::value;
+    constexpr bool f = decltype(FLY)::value;
+    return dW && !x.x ? dense_bwd_products<T, kd, kPacked, f>(ax, aw, part, st)
+                      : dense_bwd_products<T, kd, kFull, f>(ax, aw, part, st);
+  };
+  using Full = std::integral_constant<Kind, kFull>;
+  if (!fly) return run(Full{}, std::false_type{});
+  if (act == E3_ACT_NONE) return run(Full{}, std::true_type{});
+  return z.x ? run(std::integral_constant<Kind, kGradFull>{}, std::true_type{})
+             : run(std::integral_constant<Kind, kGradPacked>{}, std::true_type{});
+}
+
+template <class T>
+e3_status dense_bwd_call(const DenseBwdCall& c) {
+  return dense_bwd<T>({static_cast<const T*>(c.x), c.ldx, c.xq, c.xc}, static_cast<const T*>(c.W),
+                      {static_cast<const T*>(c.z), c.ldz, c.zq, c.zc}, c.act, static_cast<const T*>(c.dy), c.lddy,
+                      static_cast<T*>(c.dx), c.lddx, static_cast<T*>(c.dW), static_cast<T*>(c.db), c.ws, c.M, c.K, c.N,
+                      c.st);
+}
+
+}  // namespace

@@ -307,6 +307,7 @@ struct Tile {
             for (int j = 0; j < RN; ++j)
               acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[q][j], x[p][i], acc[i][j], 0, 0, 0);
         }
+      if constexpr (RM * RN > 4) __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -404,7 +405,7 @@ struct Tile {
       // the wave's own writes: LDS serves a wave's accesses in order
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_wave_barrier();
-#pragma unroll
+#pragma unroll 2
       for (int r = 0; r < 32; r += PASS) {
         const int col = l % PER * V;
         float v[V];
