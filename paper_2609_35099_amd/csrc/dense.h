@@ -41,35 +41,59 @@ struct DenseArgs {
 };
 
 // What follows the sums of one piece of a row, row0 + lr with row0 uniform (so
-// that a thread multiplies by a row stride once, not per piece); the lanes of a
+// that a thread multiplies by a row stride once, not per piece).  The lanes of a
 // group of 32 columns take part together, also where rows (ok) or columns end.
+// The piece of the bias is loaded once for all rows, that of the residual ahead
+// of the sums.
+template <class T>
+struct Tail {
+  static constexpr int V = Elem<T>::V;
+  float bias[V];
+  __device__ __forceinline__ Tail(const DenseArgs& a, int col) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) bias[i] = 0.0f;
+    if (a.bias) ld_piece<T>(static_cast<const T*>(a.bias) + col, a.cols - col, bias);
+  }
+  using Raw = typename Elem<T>::vec;
+  static __device__ __forceinline__ Raw residual(const DenseArgs& a, int64_t row0, int lr, bool ok, int col) {
+    if (!a.res) return Raw{};
+    return ld_raw<T>(static_cast<const T*>(a.res) + (row0 * a.ldr + (lr * a.ldr + col)), ok ? a.cols - col : 0);
+  }
+  // FAST: the piece is inside the row and streams, with no branch around the store
+  // of y: in a loop over rows, the loads that the next round waits for are older
+  // than the stores, and only a known number of stores lets the wait leave them
+  // in flight.
+  template <bool FAST = false>
+  __device__ __forceinline__ void out(const DenseArgs& a, int64_t row0, int lr, bool ok, int col, Raw res,
+                                      float (&v)[V]) const {
+    const int n = FAST ? V : ok ? a.cols - col : 0;
+    auto at = [&](int64_t ld) { return row0 * ld + (lr * ld + col); };
+    auto pack = [&](int8_t* q, uint8_t* c) {
+      const int64_t groups = (a.cols + kGroup - 1) / kGroup;
+      pack8_piece<V>(v, col, n, q + (row0 * a.cols + (int64_t)lr * a.cols), c + (row0 * groups + lr * groups));
+    };
+    if (a.bias)
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] += bias[i];
+    if (a.z) st_piece<T>(static_cast<T*>(a.z) + at(a.ldz), n, v, a.nt);
+    if (a.zq) pack(a.zq, a.zc);
+    act_piece(a.act, v);
+    if (a.res) {
+      float u[V];
+      Elem<T>::get(res, u);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] += u[i];
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = Elem<T>::round(v[i]);
+    st_piece<T>(static_cast<T*>(a.y) + at(a.ldy), n, v, FAST || a.nt);
+    if (a.yq) pack(a.yq, a.yc);
+  }
+};
 template <class T, int V>
 __device__ __forceinline__ void dense_tail(const DenseArgs& a, int64_t row0, int lr, bool ok, int col, float (&v)[V]) {
-  static_assert(V == Elem<T>::V);
-  const int n = ok ? a.cols - col : 0;
-  auto at = [&](int64_t ld) { return row0 * ld + (lr * ld + col); };
-  auto pack = [&](int8_t* q, uint8_t* c) {
-    const int64_t groups = (a.cols + kGroup - 1) / kGroup;
-    pack8_piece<V>(v, col, n, q + (row0 * a.cols + (int64_t)lr * a.cols), c + (row0 * groups + lr * groups));
-  };
-  float u[V];
-  if (a.bias) {
-    ld_piece<T>(static_cast<const T*>(a.bias) + col, n, u);
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] += u[i];
-  }
-  if (a.z) st_piece<T>(static_cast<T*>(a.z) + at(a.ldz), n, v, a.nt);
-  if (a.zq) pack(a.zq, a.zc);
-  act_piece(a.act, v);
-  if (a.res) {
-    ld_piece<T>(static_cast<const T*>(a.res) + at(a.ldr), n, u);
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] += u[i];
-  }
-#pragma unroll
-  for (int i = 0; i < V; ++i) v[i] = Elem<T>::round(v[i]);
-  st_piece<T>(static_cast<T*>(a.y) + at(a.ldy), n, v, a.nt);
-  if (a.yq) pack(a.yq, a.yc);
+  const Tail<T> tail(a, col);
+  tail.out(a, row0, lr, ok, col, Tail<T>::residual(a, row0, lr, ok, col), v);
 }
 
 // Value (m, c) of a memory row m of a tile's operand.
@@ -103,6 +127,46 @@ struct Job {
   static constexpr Kind KA = KA_, KB = KB_;
   static constexpr bool SUM = SUM_;  // with the column sums of B
 };
+// The results of rows row0 to row0 + 31 and 32 RN columns from col0 on.
+template <class J, int RN, bool FAST = false>
+__device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_t row0, int col0, int64_t k0, int64_t end,
+                                           float (*out)[32 * RN + 4], const f16v (&acc)[RN]) {
+  using T = typename J::T;
+  using R = Rows32<T, RN>;
+  constexpr int V = R::V;
+  const int col = col0 + R::col(), lr = R::row();
+  const Tail<T> tail(a, col);
+  typename Tail<T>::Raw res[R::N];
+#pragma unroll
+  for (int i = 0; i < R::N; ++i)
+    res[i] = Tail<T>::residual(a, row0 + i * R::PASS, lr, row0 + i * R::PASS + lr < a.rows, col);
+  R::put(out, acc);
+  if constexpr (sizeof(T) == 4) {
+    if (R::bad(acc))
+      R::mend(out, [&](int r, int c) {
+        return row0 + r < a.rows && col0 + c < a.cols
+                   ? dense_again<T, J::FA, J::FB, J::KA, J::KB>(a, row0 + r, col0 + c, k0, end)
+                   : 0.0f;
+      });
+  }
+#pragma unroll
+  for (int i = 0; i < R::N; ++i) {
+    const int64_t rowu = row0 + i * R::PASS;
+    const bool ok = FAST || rowu + lr < a.rows;
+    float v[V];
+    R::get(out, i, v);
+    if (!FAST && a.part) {
+      float* p = a.part + (split * a.pitch + rowu * a.cols) + ((int64_t)lr * a.cols + col);
+#pragma unroll
+      for (int e = 0; e < V; e += 4)
+        st_piece<float>(p + e, (ok ? a.cols - col : 0) - e, reinterpret_cast<float(&)[4]>(v[e]));
+    } else {
+      tail.template out<FAST>(a, rowu, lr, ok, col, res[i], v);
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Tiles by type and size; what a library product reaches is 1,070 TFLOP/s in
 // bfloat16 and 143 in float32 (16,384 x 1,024 x 4,096).
 //   bfloat16, 256 x 256: 16 waves of 64 x 64, steps of 32, two buffers, one
@@ -163,34 +227,9 @@ __device__ __forceinline__ void dense_block(const DenseArgs& a, typename Tl::Sha
       });
   }
   if constexpr (!ONLY)
-  t.finish(sh, [&](int r, int lr, int c, float(&v)[V]) {
-    const int64_t rowu = r0 + r, row = rowu + lr;
-    const int col = c0 + c;
-    const int n = row < a.rows ? a.cols - col : 0;
-    if constexpr (sizeof(T) == 4) {
-      float z = 0.0f;
-#pragma unroll
-      for (int e = 0; e < V; ++e) z += v[e] * 0.0f;
-      if (z != 0.0f) {
-        float t[V];
-#pragma clang loop unroll(disable)
-        for (int e = 0; e < V; ++e) {
-          const float again = e < n ? dense_again<T, J::FA, J::FB, J::KA, J::KB>(a, row, col + e, k0, end) : 0.0f;
-#pragma unroll
-          for (int q = 0; q < V; ++q) t[q] = q == e ? again : t[q];
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = v[e] * 0.0f != 0.0f ? t[e] : v[e];
-      }
-    }
-    if (a.part) {
-      float* p = a.part + (split * a.pitch + rowu * a.cols) + ((int64_t)lr * a.cols + col);
-#pragma unroll
-      for (int e = 0; e < V; e += 4) st_piece<float>(p + e, n - e, reinterpret_cast<float(&)[4]>(v[e]));
-    } else {
-      dense_tail<T, V>(a, rowu, lr, row < a.rows, col, v);
-    }
-  });
+    t.finish(sh, [&](int r, int c, auto out, auto& acc) {
+      rows32_out<J, Tl::RN>(a, split, r0 + r, c0 + c, k0, end, out, acc);
+    });
 }
 template <class J, int B>
 __global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void k_dense(DenseArgs a) {
@@ -198,6 +237,179 @@ __global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void 
   __shared__ __align__(16) typename Tl::Shared sh;
   dense_block<J, Tl, B, B>(a, sh, block_id());
 }
+// Short reductions (up to 16 KK) over many rows: no LDS and no barriers before the
+// epilogue.  A wave keeps the terms of its 32 NC columns of B in registers for
+// good and walks row blocks of 32; lane l loads the eight values of row l % 32 at
+// reduction indexes 16 kk + 8 (l / 32) on straight into the instruction's operand
+// order, the next block's while it works on one.  The waves of a workgroup take
+// neighbouring columns of the same rows.
+// What bounds a short reduction is the write of y; tiles through LDS wait for
+// their own loads, barriers and stores in turn (156,000 x 64 x 1,664 float32: 421
+// us with tiles, @PANEL@ here).
+template <class J, int KK, int NC, bool FAST>
+__global__ __launch_bounds__(256, 2) void k_dense_panel(DenseArgs a) {
+  using T = typename J::T;
+  using R = Rows32<T, NC>;
+  constexpr bool f32 = sizeof(T) == 4;
+  constexpr int V = Elem<T>::V, P = f32 ? 3 : 1, Q = 8 / V;
+  constexpr bool GF = J::KA == kGradFull, GP = J::KA == kGradPacked;
+  static_assert(J::FA == kAlong && J::KA != kPacked && J::KB == kFull && !J::SUM);
+  __shared__ __align__(16) float out[4][32][R::PITCH];
+  const int l = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), K = (int)a.red;
+  const int groups = (a.cols + 32 * NC - 1) / (32 * NC);
+  const int64_t w = block_id() * 4 + wave;
+  const int64_t chunk = w / groups;
+  if (chunk >= a.splits) return;
+  const int col0 = (int)(w % groups) * 32 * NC;
+  const int h = 8 * (l / 32);
+  // the wave's columns of B
+  bf8v wf[P][KK][NC];
+#pragma unroll
+  for (int k = 0; k < KK; ++k)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int col = col0 + 32 * c + l % 32;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int at = 16 * k + h + e;
+        const T* b = static_cast<const T*>(a.b.p);
+        v[e] = at < K && col < a.cols ? Elem<T>::one(J::FB == kAlong ? b[col * a.b.ld + at] : b[at * a.b.ld + col]) : 0.0f;
+        if (f32) v[e] *= kTermScale;
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        u4v t;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = term2(v[2 * e], v[2 * e + 1]);
+        wf[p][k][c] = __builtin_bit_cast(bf8v, t);
+      }
+    }
+  // a row block's values, as they lie in memory
+  typename Elem<T>::vec x[KK][Q], zf[GF ? KK : 1][Q];
+  Raw8<8> zp[GP ? KK : 1];
+  const T* xp = static_cast<const T*>(a.a.p);
+  const T* zfp = static_cast<const T*>(a.pre.p);
+  auto load = [&](auto fast, int64_t block) {
+    constexpr bool F = decltype(fast)::value;
+    const int last = F ? 31 : a.rows - block * 32 < 32 ? (int)(a.rows - block * 32) - 1 : 31;
+    const int64_t m = imin(l % 32, last);
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      const int at = 16 * k + h;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int n = F ? V : K - at - q * V;
+        x[k][q] = ld_raw<T>(xp + block * 32 * a.a.ld + (m * a.a.ld + at + q * V), n);
+        if constexpr (GF) zf[k][q] = ld_raw<T>(zfp + block * 32 * a.pre.ld + (m * a.pre.ld + at + q * V), n);
+      }
+      if constexpr (GP)
+        zp[k] = ld_raw8<8>(a.pre.q + block * 32 * a.pre.ld + m * a.pre.ld,
+                           a.pre.c + block * 32 * a.pre.ldc + m * a.pre.ldc, at, F ? 8 : K - at);
+    }
+  };
+  bf8v xf[P][KK];
+  auto terms = [&]() {
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      if constexpr (!f32 && !GF && !GP) {
+        xf[0][k] = __builtin_bit_cast(bf8v, x[k][0]);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) Elem<T>::get(x[k][q], reinterpret_cast<float(&)[V]>(v[q * V]));
+        if constexpr (GF || GP) {
+          float z[8];
+          if constexpr (GP) {
+            get8(zp[k], z);
+          } else {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) Elem<T>::get(zf[k][q], reinterpret_cast<float(&)[V]>(z[q * V]));
+          }
+          act_grad_piece(a.grad_act, z, v);
+        }
+        if constexpr (f32)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= kTermScale;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          u4v t;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t[e] = term2(v[2 * e], v[2 * e + 1]);
+          xf[p][k] = __builtin_bit_cast(bf8v, t);
+        }
+      }
+    }
+  };
+  auto product = [&](auto fast, int64_t block) {
+    f16v acc[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[c][e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KK; ++k)
+#pragma unroll
+      for (int s = 2 * P - 2 < 2 ? 2 * P - 2 : 2; s >= 0; --s)
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const int q = s - p;
+          if (q < 0 || q >= P) continue;
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[q][k][c], xf[p][k], acc[c], 0, 0, 0);
+        }
+    rows32_out<J, NC, decltype(fast)::value>(a, 0, block * 32, col0, 0, a.red, out[wave], acc);
+  };
+  // FAST: whole row blocks by a loop without branches around loads and stores, and
+  // what is left of the rows after it
+  const int64_t blocks = FAST ? a.rows / 32 : (a.rows + 31) / 32;
+  const std::integral_constant<bool, FAST> fast;
+  if (chunk < blocks) {
+    load(fast, chunk);
+    for (int64_t block = chunk; block < blocks; block += a.splits) {
+      terms();
+      // the last round loads a block again, so that every round has the same loads
+      load(fast, block + a.splits < blocks ? block + a.splits : block);
+      product(fast, block);
+    }
+  }
+  if (FAST && a.rows % 32 && chunk == blocks % a.splits) {
+    load(std::false_type{}, blocks);
+    terms();
+    product(std::false_type{}, blocks);
+  }
+}
+// Whether a product goes that way: a reduction that fits the registers beside its
+// columns, and rows enough for the waves to walk.
+template <class T>
+constexpr int kPanel = sizeof(T) == 4 ? 64 : 128;
+template <class T>
+bool panel(int64_t rows, int64_t cols, int64_t red) {
+  return red <= kPanel<T> && ((rows + 31) / 32) * ((cols + 63) / 64) >= 8192;
+}
+template <class J>
+e3_status dense_panel(DenseArgs a, const char* name, hipStream_t st) {
+  using T = typename J::T;
+  const int64_t groups = (a.cols + 63) / 64;
+  // two workgroups per CU, each wave on row blocks of its own
+  a.splits = (int)std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 2048 / groups));
+  const int64_t blocks = (a.splits * groups + 3) / 4;
+  TimedLaunch t_(name, st);
+  constexpr int U = kPanel<T> / 64;  // 16-index pieces in units of a quarter of the longest
+  const bool fast = a.red % (16 * U) == 0 && a.red >= 32 * U && a.cols % 64 == 0 && a.nt;
+  auto go = [&](auto KK) {
+    constexpr int kk = decltype(KK)::value;
+    auto* k = fast ? k_dense_panel<J, kk, 2, true> : k_dense_panel<J, kk, 2, false>;
+    hipLaunchKernelGGL(k, grid_of(blocks), dim3(256), 0, st, a);
+  };
+  if (a.red <= 32 * U) go(std::integral_constant<int, 2 * U>{});
+  else if (a.red <= 48 * U) go(std::integral_constant<int, 3 * U>{});
+  else go(std::integral_constant<int, 4 * U>{});
+  E3_HIP(hipGetLastError());
+  return E3_OK;
+}
+
 // The partial sums of the splits, in order, and the epilogue; after the last row
 // the column sums beside them.
 template <class T>

@@ -13,13 +13,14 @@ namespace {
 // columns stay in registers, rows go by with the next one's x in flight, and no
 // LDS is used; L lanes share a row.  Bound by the write of y: 1,248,000 x 8 x 64
 // float32 @THIN@ us, where the tile product took 156 (its steps are of 32).
-template <class T, int L, int KC>
+template <class T, int L, int KC, bool FAST>
 __global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {
   constexpr int V = Elem<T>::V, R = 256 / L, P = KC / V > 0 ? KC / V : 1;
   const int K = (int)a.red, col = ((int)blockIdx.y * L + (int)threadIdx.x % L) * V, n = a.cols - col;
   const T* W = static_cast<const T*>(a.b.p);
   const T* x = static_cast<const T*>(a.a.p);
-  float w[KC][V], bias[V] = {};
+  float w[KC][V];
+  const Tail<T> tail(a, col);
 #pragma unroll
   for (int k = 0; k < KC; ++k) {
     if (k < K) {
@@ -29,46 +30,72 @@ __global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {
       for (int i = 0; i < V; ++i) w[k][i] = 0.0f;
     }
   }
-  if (a.bias) ld_piece<T>(static_cast<const T*>(a.bias) + col, n, bias);
-  a.bias = nullptr;
   // U rows a thread and round, the next round's x in flight: with one, the rows'
   // latency was most of the time (@ONE@ us)
   constexpr int U = 4;
   constexpr int TR = R * U;  // rows of a round
   const int lr = threadIdx.x / L;
   typename Elem<T>::vec raw[U][P];
-  auto load = [&](int64_t tile) {
+  auto load = [&](auto fast, int64_t tile) {
+    constexpr bool F = decltype(fast)::value;
     const T* xt = x + tile * TR * a.a.ld;
-    const int last = a.rows - tile * TR < TR ? (int)(a.rows - tile * TR) - 1 : TR - 1;
+    const int last = F ? TR - 1 : a.rows - tile * TR < TR ? (int)(a.rows - tile * TR) - 1 : TR - 1;
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int64_t at = imin(lr + j * R, last) * a.a.ld;
 #pragma unroll
-      for (int p = 0; p < P; ++p) raw[j][p] = ld_raw<T>(xt + at + p * V, K - p * V);
+      for (int p = 0; p < P; ++p) raw[j][p] = ld_raw<T>(xt + at + p * V, F ? V : K - p * V);
     }
   };
-  int64_t tile = blockIdx.x;
-  if (tile * TR < a.rows) load(tile);
-  for (; tile * TR < a.rows; tile += gridDim.x) {
-    float v[U][V];
+  float v[U][V];
+  auto sums = [&]() {
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       float u[P][V];
 #pragma unroll
       for (int p = 0; p < P; ++p) Elem<T>::get(raw[j][p], u[p]);
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[j][i] = bias[i];
+      for (int i = 0; i < V; ++i) v[j][i] = 0.0f;
 #pragma unroll
       for (int k = 0; k < KC; ++k)  // past K both are zero
 #pragma unroll
         for (int i = 0; i < V; ++i) v[j][i] = fmaf(u[k / V][k % V], w[k][i], v[j][i]);
     }
-    if ((tile + gridDim.x) * TR < a.rows) load(tile + gridDim.x);
+  };
+  auto out = [&](auto fast, int64_t tile, const typename Tail<T>::Raw (&res)[U]) {
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int64_t row0 = tile * TR + j * R;
-      dense_tail<T, V>(a, row0, lr, row0 + lr < a.rows, col, v[j]);
+      tail.template out<decltype(fast)::value>(a, row0, lr, row0 + lr < a.rows, col, res[j], v[j]);
     }
+  };
+  auto residuals = [&](int64_t tile, typename Tail<T>::Raw (&res)[U]) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int64_t row0 = tile * TR + j * R;
+      res[j] = Tail<T>::residual(a, row0, lr, row0 + lr < a.rows, col);
+    }
+  };
+  // FAST: whole tiles by a loop without branches around loads and stores, and what
+  // is left of the rows after it
+  const int64_t tiles = FAST ? a.rows / TR : (a.rows + TR - 1) / TR;
+  const std::integral_constant<bool, FAST> fast;
+  const int64_t tile0 = blockIdx.x;
+  typename Tail<T>::Raw res[U];
+  if (tile0 < tiles) {
+    load(fast, tile0);
+    for (int64_t tile = tile0; tile < tiles; tile += gridDim.x) {
+      sums();
+      residuals(tile, res);
+      load(fast, tile + gridDim.x < tiles ? tile + gridDim.x : tile);
+      out(fast, tile, res);
+    }
+  }
+  if (FAST && tiles * TR < a.rows && blockIdx.x == tiles % gridDim.x) {
+    load(std::false_type{}, tiles);
+    residuals(tiles, res);
+    sums();
+    out(std::false_type{}, tiles, res);
   }
 }
 
@@ -134,7 +161,8 @@ e3_status dense_thin(const DenseArgs& a, hipStream_t st) {
   const int64_t tiles = (a.rows + R - 1) / R, cols = (a.cols + L * V - 1) / (L * V);
   const int64_t blocks = std::min<int64_t>(tiles, std::max<int64_t>(1, 1536 / cols));
   TimedLaunch t_("dense_thin", st);
-  hipLaunchKernelGGL((k_dense_thin<T, L, KC>), dim3((unsigned)blocks, (unsigned)cols), dim3(256), 0, st, a);
+  auto* k = a.nt && a.red == KC && a.cols % (L * V) == 0 ? k_dense_thin<T, L, KC, true> : k_dense_thin<T, L, KC, false>;
+  hipLaunchKernelGGL(k, dim3((unsigned)blocks, (unsigned)cols), dim3(256), 0, st, a);
   E3_HIP(hipGetLastError());
   return E3_OK;
 }
@@ -149,7 +177,8 @@ e3_status dense_few(const DenseArgs& a, hipStream_t st) {
 }
 
 size_t dense_fwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
-  return M <= kFew || K <= kThin ? 0 : cut_bytes(dense_cut(t, M, N, K), M, N);
+  const bool p = t == E3_F32 ? panel<float>(M, N, K) : panel<__bf16>(M, N, K);
+  return M <= kFew || K <= kThin || p ? 0 : cut_bytes(dense_cut(t, M, N, K), M, N);
 }
 template <class T>
 e3_status dense_fwd(const DenseArgs& a, float* part, hipStream_t st) {
@@ -167,7 +196,9 @@ e3_status dense_fwd(const DenseArgs& a, float* part, hipStream_t st) {
     };
     return a.red <= 8 ? with(std::integral_constant<int, 8>{}) : with(std::integral_constant<int, kThin>{});
   }
-  return dense_product<Job<T, kAlong, kAcross, kFull, kFull, false>>(a, part, "dense_fwd", st);
+  using J = Job<T, kAlong, kAcross, kFull, kFull, false>;
+  if (panel<T>(a.rows, a.cols, a.red)) return dense_panel<J>(a, "dense_fwd", st);
+  return dense_product<J>(a, part, "dense_fwd", st);
 }
 
 bool good_dims(e3_dtype t, int64_t M, int64_t K, int64_t N) {

@@ -74,16 +74,17 @@ e3_status dense_bwd_products(DenseArgs x, DenseArgs w, float* part, hipStream_t 
   using JW = Job<T, kAcross, kAcross, KX, KD, FLY>;
   const bool dx = x.y, dw = w.y, db = w.sums;
   const Cut cx = dense_cut(t, x.rows, x.cols, x.red), cw = dense_cut(t, w.rows, w.cols, w.red);
+  const bool along = panel<T>(x.rows, x.cols, x.red);
   set_cut(x, cx, part);
   set_cut(w, cw, part + cut_bytes(cx, x.rows, x.cols) / sizeof(float), w.cols);
   e3_status s = E3_OK;
-  if (dx && dw && cx.tile == 64 && cw.tile == 64) {
+  if (dx && dw && !along && cx.tile == 64 && cw.tile == 64) {
     TimedLaunch t_("dense_bwd_both", st);
     const int64_t first = cx.tiles * cx.splits;
     hipLaunchKernelGGL((k_dense_two<JX, JW, 64>), grid_of(first + cw.tiles * cw.splits), dim3(256), 0, st, x, w, first);
     E3_HIP(hipGetLastError());
   } else {
-    if (dx) s = dense_launch<JX>(x, cx, "dense_bwd_dx", st);
+    if (dx) s = along ? dense_panel<JX>(x, "dense_bwd_dx", st) : dense_launch<JX>(x, cx, "dense_bwd_dx", st);
     if (s == E3_OK && dw) s = dense_launch<JW>(w, cw, "dense_bwd_dw", st);
   }
   if constexpr (FLY && KX == kFull) {
@@ -100,7 +101,7 @@ e3_status dense_bwd_products(DenseArgs x, DenseArgs w, float* part, hipStream_t 
       E3_HIP(hipGetLastError());
     }
   }
-  if (s == E3_OK && dx && cx.splits > 1) s = dense_join<T>(x, st);
+  if (s == E3_OK && dx && !along && cx.splits > 1) s = dense_join<T>(x, st);
   // many partial sums of few columns take threads of their own (252 of 128 x 256: 6 us against 34)
   if (s == E3_OK && (dw || db) && cw.splits > 1 && cw.splits <= 16) s = dense_join<T>(w, st);
   if (s == E3_OK && (dw || db) && cw.splits > 16)

@@ -267,17 +267,14 @@ struct Tile {
   static constexpr int THREADS = WM * WN * kWave, TM = BM / WM, TN = BN / WN, RM = TM / 32, RN = TN / 32;
   using LA = Loader<T, FA, BM, BK, THREADS, KA>;
   using LB = Loader<T, FB, BN, BK, THREADS, KB>;
-  static constexpr int PITCH = TN + 4;                    // floats of a row of the results' staging
   union Shared {
     struct {
       typename LA::Lds a;
       typename LB::Lds b;
     } in[BUFS];
-    float out[WM * WN][32][PITCH];
+    float out[WM * WN][32][TN + 4];
     float sums[SUM ? THREADS / LB::Main::PER : 1][SUM ? BN : 1];
   };
-  static constexpr float kBack = sizeof(T) == 2 ? 1.0f : kTermBack;
-
   f16v acc[RM][RN];
   float sum[LB::V];  // SUM: of this thread's columns of B
 
@@ -384,40 +381,70 @@ struct Tile {
     }
   }
 
-  // Hands the results out as pieces of V values of a row, f(row, lr, col, v) with
-  // row + lr and col within the tile and row uniform; the lanes of a wave hold
-  // consecutive pieces.  Every wave goes through memory of its own.
+  // The wave's rows in blocks of 32 to out(row, col, results) with row and col of
+  // the block within the tile; every wave's staging is its own.
   template <class Fn>
-  __device__ __forceinline__ void finish(Shared& sh, Fn&& f) {
-    constexpr int V = Elem<T>::V, PER = TN / V, PASS = kWave / PER;
-    static_assert(kWave % PER == 0 && 32 % PASS == 0);
-    const int w = uniform(threadIdx.x / kWave), row0 = w / WN * TM, col0 = w % WN * TN, l = threadIdx.x % kWave;
+  __device__ __forceinline__ void finish(Shared& sh, Fn&& out) {
+    const int w = uniform(threadIdx.x / kWave), row0 = w / WN * TM, col0 = w % WN * TN;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      asm volatile("" ::: "memory");
+    for (int i = 0; i < RM; ++i) out(row0 + 32 * i, col0, sh.out[w], acc[i]);
+  }
+};
+
+// The results of 32 rows and 32 RN columns go through a wave's own staging, so
+// that a lane gets pieces of V values of a row (row l / PER of every PASS rows,
+// columns V (l % PER) on) and rows are written whole.
+template <class T, int RN>
+struct Rows32 {
+  static constexpr int V = Elem<T>::V, TN = 32 * RN, PER = TN / V, PASS = kWave / PER, N = 32 / PASS, PITCH = TN + 4;
+  static_assert(kWave % PER == 0 && 32 % PASS == 0);
+  static constexpr float kBack = sizeof(T) == 2 ? 1.0f : kTermBack;
+  static __device__ __forceinline__ int row() { return threadIdx.x % kWave / PER; }
+  static __device__ __forceinline__ int col() { return threadIdx.x % PER * V; }
+  static __device__ __forceinline__ void put(float (*out)[PITCH], const f16v (&acc)[RN]) {
+    const int l = threadIdx.x % kWave;
+    asm volatile("" ::: "memory");
 #pragma unroll
-      for (int j = 0; j < RN; ++j)
+    for (int j = 0; j < RN; ++j)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f4v*>(&sh.out[w][l % 32][32 * j + 8 * g + 4 * (l / 32)]) =
-              f4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-      // the wave's own writes: LDS serves a wave's accesses in order
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll 2
-      for (int r = 0; r < 32; r += PASS) {
-        const int col = l % PER * V;
-        float v[V];
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f4v*>(&out[l % 32][32 * j + 8 * g + 4 * (l / 32)]) =
+            f4v{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]} * kBack;
+    wait();
+  }
+  // The wave's own writes: LDS serves a wave's accesses in order.
+  static __device__ __forceinline__ void wait() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
+  // Piece i of the lane.
+  static __device__ __forceinline__ void get(const float (*out)[PITCH], int i, float (&v)[V]) {
 #pragma unroll
-        for (int e = 0; e < V; e += 4) {
-          const f4v t = *reinterpret_cast<const f4v*>(&sh.out[w][r + l / PER][col + e]);
-          v[e] = t.x * kBack, v[e + 1] = t.y * kBack, v[e + 2] = t.z * kBack, v[e + 3] = t.w * kBack;
-        }
-        f(row0 + 32 * i + r, l / PER, col0 + col, v);
-      }
-      __builtin_amdgcn_wave_barrier();
+    for (int e = 0; e < V; e += 4) {
+      const f4v t = *reinterpret_cast<const f4v*>(&out[i * PASS + row()][col() + e]);
+      v[e] = t.x, v[e + 1] = t.y, v[e + 2] = t.z, v[e + 3] = t.w;
     }
+  }
+  // Whether a sum of the wave is not finite.
+  static __device__ __forceinline__ bool bad(const f16v (&acc)[RN]) {
+    float z = 0.0f;
+#pragma unroll
+    for (int j = 0; j < RN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z = fmaf(acc[j][e], 0.0f, z);
+    return __ballot(z != 0.0f) != 0;
+  }
+  // Replaces the sums that are not finite by again(row, col).
+  template <class Fn>
+  static __device__ __forceinline__ void mend(float (*out)[PITCH], Fn&& again) {
+#pragma clang loop unroll(disable)
+    for (int i = 0; i < 32 * TN; i += kWave) {
+      const int at = i + threadIdx.x % kWave, r = at / TN, c = at % TN;
+      const float v = out[r][c];
+      if (v * 0.0f != 0.0f) out[r][c] = again(r, c);
+    }
+    wait();
   }
 };
 
