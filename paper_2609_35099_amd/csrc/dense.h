@@ -366,12 +366,17 @@ __global__ __launch_bounds__(256, 2) void k_dense_panel(DenseArgs a) {
   const int64_t blocks = FAST ? a.rows / 32 : (a.rows + 31) / 32;
   const std::integral_constant<bool, FAST> fast;
   if (chunk < blocks) {
+    // a round ends with loads and begins with stores, so that its wait for the
+    // loads of the one before leaves its own stores in flight; blocks past the
+    // end load the last one again
+    auto at = [&](int64_t b) { return b < blocks ? b : blocks - 1; };
     load(fast, chunk);
+    terms();
+    load(fast, at(chunk + a.splits));
     for (int64_t block = chunk; block < blocks; block += a.splits) {
-      terms();
-      // the last round loads a block again, so that every round has the same loads
-      load(fast, block + a.splits < blocks ? block + a.splits : block);
       product(fast, block);
+      terms();
+      load(fast, at(block + 2 * (int64_t)a.splits));
     }
   }
   if (FAST && a.rows % 32 && chunk == blocks % a.splits) {

@@ -83,12 +83,18 @@ __global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {
   const int64_t tile0 = blockIdx.x;
   typename Tail<T>::Raw res[U];
   if (tile0 < tiles) {
+    // a round ends with loads and begins with stores, so that its wait for the
+    // loads of the one before leaves its own stores in flight; tiles past the end
+    // load the last one again
+    auto at = [&](int64_t t) { return t < tiles ? t : tiles - 1; };
     load(fast, tile0);
+    sums();
+    load(fast, at(tile0 + gridDim.x));
     for (int64_t tile = tile0; tile < tiles; tile += gridDim.x) {
-      sums();
       residuals(tile, res);
-      load(fast, tile + gridDim.x < tiles ? tile + gridDim.x : tile);
       out(fast, tile, res);
+      sums();
+      load(fast, at(tile + 2 * (int64_t)gridDim.x));
     }
   }
   if (FAST && tiles * TR < a.rows && blockIdx.x == tiles % gridDim.x) {

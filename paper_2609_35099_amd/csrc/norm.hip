@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kNormFwdThreads<L>) void k_norm_fwd(NormArgs a) {
 // too few registers), one row where it takes more.
 template <int L>
 constexpr int kNormBwdThreads = L <= kWave ? 512 : L;
-template <class T, int L, int J, bool Q>
+template <class T, int L, int J, bool Q, bool FAST>
 __global__ __launch_bounds__(kNormBwdThreads<L>) void k_norm_bwd(NormArgs a) {
   constexpr int V = Elem<T>::V, NT = kNormBwdThreads<L>, R = NT / L;
   using In = RowsIn<T>;
@@ -147,30 +147,39 @@ __global__ __launch_bounds__(kNormBwdThreads<L>) void k_norm_bwd(NormArgs a) {
   if (gamma)
 #pragma unroll
     for (int j = 0; j < J; ++j) gr[j] = ld_raw<T>(gamma + (j * L + lane) * V, cols - (j * L + lane) * V);
-  float mean = 0.0f, rstd = 0.0f;
+  float mean = 0.0f, rstd = 0.0f, x[J][V], dy[J][V];
+  // FAST: every piece is whole and dx streams.  A round then has no branch around
+  // its stores, and as it ends with loads, its wait for those of the round before
+  // leaves its own stores in flight.
   auto load = [&](int64_t r) {
+    if (r >= a.rows) r = a.rows - 1;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int col = (j * L + lane) * V;
-      xr[j] = xs.template raw<Q>(r, col, cols);
-      dr[j] = ld_raw<T>(dyp + r * a.ldy + col, cols - col);
+      xr[j] = xs.template raw<Q>(r, col, FAST ? L * J * V : cols);
+      dr[j] = ld_raw<T>(dyp + r * a.ldy + col, FAST ? V : cols - col);
     }
     mean = a.mean[r], rstd = a.rstd[r];
   };
-  if (row < a.rows) load(row);
-  for (; row < a.rows; row += stride) {
-    float x[J][V], dy[J][V];
+  auto take = [&](float& m, float& rs) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       In::template get<Q>(xr[j], x[j]);
       Elem<T>::get(dr[j], dy[j]);
     }
-    const float m = mean, rs = rstd;
-    if (row + stride < a.rows) load(row + stride);
+    m = mean, rs = rstd;
+  };
+  float m = 0.0f, rs = 0.0f;
+  if (row < a.rows) {
+    load(row);
+    take(m, rs);
+    load(row + stride);
+  }
+  for (; row < a.rows; row += stride) {
     float c0 = 0.0f, c1 = 0.0f;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int col = (j * L + lane) * V, n = cols - col;
+      const int col = (j * L + lane) * V, n = FAST ? V : cols - col;
       float g[V];
       if (gamma) Elem<T>::get(gr[j], g);
 #pragma unroll
@@ -184,7 +193,7 @@ __global__ __launch_bounds__(kNormBwdThreads<L>) void k_norm_bwd(NormArgs a) {
         c1 += dy[j][i] * x[j][i];
       }
     }
-    if (a.dx) {
+    if (FAST || a.dx) {
       c0 = row_sum<L>(c0, s) / (float)cols;
       c1 = row_sum<L>(c1, s) / (float)cols;
 #pragma unroll
@@ -192,9 +201,11 @@ __global__ __launch_bounds__(kNormBwdThreads<L>) void k_norm_bwd(NormArgs a) {
         const int col = (j * L + lane) * V;
 #pragma unroll
         for (int i = 0; i < V; ++i) dy[j][i] = rs * (dy[j][i] - c0 - x[j][i] * c1);
-        st_piece<T>(static_cast<T*>(a.dx) + row * a.lddx + col, cols - col, dy[j], a.nt);
+        st_piece<T>(static_cast<T*>(a.dx) + row * a.lddx + col, FAST ? V : cols - col, dy[j], FAST || a.nt);
       }
     }
+    take(m, rs);
+    load(row + 2 * stride);
   }
   if (!a.part) return;
   float* out = a.part + (int64_t)blockIdx.x * 2 * cols;
@@ -370,7 +381,9 @@ e3_status norm_bwd(const NormArgs& a, hipStream_t st) {
     constexpr int l = decltype(L)::value, j = decltype(J)::value;
     if constexpr (j > 0) {
       TimedLaunch t_("layer_norm_bwd", st);
-      auto* k = a.x ? k_norm_bwd<T, l, j, false> : k_norm_bwd<T, l, j, true>;
+      const bool fast = a.dx && a.nt && a.cols == l * j * Elem<T>::V;
+      auto* k = a.x ? (fast ? k_norm_bwd<T, l, j, false, true> : k_norm_bwd<T, l, j, false, false>)
+                    : (fast ? k_norm_bwd<T, l, j, true, true> : k_norm_bwd<T, l, j, true, false>);
       hipLaunchKernelGGL(k, dim3(a.blocks), dim3(kNormBwdThreads<l>), 0, st, a);
       E3_HIP(hipGetLastError());
     } else {
