@@ -57,6 +57,13 @@ struct Tail {
   using Raw = typename Elem<T>::vec;
   static __device__ __forceinline__ Raw residual(const DenseArgs& a, int64_t row0, int lr, bool ok, int col) {
     if (!a.res) return Raw{};
+    const int64_t total = (a.rows - 1) * a.ldr + a.cols;
+    if (total >= V) {
+      const int n = a.cols - col;
+      const int64_t row = ok ? row0 + lr : 0;  // any row inside
+      return __builtin_bit_cast(Raw, ld_span<u4v>(static_cast<const T*>(a.res), row * a.ldr + col, total,
+                                                  !ok || n < 0 ? 0 : n < V ? n : V));
+    }
     return ld_raw<T>(static_cast<const T*>(a.res) + (row0 * a.ldr + (lr * a.ldr + col)), ok ? a.cols - col : 0);
   }
   // FAST: the piece is inside the row and streams, with no branch around the store

@@ -254,7 +254,8 @@ e3_status e3_dense_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* W
   if (ws_bytes < need) return E3_ERR_WORKSPACE_TOO_SMALL;
   if (need && (!ws || misaligned(E3_F32, ws))) return E3_ERR_INVALID_ARG;
   DenseArgs a{};
-  a.a = {x, ldx}, a.b = {W, N}, a.rows = M, a.cols = (int)N, a.red = K;
+  a.a = {x, ldx, nullptr, nullptr, 0, (M - 1) * ldx + K}, a.b = {W, N, nullptr, nullptr, 0, K * N};
+  a.rows = M, a.cols = (int)N, a.red = K;
   a.bias = bias, a.res = res, a.ldr = ldr, a.act = act, a.y = y, a.ldy = ldy, a.z = z, a.ldz = ldz, a.zq = zq;
   a.zc = zc, a.yq = yq, a.yc = yc, a.nt = streams(dtype, M, N);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);

@@ -65,6 +65,41 @@ __global__ __launch_bounds__(256) void k_dense_dz(RowsIn<T> z, int act, const T*
   }
 }
 
+// Layers of which a matrix is shorter than a piece: a wave per value of dx, dW and
+// db, whose lanes take every 64th term.  (One row or column, or nearly; a long
+// reduction is slow here.)
+template <class T>
+__global__ __launch_bounds__(256) void k_dense_bwd_tiny(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy,
+                                                        int64_t lddy, T* dx, int64_t lddx, T* dW, T* db, int64_t M,
+                                                        int K, int N) {
+  const int l = threadIdx.x % kWave;
+  int64_t u = block_id() * 4 + threadIdx.x / kWave;
+  auto dz = [&](int64_t m, int n) {
+    const float v = Elem<T>::one(dy[m * lddy + n]);
+    return act == E3_ACT_NONE ? v : v * act_grad(act, z.value(m, n, N));
+  };
+  float v = 0.0f;
+  T* out;
+  if (u < M * K) {
+    if (!dx) return;
+    const int64_t m = u / K, k = u % K;
+    for (int n = l; n < N; n += kWave) v = fmaf(Elem<T>::round(dz(m, n)), Elem<T>::one(W[k * N + n]), v);
+    out = dx + m * lddx + k;
+  } else if ((u -= M * K) < (int64_t)K * N) {
+    if (!dW) return;
+    const int k = (int)(u / N), n = (int)(u % N);
+    for (int64_t m = l; m < M; m += kWave) v = fmaf(x.value(m, k, K), Elem<T>::round(dz(m, n)), v);
+    out = dW + u;
+  } else {
+    u -= (int64_t)K * N;
+    if (!db || u >= N) return;
+    for (int64_t m = l; m < M; m += kWave) v += dz(m, (int)u);
+    out = db + u;
+  }
+  v = sum_lanes<kWave>(v);
+  if (l == 0) *out = (T)v;
+}
+
 // ------------------------------------------------------------ host
 // dx and dW (FLY: and db) of a layer whose operand dz is of kind KD and x of KX.
 template <class T, Kind KD, Kind KX, bool FLY>
@@ -113,6 +148,15 @@ template <class T>
 e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, int64_t lddy, T* dx, int64_t lddx, T* dW,
                     T* db, char* ws, int64_t M, int64_t K, int64_t N, hipStream_t st) {
   constexpr e3_dtype t = std::is_same_v<T, float> ? E3_F32 : E3_BF16;
+  constexpr int V = Elem<T>::V;
+  if (M * N < V || M * K < V || K * N < V) {  // a matrix may be shorter than a piece
+    TimedLaunch t_("dense_bwd_tiny", st);
+    const int64_t outs = M * K + K * N + N;
+    hipLaunchKernelGGL(k_dense_bwd_tiny<T>, grid_of((outs + 3) / 4), dim3(256), 0, st, x, W, z, act, dy, lddy, dx, lddx,
+                       dW, db, M, (int)K, (int)N);
+    E3_HIP(hipGetLastError());
+    return E3_OK;
+  }
   const DenseBwdWs w = dense_bwd_ws(t, M, K, N);
   const bool fly = K <= kOnTheFly;
   T* dz = reinterpret_cast<T*>(ws);
@@ -131,10 +175,12 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
     if (s != E3_OK) return s;
   }
   DenseArgs ax{}, aw{};
-  const Side d{own ? dz : dy, own ? N : lddy}, pre{z.x, z.x ? z.ld : N, z.q, z.c, (N + kGroup - 1) / kGroup};
-  ax.a = d, ax.b = {W, N}, ax.pre = pre, ax.grad_act = act, ax.rows = M, ax.cols = (int)K, ax.red = N;
+  const int64_t ldd = own ? N : lddy, ldz = z.x ? z.ld : N, ldx = x.x ? x.ld : K;
+  const Side d{own ? dz : dy, ldd, nullptr, nullptr, 0, (M - 1) * ldd + N};
+  const Side pre{z.x, ldz, z.q, z.c, (N + kGroup - 1) / kGroup, (M - 1) * ldz + N};
+  ax.a = d, ax.b = {W, N, nullptr, nullptr, 0, K * N}, ax.pre = pre, ax.grad_act = act, ax.rows = M, ax.cols = (int)K, ax.red = N;
   ax.y = dx, ax.ldy = lddx, ax.nt = streams(t, M, K);
-  aw.a = {x.x, x.x ? x.ld : K, x.q, x.c, (K + kGroup - 1) / kGroup}, aw.b = d, aw.pre = pre, aw.grad_act = act;
+  aw.a = {x.x, ldx, x.q, x.c, (K + kGroup - 1) / kGroup, (M - 1) * ldx + K}, aw.b = d, aw.pre = pre, aw.grad_act = act;
   aw.rows = K, aw.cols = (int)N, aw.red = M, aw.y = dW, aw.ldy = N, aw.sums = fly ? db : nullptr;
   auto run = [&](auto KD, auto FLY) {
     constexpr Kind kd = decltype(KD)::value;

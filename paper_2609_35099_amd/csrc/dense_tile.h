@@ -52,6 +52,7 @@ struct Side {
   const int8_t* q;    // packed (p null): ld values and ldc exponents a row
   const uint8_t* c;
   int64_t ldc;
+  int64_t total;      // values from the first to the last, at least a piece
 };
 
 // LDS planes of R rows (or columns) by BK reduction indexes.  16-byte slots are
@@ -87,22 +88,6 @@ struct Plane {
   }
 };
 
-// The 16 (8) bytes r moved down by `bits`, zeros from above.
-__device__ __forceinline__ u4v shift_down(u4v r, unsigned bits) {
-  uint64_t lo = (uint64_t)r.y << 32 | r.x, hi = (uint64_t)r.w << 32 | r.z;
-  if (bits & 64) lo = hi, hi = 0;
-  const unsigned b = bits & 63;
-  lo = b ? lo >> b | hi << (64 - b) : lo;
-  hi >>= b;
-  if (bits >= 128) lo = hi = 0;
-  return u4v{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
-}
-__device__ __forceinline__ u2v shift_down(u2v r, unsigned bits) {
-  const uint64_t v = bits < 64 ? ((uint64_t)r.y << 32 | r.x) >> bits : 0;
-  return u2v{(unsigned)v, (unsigned)(v >> 32)};
-}
-__device__ __forceinline__ unsigned shift_down(unsigned r, unsigned bits) { return bits < 32 ? r >> bits : 0u; }
-
 // A thread's N pieces of V values of a tile of memory rows of W values, as they
 // lie in memory; R and BK are the tile's output and reduction indexes.
 template <class T, Form F, int R, int BK, int THREADS, bool Q>
@@ -126,8 +111,7 @@ struct Fetch {
   // are not stored.  WHOLE: no piece crosses a row's end and all reduction
   // indexes are inside (a tile's own loop: with both ways in one loop, the loaded
   // registers were copied where the ways meet, which waits for the loads).
-  // Otherwise a piece that crosses a row's end is loaded from where it still
-  // fits and moved down; only rows shorter than a piece go by values.
+  // Otherwise pieces may reach into the next row (ld_span) and are cut.
   template <bool WHOLE>
   __device__ __forceinline__ void load(const Side& s, int64_t r0, int64_t rows, int64_t k0, int64_t end) {
     // memory row m0 + row_of(i), column c0 + col_of(): the uniform part in the base
@@ -146,36 +130,18 @@ struct Fetch {
       }
       return;
     }
-    const bool fits = cend >= V;
-    const int left = cend - c0 < 1024 ? (int)(cend - c0) : 1024;  // columns from c0 on
-    const int over = lc > left - V ? lc - (left - V) : 0;          // how far the piece reaches out
-    const unsigned bits = over >= V ? 8 * sizeof(Raw) : (unsigned)over * BITS;
+    const E* first = Q ? reinterpret_cast<const E*>(s.q) : static_cast<const E*>(s.p);
+    const int left = cend - c0 < 1024 ? (int)(cend - c0) : 1024;  // columns from c0 on, at least one
+    const int n = left - lc < V ? (left - lc > 0 ? left - lc : 0) : V;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const bool in = F == kAlong || row_of(i) <= mlast;
       const int64_t m = imin(row_of(i), mlast);
-      const E* q = p + m * s.ld;
-      if (fits) {
-        raw[i] = shift_down(*reinterpret_cast<const Any*>(q + (over ? left - V : lc)), in ? bits : 8 * sizeof(Raw));
-      } else {
-        unsigned w[sizeof(Raw) / 4] = {};
-        const int n = in && over < V ? left - lc : 0;
-        for (int e = 0; e < V; ++e)
-          if (e < n) {
-            unsigned u;
-            if constexpr (Q) u = (uint8_t)q[lc + e];
-            else if constexpr (sizeof(E) == 2) u = __builtin_bit_cast(unsigned short, q[lc + e]);
-            else u = __builtin_bit_cast(unsigned, q[lc + e]);
-            w[e * BITS / 32] |= u << (e * BITS % 32);
-          }
-        if constexpr (sizeof(Raw) == 16) raw[i] = u4v{w[0], w[1], w[2], w[3]};
-        else if constexpr (sizeof(Raw) == 8) raw[i] = u2v{w[0], w[1]};
-        else raw[i] = w[0];
-      }
-      // a step's exponent only where something was read: a NaN step times a zero is NaN
+      raw[i] = ld_span<Raw>(first, (m0 + m) * s.ld + c0 + lc, s.total, in ? n : 0);
       if constexpr (Q) {
-        exps[i] = 0;
-        if (in && over < V) exps[i] = pc[m * s.ldc + lc / kGroup];
+        // a step's exponent only where something was read: a NaN step times a zero is NaN
+        const unsigned char e = pc[m * s.ldc + imin(lc, left - 1) / kGroup];
+        exps[i] = in && n > 0 ? e : 0;
       }
     }
   }

@@ -68,10 +68,45 @@ __device__ __forceinline__ void ld_piece(const T* p, int n, float (&v)[Elem<T>::
 template <class T>
 __device__ __forceinline__ typename Elem<T>::vec ld_raw(const T* p, int n) {
   if (n >= Elem<T>::V) return *reinterpret_cast<const typename Elem<T>::vec*>(p);
+  if (n <= 0) return typename Elem<T>::vec{};
   float v[Elem<T>::V];
 #pragma unroll
   for (int i = 0; i < Elem<T>::V; ++i) v[i] = i < n ? Elem<T>::one(p[i]) : 0.0f;
   return Elem<T>::put(v);
+}
+// The 16, 8 or 4 bytes r moved down by `bits`, zeros from above; its lowest bits.
+__device__ __forceinline__ u4v shift_down(u4v r, unsigned bits) {
+  uint64_t lo = (uint64_t)r.y << 32 | r.x, hi = (uint64_t)r.w << 32 | r.z;
+  if (bits & 64) lo = hi, hi = 0;
+  const unsigned b = bits & 63;
+  lo = b ? lo >> b | hi << (64 - b) : lo;
+  hi >>= b;
+  if (bits >= 128) lo = hi = 0;
+  return u4v{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+__device__ __forceinline__ u2v shift_down(u2v r, unsigned bits) {
+  const uint64_t v = bits < 64 ? ((uint64_t)r.y << 32 | r.x) >> bits : 0;
+  return u2v{(unsigned)v, (unsigned)(v >> 32)};
+}
+__device__ __forceinline__ unsigned shift_down(unsigned r, unsigned bits) { return bits < 32 ? r >> bits : 0u; }
+__device__ __forceinline__ unsigned low_bits(unsigned r, int bits) {
+  return bits >= 32 ? r : bits <= 0 ? 0u : r & ~(~0u << bits);
+}
+__device__ __forceinline__ u2v low_bits(u2v r, int bits) { return u2v{low_bits(r.x, bits), low_bits(r.y, bits - 32)}; }
+__device__ __forceinline__ u4v low_bits(u4v r, int bits) {
+  return u4v{low_bits(r.x, bits), low_bits(r.y, bits - 32), low_bits(r.z, bits - 64), low_bits(r.w, bits - 96)};
+}
+// Values at .. at + n - 1 of a matrix that spans `total` values from p (the rest
+// of the piece zero) without a branch, so that several loads are in flight: a
+// piece that would reach past the span is loaded from its last values and moved
+// down.  total is at least a piece.
+template <class R, class E>
+__device__ __forceinline__ R ld_span(const E* p, int64_t at, int64_t total, int n) {
+  typedef R Any __attribute__((aligned(sizeof(E))));
+  constexpr int V = sizeof(R) / sizeof(E), BITS = 8 * sizeof(E);
+  const int64_t start = at < total - V ? at : total - V, over = at - start;
+  const R r = shift_down(*reinterpret_cast<const Any*>(p + start), (over < V ? (unsigned)over : (unsigned)V) * BITS);
+  return low_bits(r, n * BITS);
 }
 // nt: past the caches, for outputs that do not fit them (rule and figures at
 // streams()).
@@ -259,6 +294,10 @@ struct RowsIn {
   __device__ __forceinline__ void load(int64_t row, int col, int cols, float (&v)[Elem<T>::V]) const {
     if (x) get<false>(raw<false>(row, col, cols), v);
     else get<true>(raw<true>(row, col, cols), v);
+  }
+  __device__ __forceinline__ float value(int64_t row, int col, int cols) const {
+    if (x) return Elem<T>::one(x[row * ld + col]);
+    return (float)q[row * cols + col] * step8(c[row * ((cols + kGroup - 1) / kGroup) + col / kGroup]);
   }
 };
 
