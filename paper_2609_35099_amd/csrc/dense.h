@@ -177,8 +177,10 @@ __device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_
 // Tiles by type and size; what a library product reaches is 1,070 TFLOP/s in
 // bfloat16 and 143 in float32 (16,384 x 1,024 x 4,096).
 //   bfloat16, 256 x 256: 16 waves of 64 x 64, steps of 32, two buffers, one
-//     workgroup per CU: 940 (forward), 1,083 (dx), 1,056 TFLOP/s (dW); 8 waves of
-//     128 x 64 760, 940, 1,019.
+//     workgroup per CU: 1,083 (dx), 1,056 TFLOP/s (dW); 8 waves of 128 x 64 940,
+//     1,019.  The forward takes 256 x 128 by 8 waves, two workgroups per CU, so that
+//     one's activations run beside the other's product (902 for the bare product,
+//     942 with 256 x 256; with gelu and z in 8 bits @F128@ us against 261).
 //   bfloat16, 128 and 64: 4 waves, steps of 64, two buffers, two workgroups and
 //     more: 685, 906, 867.
 //   float32, 128 x 128: one buffer of the three planes; rows along the reduction
@@ -186,10 +188,11 @@ __device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_
 //     across with 4 (208; 8 193).
 template <class J, int B>
 struct TileOf {
-  static constexpr bool f32 = sizeof(typename J::T) == 4;
-  static constexpr int WM = B == 256 || (f32 && B == 128 && J::FA == kAlong) ? 4 : 2, WN = B == 256 ? 4 : 2;
+  static constexpr bool f32 = sizeof(typename J::T) == 4, fwd = J::FA == kAlong && J::FB == kAcross;
+  static constexpr int BN = B == 256 && fwd ? 128 : B;
+  static constexpr int WM = B == 256 || (f32 && B == 128 && J::FA == kAlong) ? 4 : 2, WN = B == 256 ? BN / 64 : 2;
   static constexpr int BK = f32 || B == 256 ? 32 : 64, THREADS = WM * WN * kWave, OCC = B == 256 ? 4 : 2;
-  using type = Tile<typename J::T, J::FA, J::FB, B, B, BK, WM, WN, J::KA, J::KB, J::SUM, f32 ? 1 : 2>;
+  using type = Tile<typename J::T, J::FA, J::FB, B, BN, BK, WM, WN, J::KA, J::KB, J::SUM, f32 ? 1 : 2>;
 };
 
 // Which tile block u of tm x tn takes: blocks go round robin to the XCDs, so an
@@ -242,7 +245,7 @@ template <class J, int B>
 __global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void k_dense(DenseArgs a) {
   using Tl = typename TileOf<J, B>::type;
   __shared__ __align__(16) typename Tl::Shared sh;
-  dense_block<J, Tl, B, B>(a, sh, block_id());
+  dense_block<J, Tl, B, TileOf<J, B>::BN>(a, sh, block_id());
 }
 // Short reductions (up to 16 KK) over many rows: no LDS and no barriers before the
 // epilogue.  A wave keeps the terms of its 32 NC columns of B in registers for
@@ -456,27 +459,34 @@ __global__ __launch_bounds__(256) void k_dense_join(DenseArgs a, int splits) {
 // How a product is cut: square tiles, and splits of its reduction where the
 // tiles alone would leave much of the card idle.
 struct Cut {
-  int tile, splits;
+  int tile, splits;  // of tile x tile; 256: 256 x 128 where the forward's epilogue follows
   int64_t tiles, chunk;
 };
 constexpr int kFill = 512;  // workgroups of the smaller tiles that fill the card
-Cut dense_cut(e3_dtype t, int64_t rows, int64_t cols, int64_t red) {
+Cut dense_cut(e3_dtype t, int64_t rows, int64_t cols, int64_t red, bool fwd = false) {
   Cut c{};
-  auto tiles = [&](int b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); };
-  c.tile = rows <= 64 || cols <= 64 || tiles(128) < kFill / 2 ? 64 : 128;
+  auto tiles = [&](int b, int bn = 0) {
+    bn = bn ? bn : b;
+    return ((rows + b - 1) / b) * ((cols + bn - 1) / bn);
+  };
+  const int64_t t128 = tiles(128), t256 = tiles(256);
   int64_t fill = kFill;
+  // Small tiles where there are few: more of them are on a CU and wait for memory
+  // together (bfloat16 4,096 x 512 x 1,024 14 us against 27, 2,048^3 36 against 39;
+  // float32 4,096 x 512 x 1,024 38 against 41, but 2,048^3 125 against 107: long
+  // reductions are split instead, as is dW of 100,003 x 128 x 256, 65 against 84).
+  const bool few = t == E3_BF16 ? t128 < kFill && red < 8192 : t128 < kFill / 2 && red < 1024;
+  c.tile = rows <= 64 || cols <= 64 || few ? 64 : 128;
   if (t == E3_BF16 && rows > 128 && cols > 128) {
     // rounds of the card by the time of one: four times the work of a 128 x 128
-    // tile, of which two run on a CU at 0.78 of the rate
-    auto time = [&](int64_t n, int64_t slots, double round) {
-      const int64_t s = std::max<int64_t>(1, std::min(slots / n, red / 512));
-      return (double)((n * s + slots - 1) / slots) * round / (double)s;
-    };
-    if (time(tiles(256), 256, 4.0) <= time(tiles(128), 512, 2.56)) c.tile = 256, fill = 256;
+    // tile, of which two run on a CU at 0.78 of the rate; splits of 2,048 at least
+    const int64_t s = std::max<int64_t>(1, std::min(256 / t256, red / 2048));
+    const double big = (double)((t256 * s + 255) / 256) * 4.0 / (double)s;
+    if (t256 * s >= 192 && big <= (double)((t128 + kFill - 1) / kFill) * 2.56) c.tile = 256, fill = fwd ? 512 : 256;
   }
-  c.tiles = tiles(c.tile);
+  c.tiles = c.tile == 256 && fwd ? tiles(256, 128) : tiles(c.tile);
   // at least 256 indexes a split; few tiles of few indexes take down to 64
-  const int64_t least = c.tiles * (red / 256) < kFill / 8 ? 64 : c.tile == 256 ? 512 : 256;
+  const int64_t least = c.tiles * (red / 256) < kFill / 8 ? 64 : c.tile == 256 ? 2048 : 256;
   const int64_t s = std::max<int64_t>(
       1, std::min<int64_t>({fill / std::max<int64_t>(c.tiles, 1), (red + least - 1) / least, 256}));
   c.chunk = std::max<int64_t>(64, ((red + s - 1) / s + 63) / 64 * 64);
@@ -548,7 +558,7 @@ constexpr e3_dtype dtype_of(const float*) { return E3_F32; }
 constexpr e3_dtype dtype_of(const __bf16*) { return E3_BF16; }
 template <class J>
 e3_status dense_product(DenseArgs a, float* part, const char* name, hipStream_t st) {
-  const Cut c = dense_cut(dtype_of(static_cast<const typename J::T*>(nullptr)), a.rows, a.cols, a.red);
+  const Cut c = dense_cut(dtype_of(static_cast<const typename J::T*>(nullptr)), a.rows, a.cols, a.red, true);
   set_cut(a, c, part);
   const e3_status s = dense_launch<J>(a, c, name, st);
   return s != E3_OK || c.splits == 1 ? s : dense_join<typename J::T>(a, st);

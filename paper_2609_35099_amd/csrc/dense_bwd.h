@@ -9,7 +9,7 @@ template <class J, int B>
 __global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void k_dense_sums(DenseArgs a) {
   using Tl = typename TileOf<J, B>::type;
   __shared__ __align__(16) typename Tl::Shared sh;
-  dense_block<J, Tl, B, B, true>(a, sh, block_id());
+  dense_block<J, Tl, B, TileOf<J, B>::BN, true>(a, sh, block_id());
 }
 // Two products in one launch: the first `first` blocks take the first.
 template <class J, class K, int B>

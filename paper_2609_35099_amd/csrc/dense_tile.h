@@ -66,7 +66,7 @@ struct Plane {
   static constexpr int kShare = F == kAlong ? (S >= 16 ? 1 : 16 / S) : 1;  // rows over all banks
   unsigned short v[P][R * BK];
   static __device__ __forceinline__ int off(int row, int slot) {
-    const int x = F == kAlong ? (row / kShare) & (S - 1 < 7 ? S - 1 : 7) : (2 * (row & 3)) & (S - 1);
+    const int x = F == kAlong ? (row / kShare) & (S - 1 < 15 ? S - 1 : 15) : (2 * (row & 3)) & (S - 1);
     return row * W + ((slot ^ x) * 8);
   }
   // The fragment of rows (columns) r0 + l % 32 at reduction indexes k0 + 8 (l / 32) on.
