@@ -66,10 +66,11 @@ struct Tail {
     }
     return ld_raw<T>(static_cast<const T*>(a.res) + (row0 * a.ldr + (lr * a.ldr + col)), ok ? a.cols - col : 0);
   }
-  // FAST: the piece is inside the row and streams, with no branch around the store
-  // of y: in a loop over rows, the loads that the next round waits for are older
-  // than the stores, and only a known number of stores lets the wait leave them
-  // in flight.
+  // FAST: the piece is inside the row, y streams, and there is neither a residual
+  // nor an output beside it (plain()), so that a round of a loop over rows has no
+  // branch around a load or store: the loads that the next round waits for are
+  // older than the stores, and only a known number of stores lets the wait leave
+  // them in flight.
   template <bool FAST = false>
   __device__ __forceinline__ void out(const DenseArgs& a, int64_t row0, int lr, bool ok, int col, Raw res,
                                       float (&v)[V]) const {
@@ -79,13 +80,13 @@ struct Tail {
       const int64_t groups = (a.cols + kGroup - 1) / kGroup;
       pack8_piece<V>(v, col, n, q + (row0 * a.cols + (int64_t)lr * a.cols), c + (row0 * groups + lr * groups));
     };
-    if (a.bias)
+    if (FAST || a.bias)
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] += bias[i];
-    if (a.z) st_piece<T>(static_cast<T*>(a.z) + at(a.ldz), n, v, a.nt);
-    if (a.zq) pack(a.zq, a.zc);
+    if (!FAST && a.z) st_piece<T>(static_cast<T*>(a.z) + at(a.ldz), n, v, a.nt);
+    if (!FAST && a.zq) pack(a.zq, a.zc);
     act_piece(a.act, v);
-    if (a.res) {
+    if (!FAST && a.res) {
       float u[V];
       Elem<T>::get(res, u);
 #pragma unroll
@@ -93,9 +94,11 @@ struct Tail {
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = Elem<T>::round(v[i]);
-    st_piece<T>(static_cast<T*>(a.y) + at(a.ldy), n, v, FAST || a.nt);
-    if (a.yq) pack(a.yq, a.yc);
+    if constexpr (FAST) __builtin_nontemporal_store(Elem<T>::put(v), reinterpret_cast<Raw*>(static_cast<T*>(a.y) + at(a.ldy)));
+    else st_piece<T>(static_cast<T*>(a.y) + at(a.ldy), n, v, a.nt);
+    if (!FAST && a.yq) pack(a.yq, a.yc);
   }
+  static bool plain(const DenseArgs& a) { return a.nt && !a.res && !a.z && !a.zq && !a.yq; }
 };
 template <class T, int V>
 __device__ __forceinline__ void dense_tail(const DenseArgs& a, int64_t row0, int lr, bool ok, int col, float (&v)[V]) {
@@ -146,7 +149,7 @@ __device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_
   typename Tail<T>::Raw res[R::N];
 #pragma unroll
   for (int i = 0; i < R::N; ++i)
-    res[i] = Tail<T>::residual(a, row0 + i * R::PASS, lr, row0 + i * R::PASS + lr < a.rows, col);
+    if (!FAST) res[i] = Tail<T>::residual(a, row0 + i * R::PASS, lr, row0 + i * R::PASS + lr < a.rows, col);
   R::put(out, acc);
   if constexpr (sizeof(T) == 4) {
     if (R::bad(acc))
@@ -395,6 +398,98 @@ __global__ __launch_bounds__(256, 2) void k_dense_panel(DenseArgs a) {
     product(std::false_type{}, blocks);
   }
 }
+// The same where rows have columns for several waves: WPB waves of a workgroup
+// bring each row block to LDS together, so that its terms are formed once and not
+// by every wave (a third of the vector work in float32, which is what bounds the
+// kernel above: 156,000 x 64 x 1,664 @PANEL@ us there, @SHARED@ here).  Columns are
+// whole multiples of 64 WPB, the reduction is at most BK, y streams.
+template <class J, int BK, int WPB>
+__global__ __launch_bounds__(WPB* kWave, 2) void k_dense_shared(DenseArgs a) {
+  using T = typename J::T;
+  using LA = Loader<T, kAlong, 32, BK, WPB * kWave, J::KA>;
+  constexpr int NC = 2, KK = BK / 16, P = LA::P;
+  static_assert(J::FA == kAlong && J::KA != kPacked && J::KB == kFull && !J::SUM);
+  __shared__ __align__(16) typename LA::Lds in[2];
+  __shared__ __align__(16) float out[WPB][32][Rows32<T, NC>::PITCH];
+  const int l = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), K = (int)a.red;
+  const int groups = a.cols / (64 * WPB);
+  const int64_t chunk = block_id() / groups;
+  if (chunk >= a.splits) return;
+  const int col0 = ((int)(block_id() % groups) * WPB + wave) * 64;
+  bf8v wf[P][KK][NC];
+#pragma unroll
+  for (int k = 0; k < KK; ++k)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int col = col0 + 32 * c + l % 32;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int at = 16 * k + 8 * (l / 32) + e;
+        const T* b = static_cast<const T*>(a.b.p);
+        v[e] = at < K ? Elem<T>::one(J::FB == kAlong ? b[col * a.b.ld + at] : b[at * a.b.ld + col]) : 0.0f;
+        if (P > 1) v[e] *= kTermScale;
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        u4v t;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = term2(v[2 * e], v[2 * e + 1]);
+        wf[p][k][c] = __builtin_bit_cast(bf8v, t);
+      }
+    }
+  const int64_t blocks = (a.rows + 31) / 32, whole = a.rows / 32;
+  LA la;
+  float none[LA::V];
+  auto load = [&](int64_t block) {
+    if (block >= blocks) block = blocks - 1;
+    // (the pieces of a short reduction are cut)
+    if (K == BK) la.template load<true>(a.a, a.pre, block * 32, a.rows, 0, BK);
+    else la.template load<false>(a.a, a.pre, block * 32, a.rows, 0, K);
+  };
+  int cur = 0;
+  f16v acc[NC];
+  auto product = [&]() {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[c][e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      bf8v xf[P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) xf[p] = in[cur].frag(p, 0, 16 * k);
+#pragma unroll
+      for (int s = 2 * P - 2 < 2 ? 2 * P - 2 : 2; s >= 0; --s)
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const int q = s - p;
+          if (q < 0 || q >= P) continue;
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[q][k][c], xf[p], acc[c], 0, 0, 0);
+        }
+    }
+  };
+  if (chunk >= blocks) return;  // the whole workgroup
+  load(chunk);
+  la.template store<false>(in[0], a.grad_act, none);
+  load(chunk + a.splits);
+  __syncthreads();
+  int64_t block = chunk;
+  for (; block < whole; block += a.splits) {
+    product();
+    la.template store<false>(in[cur ^ 1], a.grad_act, none);
+    load(block + 2 * (int64_t)a.splits);
+    rows32_out<J, NC, true>(a, 0, block * 32, col0, 0, a.red, out[wave], acc);
+    __syncthreads();
+    cur ^= 1;
+  }
+  if (block < blocks) {  // the last rows, fewer than 32
+    product();
+    rows32_out<J, NC>(a, 0, block * 32, col0, 0, a.red, out[wave], acc);
+  }
+}
 // Whether a product goes that way: a reduction that fits the registers beside its
 // columns, and rows enough for the waves to walk.
 template <class T>
@@ -406,21 +501,49 @@ bool panel(int64_t rows, int64_t cols, int64_t red) {
 template <class J>
 e3_status dense_panel(DenseArgs a, const char* name, hipStream_t st) {
   using T = typename J::T;
-  const int64_t groups = (a.cols + 63) / 64;
+  if constexpr (sizeof(T) == 4) {
+    // Shared row blocks: four waves, or two where the terms of B are few (more
+    // would leave them without registers for two workgroups per CU); the columns
+    // past the last 256 in a launch of their own.
+    const int64_t four = a.cols / 256 * 256;
+    const int wpb = four == a.cols || (a.red > 32 && four > 0) ? 4 : a.red <= 32 && a.cols % 128 == 0 ? 2 : 0;
+    if (Tail<T>::plain(a) && wpb) {
+      DenseArgs m = a;
+      if (wpb == 4) m.cols = (int)four;
+      const int64_t col = m.cols / (64 * wpb);
+      m.splits = (int)std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 2048 / wpb / col));
+      {
+        TimedLaunch t_(name, st);
+        auto* k = wpb == 2 ? k_dense_shared<J, 32, 2> : a.red <= 32 ? k_dense_shared<J, 32, 4> : k_dense_shared<J, 64, 4>;
+        hipLaunchKernelGGL(k, grid_of(m.splits * col), dim3(wpb * kWave), 0, st, m);
+        E3_HIP(hipGetLastError());
+      }
+      if (m.cols == a.cols) return E3_OK;
+      a.cols -= m.cols;
+      a.b.p = static_cast<const T*>(a.b.p) + (J::FB == kAlong ? m.cols * a.b.ld : m.cols);
+      a.y = static_cast<T*>(a.y) + m.cols;
+      if (a.bias) a.bias = static_cast<const T*>(a.bias) + m.cols;
+      return dense_panel<J>(a, name, st);
+    }
+  }
   // two workgroups per CU, each wave on row blocks of its own
+  const int64_t groups = (a.cols + 63) / 64;
   a.splits = (int)std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 2048 / groups));
   const int64_t blocks = (a.splits * groups + 3) / 4;
   TimedLaunch t_(name, st);
-  constexpr int U = kPanel<T> / 64;  // 16-index pieces in units of a quarter of the longest
-  const bool fast = a.red % (16 * U) == 0 && a.red >= 32 * U && a.cols % 64 == 0 && a.nt;
   auto go = [&](auto KK) {
     constexpr int kk = decltype(KK)::value;
+    const bool fast = a.red == 16 * kk && a.cols % 64 == 0 && Tail<T>::plain(a);
     auto* k = fast ? k_dense_panel<J, kk, 2, true> : k_dense_panel<J, kk, 2, false>;
     hipLaunchKernelGGL(k, grid_of(blocks), dim3(256), 0, st, a);
   };
-  if (a.red <= 32 * U) go(std::integral_constant<int, 2 * U>{});
-  else if (a.red <= 48 * U) go(std::integral_constant<int, 3 * U>{});
-  else go(std::integral_constant<int, 4 * U>{});
+  if (a.red <= 32) go(std::integral_constant<int, 2>{});
+  else if (sizeof(T) == 4 && a.red <= 48) go(std::integral_constant<int, 3>{});
+  else if (a.red <= 64) go(std::integral_constant<int, 4>{});
+  else if constexpr (sizeof(T) == 2) {
+    if (a.red <= 96) go(std::integral_constant<int, 6>{});
+    else go(std::integral_constant<int, 8>{});
+  }
   E3_HIP(hipGetLastError());
   return E3_OK;
 }

@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {
     sums();
     load(fast, at(tile0 + gridDim.x));
     for (int64_t tile = tile0; tile < tiles; tile += gridDim.x) {
-      residuals(tile, res);
+      if (!FAST) residuals(tile, res);
       out(fast, tile, res);
       sums();
       load(fast, at(tile + 2 * (int64_t)gridDim.x));
@@ -167,7 +167,7 @@ e3_status dense_thin(const DenseArgs& a, hipStream_t st) {
   const int64_t tiles = (a.rows + R - 1) / R, cols = (a.cols + L * V - 1) / (L * V);
   const int64_t blocks = std::min<int64_t>(tiles, std::max<int64_t>(1, 1536 / cols));
   TimedLaunch t_("dense_thin", st);
-  auto* k = a.nt && a.red == KC && a.cols % (L * V) == 0 ? k_dense_thin<T, L, KC, true> : k_dense_thin<T, L, KC, false>;
+  auto* k = Tail<T>::plain(a) && a.red == KC && a.cols % (L * V) == 0 ? k_dense_thin<T, L, KC, true> : k_dense_thin<T, L, KC, false>;
   hipLaunchKernelGGL(k, dim3((unsigned)blocks, (unsigned)cols), dim3(256), 0, st, a);
   E3_HIP(hipGetLastError());
   return E3_OK;

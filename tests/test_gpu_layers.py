@@ -343,6 +343,76 @@ def test_dense_many_rows(e3, dt, M, K, N):
             assert rel_l2(host(g), w) < TOL_BWD[dt]
 
 
+# rows enough for the kernels that walk row blocks with W in registers: whole and partial blocks of 32
+# rows, K at and off their steps, columns in whole 64s, 128s, 256s and ragged; outputs past the caches
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("M,K,N,gap", [(262149, 64, 64, 0), (262176, 32, 64, 0), (131077, 48, 128, 0), (100003, 64, 320, 0),
+                                       (70001, 30, 256, 0), (66001, 64, 300, 5), (140000, 128, 128, 0),
+                                       (262149, 61, 61, 3), (160000, 8, 64, 0), (550001, 8, 64, 0), (262149, 16, 130, 0),
+                                       (140001, 96, 64, 2)])
+def test_dense_row_blocks(e3, dt, M, K, N, gap):
+    import torch
+    rng = _rng(M, K, N)
+    x = rng.standard_normal((M, K), dtype=np.float32)
+    W, b = rng.standard_normal((K, N)) / np.sqrt(K), rng.standard_normal(N)
+    xd, Wd, bd = dev(x, dt, gap, 1 if gap else 0), dev(W, dt), dev(b, dt)
+    xd[5, K - 1], xd[M - 2, 0] = float("inf"), float("nan")
+    # a sample of rows: the first and last blocks, and some between
+    rows = np.unique(np.concatenate([np.arange(70), rng.integers(0, M, 3000), np.arange(M - 70, M)]))
+    at = torch.from_numpy(rows).cuda()
+    print("[case] dense, row blocks", dt, M, K, N, gap, flush=True)
+    with np.errstate(invalid="ignore"):
+        z = host(xd[at]) @ host(Wd) + host(bd)
+    fine = np.isfinite(z)
+    assert not fine[5].any() and not fine[-2].any() and fine.sum() == (len(rows) - 2) * N
+    y = e3.dense_fwd(xd, Wd, bd, act="silu")
+    got = host(y[at])
+    assert np.array_equal(np.isnan(got[-2]), np.isnan(z[-2])) and rel_l2(got[fine], rounded(ol.act("silu", z[fine])[0], dt)) < TOL[dt]
+    assert bool(torch.isfinite(y).all(1).sum() >= M - 2)
+    plain = e3.dense_fwd(xd, Wd)
+    with np.errstate(invalid="ignore"):
+        ref = host(xd[at]) @ host(Wd)
+    assert np.array_equal(host(plain[at])[~fine], ref[~fine], equal_nan=True)
+    assert rel_l2(host(plain[at])[fine], rounded(ref[fine], dt)) < TOL[dt]
+    # with everything beside y: the same y, into rows of a wider tensor
+    r = torch.zeros_like(y)
+    out, untouched = out_like((M, N), dt, gap, gap)
+    _, zz, z8, y8 = e3.dense_fwd(xd, Wd, bd, r, act="silu", keep=("z", "z8", "y8"), out=out)
+    assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(y)) and untouched()
+    assert rel_l2(host(zz[at])[fine], rounded(z[fine], dt)) < TOL[dt]
+    keep = np.isfinite(z).all(1)
+    near_steps(e3.Packed8(z8.q[at][torch.from_numpy(keep).cuda()], z8.c[at][torch.from_numpy(keep).cuda()]), z[keep])
+    q, c = ol.pack8(host(y[at]))
+    assert np.array_equal(y8.q[at].cpu().numpy(), q) and np.array_equal(y8.c[at].cpu().numpy(), c)
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("M,K,N,gap", [(262149, 64, 64, 0), (131077, 256, 64, 0), (140000, 128, 32, 0), (100003, 300, 61, 2),
+                                       (140001, 64, 128, 0)])
+@pytest.mark.parametrize("ckpt", [False, True])
+def test_dense_backward_row_blocks(e3, dt, M, K, N, gap, ckpt):
+    import torch
+    rng = _rng(M, K, N)
+    x, dy, z = (rng.standard_normal(s, dtype=np.float32) for s in ((M, K), (M, N), (M, N)))
+    W = rng.standard_normal((K, N)) / np.sqrt(K)
+    xd, Wd, dyd, zd = dev(x, dt, gap, gap), dev(W, dt), dev(dy, dt, gap, gap), dev(z, dt, gap, gap)
+    xin, zin = (e3.pack8(xd), e3.pack8(zd)) if ckpt else (xd, zd)
+    xr, zr = (values(xin), values(zin)) if ckpt else (host(xd), host(zd))
+    for act in ("none", "gelu"):
+        print("[case] dense_bwd, row blocks", dt, M, K, N, gap, ckpt, act, flush=True)
+        got = e3.dense_bwd(xin, Wd, dyd, None if act == "none" else zin, act=act)
+        if act == "gelu":
+            from scipy.special import ndtr
+            dz = host(dyd) * (ndtr(zr) + zr * np.exp(-0.5 * zr * zr) / np.sqrt(2 * np.pi))
+        else:
+            dz = host(dyd)
+        ref = [*ol.dense_bwd(xr, host(Wd), rounded(dz, dt))[:2], dz.sum(0)]
+        for g, w in zip(got, ref):
+            assert rel_l2(host(g), rounded(w, dt)) < TOL_BWD[dt]
+        for k, w in enumerate(("dx", "dW", "db")):
+            assert torch.equal(e3.dense_bwd(xin, Wd, dyd, None if act == "none" else zin, act=act, want=(w,))[k], got[k])
+
+
 @pytest.mark.parametrize("M,K,N", [(3, 40, 50), (200, 130, 70), (1000, 64, 64)])
 def test_dense_infinities_and_nans_stay_in_their_rows_and_columns(e3, M, K, N):
     """An infinity in x reaches its own row of y, one in W its own column, as in float32 arithmetic;
