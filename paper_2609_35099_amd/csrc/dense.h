@@ -609,7 +609,8 @@ Cut dense_cut(e3_dtype t, int64_t rows, int64_t cols, int64_t red, bool fwd = fa
   }
   c.tiles = c.tile == 256 && fwd ? tiles(256, 128) : tiles(c.tile);
   // at least 256 indexes a split; few tiles of few indexes take down to 64
-  const int64_t least = c.tiles * (red / 256) < kFill / 8 ? 64 : c.tile == 256 ? 2048 : 256;
+  int64_t least = c.tiles * (red / 256) < kFill / 8 ? 64 : c.tile == 256 ? 2048 : 256;
+  if (red <= 384) least = 384;  // what a launch to join them takes is longer
   const int64_t s = std::max<int64_t>(
       1, std::min<int64_t>({fill / std::max<int64_t>(c.tiles, 1), (red + least - 1) / least, 256}));
   c.chunk = std::max<int64_t>(64, ((red + s - 1) / s + 63) / 64 * 64);

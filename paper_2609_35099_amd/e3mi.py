@@ -161,11 +161,17 @@ def _ptr(t, name, shape=None, dtype="float32"):
     return t.data_ptr() if t.numel() else None
 
 
+_current = None   # torch's raw-stream and device queries
+
+
 def _stream(stream):
     if stream is not None:
         return stream.cuda_stream
-    c = _torch()._C   # torch.cuda.current_stream().cuda_stream, without the stream object (2.8 us a call)
-    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
+    global _current
+    if _current is None:   # torch.cuda.current_stream().cuda_stream, without the stream object (2.8 us a call)
+        c = _torch()._C
+        _current = c._cuda_getCurrentRawStream, c._cuda_getDevice
+    return _current[0](_current[1]())
 
 
 def _on_stream(fn):
@@ -686,20 +692,22 @@ _LAYER_DTYPES = {}   # torch dtype -> (e3_dtype, its name)
 
 
 def _layer_dtype(t, name):
-    torch = _torch()
-    if not _LAYER_DTYPES:
+    """(e3_dtype, type's name) of a tensor the layers take."""
+    try:
+        return _LAYER_DTYPES[t.dtype]
+    except (KeyError, AttributeError):
+        torch = _torch()
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch tensor") from None
         _LAYER_DTYPES.update({torch.float32: (0, "float32"), torch.bfloat16: (1, "bfloat16")})
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor")
-    got = _LAYER_DTYPES.get(t.dtype)
-    if got is None:
-        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    return got
+        if t.dtype not in _LAYER_DTYPES:
+            raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}") from None
+        return _LAYER_DTYPES[t.dtype]
 
 
 def _rows(t, name, shape, dtype):
     """(pointer, row stride) of a matrix whose rows are contiguous; rows may be strided."""
-    torch = _torch()
+    torch = _modules[0] if _modules else _torch()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     if t.dtype is not _modules[1][dtype]:
@@ -709,16 +717,20 @@ def _rows(t, name, shape, dtype):
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     m, n = shape
+    if m > 1:
+        ld, one = t.stride()
+        if one == 1 and ld >= n:
+            return t.data_ptr(), ld
+        if n > 1 and one != 1:
+            raise ValueError(f"{name} must have contiguous rows")
+        if ld < n:
+            raise ValueError(f"{name} has overlapping rows")
+        return t.data_ptr(), ld
     if m == 0:
         return None, n
-    ld, one = t.stride()
-    if n > 1 and one != 1:
+    if n > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    if m == 1:
-        ld = n
-    elif ld < n:
-        raise ValueError(f"{name} has overlapping rows")
-    return t.data_ptr(), ld
+    return t.data_ptr(), n
 
 
 class Packed8:
@@ -765,9 +777,10 @@ def _kept(t, name, shape, dtype):
 
 
 def _matrix(t, name):
-    if len(t.shape) != 2:
-        raise ValueError(f"{name} must be a matrix, got shape {tuple(t.shape)}")
-    return t.shape
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} must be a matrix, got shape {tuple(shape)}")
+    return shape
 
 
 @_on_stream
