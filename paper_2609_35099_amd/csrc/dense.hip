@@ -12,7 +12,8 @@ namespace {
 // Reductions of at most KC <= 16 (a radial basis): the weights of a thread's V
 // columns stay in registers, rows go by with the next one's x in flight, and no
 // LDS is used; L lanes share a row.  Bound by the write of y: 1,248,000 x 8 x 64
-// float32 @THIN@ us, where the tile product took 156 (its steps are of 32).
+// float32 with silu 58 us (6.2 TB/s; 320 MB of zeros take 46), where the tile
+// product took 156 (its steps are of 32).
 template <class T, int L, int KC, bool FAST>
 __global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {
   constexpr int V = Elem<T>::V, R = 256 / L, P = KC / V > 0 ? KC / V : 1;
@@ -30,8 +31,8 @@ __global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {
       for (int i = 0; i < V; ++i) w[k][i] = 0.0f;
     }
   }
-  // U rows a thread and round, the next round's x in flight: with one, the rows'
-  // latency was most of the time (@ONE@ us)
+  // U rows a thread and round, the next round's x in flight (one row a round: 129
+  // us against 117 before the stores were non-temporal)
   constexpr int U = 4;
   constexpr int TR = R * U;  // rows of a round
   const int lr = threadIdx.x / L;
@@ -106,7 +107,8 @@ __global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {
 }
 
 // At most MR <= 8 rows: W is read once, straight to registers, and that is what
-// bounds it.  A workgroup takes 32 columns; its lanes of a column piece take
+// bounds it (one row of 1,024 to 4,096 in bfloat16 5.8 us, of which a launch is
+// about half).  A workgroup takes 32 columns; its lanes of a column piece take
 // every G-th reduction index, and their sums are added over the wave and then
 // over the waves in order.
 template <class T, int MR>
