@@ -54,17 +54,22 @@ struct Tail {
     for (int i = 0; i < V; ++i) bias[i] = 0.0f;
     if (a.bias) ld_piece<T>(static_cast<const T*>(a.bias) + col, a.cols - col, bias);
   }
-  using Raw = typename Elem<T>::vec;
+  struct Raw {
+    u4v v;
+    Cutting cut;
+  };
+  static constexpr unsigned kUncut = 128;
   static __device__ __forceinline__ Raw residual(const DenseArgs& a, int64_t row0, int lr, bool ok, int col) {
-    if (!a.res) return Raw{};
+    Raw r{{}, {kUncut}};
+    if (!a.res) return r;
     const int64_t total = (a.rows - 1) * a.ldr + a.cols;
-    if (total >= V) {
-      const int n = a.cols - col;
-      const int64_t row = ok ? row0 + lr : 0;  // any row inside
-      return __builtin_bit_cast(Raw, ld_span<u4v>(static_cast<const T*>(a.res), row * a.ldr + col, total,
-                                                  !ok || n < 0 ? 0 : n < V ? n : V));
-    }
-    return ld_raw<T>(static_cast<const T*>(a.res) + (row0 * a.ldr + (lr * a.ldr + col)), ok ? a.cols - col : 0);
+    const int n = a.cols - col;
+    const T* p = static_cast<const T*>(a.res);
+    if (total >= V)
+      r.v = ld_span<u4v>(p, (ok ? row0 + lr : 0) * a.ldr + col, total, !ok || n < 0 ? 0 : n < V ? n : V, r.cut);
+    else
+      r.v = __builtin_bit_cast(u4v, ld_raw<T>(p + (row0 * a.ldr + (lr * a.ldr + col)), ok ? n : 0));
+    return r;
   }
   // FAST: the piece is inside the row, y streams, and there is neither a residual
   // nor an output beside it (plain()), so that a round of a loop over rows has no
@@ -88,13 +93,14 @@ struct Tail {
     act_piece(a.act, v);
     if (!FAST && a.res) {
       float u[V];
-      Elem<T>::get(res, u);
+      if (__ballot(res.cut.down_keep != kUncut)) res.v = res.cut(res.v);
+      Elem<T>::get(__builtin_bit_cast(typename Elem<T>::vec, res.v), u);
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] += u[i];
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = Elem<T>::round(v[i]);
-    if constexpr (FAST) __builtin_nontemporal_store(Elem<T>::put(v), reinterpret_cast<Raw*>(static_cast<T*>(a.y) + at(a.ldy)));
+    if constexpr (FAST) __builtin_nontemporal_store(Elem<T>::put(v), reinterpret_cast<typename Elem<T>::vec*>(static_cast<T*>(a.y) + at(a.ldy)));
     else st_piece<T>(static_cast<T*>(a.y) + at(a.ldy), n, v, a.nt);
     if (!FAST && a.yq) pack(a.yq, a.yc);
   }
@@ -478,13 +484,17 @@ __global__ __launch_bounds__(WPB* kWave, 2) void k_dense_shared(DenseArgs a) {
   };
   if (chunk >= blocks) return;  // the whole workgroup
   load(chunk);
-  la.template store<false>(in[0], a.grad_act, none);
+  auto store = [&](typename LA::Lds& to) {
+    if (K == BK) la.template store<false, true>(to, a.grad_act, none);
+    else la.template store<false, false>(to, a.grad_act, none);
+  };
+  store(in[0]);
   load(chunk + a.splits);
   __syncthreads();
   int64_t block = chunk;
   for (; block < whole; block += a.splits) {
     product();
-    la.template store<false>(in[cur ^ 1], a.grad_act, none);
+    store(in[cur ^ 1]);
     load(block + 2 * (int64_t)a.splits);
     rows32_out<J, NC, true>(a, 0, block * 32, col0, 0, a.red, out[wave], acc);
     __syncthreads();

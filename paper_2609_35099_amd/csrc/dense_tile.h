@@ -100,18 +100,33 @@ struct Fetch {
   typedef Raw Any __attribute__((aligned(sizeof(E))));
   Raw raw[N];
   unsigned char exps[Q ? N : 1];
+  Cutting cut[N];  // of pieces that are not whole
 
   static __device__ __forceinline__ int row_of(int i) { return threadIdx.x / PER + i * (THREADS / PER); }
   static __device__ __forceinline__ int col_of() { return threadIdx.x % PER * V; }
-  static __device__ __forceinline__ bool whole_cols(int64_t r0, int64_t rows) { return F == kAlong || r0 + W <= rows; }
+  // The reduction index before which the tile's pieces are inside the matrix's
+  // span: where rows or columns end within the tile (across), pieces past the end
+  // hold values of the next row, which only reach results that are not stored.
+  static __device__ __forceinline__ int64_t whole_until(const Side& s, int64_t r0, int64_t rows) {
+    constexpr int64_t all = (int64_t)1 << 62;
+    if (F == kAlong || r0 + W <= rows) return all;
+    const int64_t room = s.total - r0 - W;
+    int64_t m = room < 0 ? 0 : room / s.ld + 1;
+    if constexpr (Q) {
+      const int64_t left = s.total / s.ld * s.ldc - r0 / kGroup - W / kGroup, mc = left < 0 ? 0 : left / s.ldc + 1;
+      m = mc < m ? mc : m;
+    }
+    return m;
+  }
 
   // The tile at output index r0 and reduction index k0 of an operand with `rows`
   // output indexes; reduction indexes from `end` on are zero; output indexes
   // past the end read as the last row (along) or zero (across): their results
-  // are not stored.  WHOLE: no piece crosses a row's end and all reduction
-  // indexes are inside (a tile's own loop: with both ways in one loop, the loaded
-  // registers were copied where the ways meet, which waits for the loads).
-  // Otherwise pieces may reach into the next row (ld_span) and are cut.
+  // are not stored.  WHOLE: all reduction indexes and all pieces are inside (up to
+  // whole_until(); a loop of its own: with both ways in one, the loaded registers
+  // were copied where the ways meet, which waits for the loads).
+  // Otherwise pieces may reach into the next row (ld_span) and are cut when they
+  // are used.
   template <bool WHOLE>
   __device__ __forceinline__ void load(const Side& s, int64_t r0, int64_t rows, int64_t k0, int64_t end) {
     // memory row m0 + row_of(i), column c0 + col_of(): the uniform part in the base
@@ -137,23 +152,26 @@ struct Fetch {
     for (int i = 0; i < N; ++i) {
       const bool in = F == kAlong || row_of(i) <= mlast;
       const int64_t m = imin(row_of(i), mlast);
-      raw[i] = ld_span<Raw>(first, (m0 + m) * s.ld + c0 + lc, s.total, in ? n : 0);
-      if constexpr (Q) {
-        // a step's exponent only where something was read: a NaN step times a zero is NaN
-        const unsigned char e = pc[m * s.ldc + imin(lc, left - 1) / kGroup];
-        exps[i] = in && n > 0 ? e : 0;
-      }
+      raw[i] = ld_span<Raw>(first, (m0 + m) * s.ld + c0 + lc, s.total, in ? n : 0, cut[i]);
+      if constexpr (Q) exps[i] = pc[m * s.ldc + imin(lc, left - 1) / kGroup];
     }
   }
-  // The values of piece i.
+  // Piece i as it lies in memory, and its values.
+  template <bool WHOLE>
+  __device__ __forceinline__ Raw bits(int i) const {
+    return WHOLE ? raw[i] : cut[i](raw[i]);
+  }
+  template <bool WHOLE>
   __device__ __forceinline__ void get(int i, float (&v)[V]) const {
+    const Raw b = bits<WHOLE>(i);
     if constexpr (Q) {
       Raw8<V> r;
-      r.e = exps[i];
-      if constexpr (V == 4) r.w[0] = raw[i]; else r.w[0] = raw[i].x, r.w[1] = raw[i].y;
+      // a step's exponent only where something was read: a NaN step times a zero is NaN
+      r.e = !WHOLE && cut[i].none() ? 0u : exps[i];
+      if constexpr (V == 4) r.w[0] = b; else r.w[0] = b.x, r.w[1] = b.y;
       get8(r, v);
     } else {
-      Elem<T>::get(__builtin_bit_cast(typename Elem<T>::vec, raw[i]), v);
+      Elem<T>::get(__builtin_bit_cast(typename Elem<T>::vec, b), v);
     }
   }
 };
@@ -177,7 +195,12 @@ struct Loader {
   Main x;
   typename std::conditional<G, Pre, None>::type z;
 
-  static __device__ __forceinline__ bool whole_cols(int64_t r0, int64_t rows) { return Main::whole_cols(r0, rows); }
+  static __device__ __forceinline__ int64_t whole_until(const Side& s, const Side& pre, int64_t r0, int64_t rows) {
+    const int64_t m = Main::whole_until(s, r0, rows);
+    if constexpr (!G) return m;
+    const int64_t p = Pre::whole_until(pre, r0, rows);
+    return p < m ? p : m;
+  }
   template <bool WHOLE>
   __device__ __forceinline__ void load(const Side& s, const Side& pre, int64_t r0, int64_t rows, int64_t k0,
                                        int64_t end) {
@@ -185,20 +208,20 @@ struct Loader {
     if constexpr (G) z.template load<WHOLE>(pre, r0, rows, k0, end);
   }
   // To LDS; `sum` (where wanted) grows by the values of the thread's columns.
-  template <bool SUM>
+  template <bool SUM, bool WHOLE>
   __device__ __forceinline__ void store(Lds& l, int act, float (&sum)[V]) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int row = Main::row_of(i), col = Main::col_of();
       const int o = Lds::off(row, col / 8) + col % 8;
       if constexpr (KD == kFull && sizeof(T) == 2 && !SUM) {
-        *reinterpret_cast<u4v*>(&l.v[0][o]) = x.raw[i];
+        *reinterpret_cast<u4v*>(&l.v[0][o]) = x.template bits<WHOLE>(i);
       } else {
         float v[V];
-        x.get(i, v);
+        x.template get<WHOLE>(i, v);
         if constexpr (G) {
           float w[V];
-          z.get(i, w);
+          z.template get<WHOLE>(i, w);
           act_grad_piece(act, w, v);
         }
         if constexpr (SUM)
@@ -293,7 +316,11 @@ struct Tile {
     if constexpr (SUM)
 #pragma unroll
       for (int e = 0; e < LB::V; ++e) sum[e] = 0.0f;
-    const int64_t whole = LA::whole_cols(r0, rows) && LB::whole_cols(c0, cols) ? k0 + (end - k0) / BK * BK : k0;
+    int64_t until = ONLY ? end : LA::whole_until(g.a, g.z, r0, rows);
+    const int64_t ub = LB::whole_until(g.b, g.z, c0, cols);
+    until = until < ub ? until : ub;
+    until = until < end ? until : end;
+    const int64_t whole = until > k0 ? k0 + (until - k0) / BK * BK : k0;
     steps<true, ONLY>(sh, g, r0, rows, c0, cols, k0, whole, row0, col0);
     steps<false, ONLY>(sh, g, r0, rows, c0, cols, whole, end, row0, col0);
   }
@@ -309,8 +336,8 @@ struct Tile {
     };
     auto store = [&](int buf) {
       float none[LA::V];
-      if constexpr (!ONLY) la.template store<false>(sh.in[buf].a, g.act, none);
-      lb.template store<SUM>(sh.in[buf].b, g.act, sum);
+      if constexpr (!ONLY) la.template store<false, WHOLE>(sh.in[buf].a, g.act, none);
+      lb.template store<SUM, WHOLE>(sh.in[buf].b, g.act, sum);
     };
     load(k);
     __syncthreads();

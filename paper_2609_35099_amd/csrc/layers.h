@@ -96,17 +96,26 @@ __device__ __forceinline__ u2v low_bits(u2v r, int bits) { return u2v{low_bits(r
 __device__ __forceinline__ u4v low_bits(u4v r, int bits) {
   return u4v{low_bits(r.x, bits), low_bits(r.y, bits - 32), low_bits(r.z, bits - 64), low_bits(r.w, bits - 96)};
 }
-// Values at .. at + n - 1 of a matrix that spans `total` values from p (the rest
-// of the piece zero) without a branch, so that several loads are in flight: a
+// Values at .. at + n - 1 of a matrix that spans `total` values from p, the rest
+// of the piece zero, without a branch, so that several loads are in flight: a
 // piece that would reach past the span is loaded from its last values and moved
-// down.  total is at least a piece.
+// down.  total is at least a piece.  The load and its cutting are apart: cutting
+// waits for the load.
+struct Cutting {
+  unsigned down_keep;  // bits to move down << 16 | bits to keep
+  template <class R>
+  __device__ __forceinline__ R operator()(R r) const {
+    return low_bits(shift_down(r, down_keep >> 16), (int)(down_keep & 0xffffu));
+  }
+  __device__ __forceinline__ bool none() const { return (down_keep & 0xffffu) == 0; }
+};
 template <class R, class E>
-__device__ __forceinline__ R ld_span(const E* p, int64_t at, int64_t total, int n) {
+__device__ __forceinline__ R ld_span(const E* p, int64_t at, int64_t total, int n, Cutting& cut) {
   typedef R Any __attribute__((aligned(sizeof(E))));
   constexpr int V = sizeof(R) / sizeof(E), BITS = 8 * sizeof(E);
   const int64_t start = at < total - V ? at : total - V, over = at - start;
-  const R r = shift_down(*reinterpret_cast<const Any*>(p + start), (over < V ? (unsigned)over : (unsigned)V) * BITS);
-  return low_bits(r, n * BITS);
+  cut.down_keep = (over < V ? (unsigned)over : (unsigned)V) * BITS << 16 | (unsigned)(n * BITS);
+  return *reinterpret_cast<const Any*>(p + start);
 }
 // nt: past the caches, for outputs that do not fit them (rule and figures at
 // streams()).
