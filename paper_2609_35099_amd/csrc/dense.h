@@ -192,16 +192,19 @@ __device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_
 //     942 with 256 x 256; with gelu and z in 8 bits 244 us against 261).
 //   bfloat16, 128 and 64: 4 waves, steps of 64, two buffers, two workgroups and
 //     more: 685, 906, 867.
-//   float32, 128 x 128: one buffer of the three planes; rows along the reduction
-//     with 8 waves of 32 x 64 (179 TFLOP/s; 4 of 64 x 64 161, 256 x 256 145),
-//     across with 4 (208; 8 193).
+//   float32: one buffer of the three planes.  Rows along the reduction take 64 x
+//     128 by 4 waves, four workgroups per CU that load, split and multiply beside
+//     each other (128 x 128 by 8 waves, two per CU: dx of 100,003 x 128 x 256 96 us
+//     against 79, forward 100,000 x 128 x 256 80 against 64, 60,000 x 100 x 1,000 187
+//     against 158, but 4,096 x 2,048 x 1,024 143 against 150); across 128 x 128 by 4
+//     (208 TFLOP/s; 8 193).
 template <class J, int B>
 struct TileOf {
-  static constexpr bool f32 = sizeof(typename J::T) == 4, fwd = J::FA == kAlong && J::FB == kAcross;
-  static constexpr int BN = B == 256 && fwd ? 128 : B;
-  static constexpr int WM = B == 256 || (f32 && B == 128 && J::FA == kAlong) ? 4 : 2, WN = B == 256 ? BN / 64 : 2;
+  static constexpr bool f32 = sizeof(typename J::T) == 4, along = J::FA == kAlong, fwd = along && J::FB == kAcross;
+  static constexpr int BM = f32 && along && B == 128 ? 64 : B, BN = B == 256 && fwd ? 128 : B;
+  static constexpr int WM = B == 256 ? 4 : 2, WN = B == 256 ? BN / 64 : 2;
   static constexpr int BK = f32 || B == 256 ? 32 : 64, THREADS = WM * WN * kWave, OCC = B == 256 ? 4 : 2;
-  using type = Tile<typename J::T, J::FA, J::FB, B, BN, BK, WM, WN, J::KA, J::KB, J::SUM, f32 ? 1 : 2>;
+  using type = Tile<typename J::T, J::FA, J::FB, BM, BN, BK, WM, WN, J::KA, J::KB, J::SUM, f32 ? 1 : 2>;
 };
 
 // Which tile block u of tm x tn takes: blocks go round robin to the XCDs, so an
@@ -255,7 +258,7 @@ template <class J, int B>
 __global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void k_dense(DenseArgs a) {
   using Tl = typename TileOf<J, B>::type;
   __shared__ __align__(16) typename Tl::Shared sh;
-  dense_block<J, Tl, B, TileOf<J, B>::BN>(a, sh, block_id());
+  dense_block<J, Tl, TileOf<J, B>::BM, TileOf<J, B>::BN>(a, sh, block_id());
 }
 // Short reductions (up to 16 KK) over many rows: no LDS and no barriers before the
 // epilogue.  A wave keeps the terms of its 32 NC columns of B in registers for
@@ -597,11 +600,12 @@ __global__ __launch_bounds__(256) void k_dense_join(DenseArgs a, int splits) {
 // How a product is cut: square tiles, and splits of its reduction where the
 // tiles alone would leave much of the card idle.
 struct Cut {
-  int tile, splits;  // of tile x tile; 256: 256 x 128 where the forward's epilogue follows
+  int tile, splits;  // TileOf's B
   int64_t tiles, chunk;
 };
+enum Product { kForward, kDx, kDw };
 constexpr int kFill = 512;  // workgroups of the smaller tiles that fill the card
-Cut dense_cut(e3_dtype t, int64_t rows, int64_t cols, int64_t red, bool fwd = false) {
+Cut dense_cut(e3_dtype t, int64_t rows, int64_t cols, int64_t red, Product which) {
   Cut c{};
   auto tiles = [&](int b, int bn = 0) {
     bn = bn ? bn : b;
@@ -620,9 +624,12 @@ Cut dense_cut(e3_dtype t, int64_t rows, int64_t cols, int64_t red, bool fwd = fa
     // tile, of which two run on a CU at 0.78 of the rate; splits of 2,048 at least
     const int64_t s = std::max<int64_t>(1, std::min(256 / t256, red / 2048));
     const double big = (double)((t256 * s + 255) / 256) * 4.0 / (double)s;
-    if (t256 * s >= 192 && big <= (double)((t128 + kFill - 1) / kFill) * 2.56) c.tile = 256, fill = fwd ? 512 : 256;
+    if (t256 * s >= 192 && big <= (double)((t128 + kFill - 1) / kFill) * 2.56)
+      c.tile = 256, fill = which == kForward ? 512 : 256;
   }
-  c.tiles = c.tile == 256 && fwd ? tiles(256, 128) : tiles(c.tile);
+  c.tiles = tiles(c.tile);
+  if (c.tile == 256 && which == kForward) c.tiles = tiles(256, 128);
+  if (c.tile == 128 && t == E3_F32 && which != kDw) c.tiles = tiles(64, 128), fill = 2 * kFill;  // 64 x 128 by TileOf
   // at least 256 indexes a split; few tiles of few indexes take down to 64
   int64_t least = c.tiles * (red / 256) < kFill / 8 ? 64 : c.tile == 256 ? 2048 : 256;
   if (red <= 384) least = 384;  // what a launch to join them takes is longer
@@ -644,7 +651,7 @@ void set_cut(DenseArgs& a, const Cut& c, float* part, int64_t tail = 0) {
 // The products of the backward form dz from dy and z on the way to LDS: once per
 // 128 columns of x, so up to this many; wider layers write dz once.  (Two rounds
 // of an activation's derivative cost less than dz's way to memory and back:
-// 100,003 x 128 x 256 float32 from 8 bits, 169 us against 234.)
+// 100,003 x 128 x 256 float32 from 8 bits, 144 us against 162.)
 constexpr int64_t kOnTheFly = 256;
 
 struct DenseBwdWs {
@@ -661,7 +668,7 @@ DenseBwdWs dense_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
     w.db = up256(w.db_blocks * N * 4);
   }
   // the partial sums of both products, side by side: one launch may make both
-  const size_t dx = cut_bytes(dense_cut(t, M, K, N), M, K), dw = cut_bytes(dense_cut(t, K, N, M), K, N, N);
+  const size_t dx = cut_bytes(dense_cut(t, M, K, N, kDx), M, K), dw = cut_bytes(dense_cut(t, K, N, M, kDw), K, N, N);
   w.part = dx + dw;
   w.total = M == 0 ? 0 : w.dz + w.db + w.part;
   return w;
@@ -698,7 +705,8 @@ constexpr e3_dtype dtype_of(const float*) { return E3_F32; }
 constexpr e3_dtype dtype_of(const __bf16*) { return E3_BF16; }
 template <class J>
 e3_status dense_product(DenseArgs a, float* part, const char* name, hipStream_t st) {
-  const Cut c = dense_cut(dtype_of(static_cast<const typename J::T*>(nullptr)), a.rows, a.cols, a.red, true);
+  const e3_dtype t = dtype_of(static_cast<const typename J::T*>(nullptr));
+  const Cut c = dense_cut(t, a.rows, a.cols, a.red, kForward);
   set_cut(a, c, part);
   const e3_status s = dense_launch<J>(a, c, name, st);
   return s != E3_OK || c.splits == 1 ? s : dense_join<typename J::T>(a, st);

@@ -186,7 +186,7 @@ e3_status dense_few(const DenseArgs& a, hipStream_t st) {
 
 size_t dense_fwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   const bool p = t == E3_F32 ? panel<float>(M, N, K) : panel<__bf16>(M, N, K);
-  return M <= kFew || K <= kThin || p ? 0 : cut_bytes(dense_cut(t, M, N, K, true), M, N);
+  return M <= kFew || K <= kThin || p ? 0 : cut_bytes(dense_cut(t, M, N, K, kForward), M, N);
 }
 template <class T>
 e3_status dense_fwd(const DenseArgs& a, float* part, hipStream_t st) {

@@ -9,7 +9,7 @@ template <class J, int B>
 __global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void k_dense_sums(DenseArgs a) {
   using Tl = typename TileOf<J, B>::type;
   __shared__ __align__(16) typename Tl::Shared sh;
-  dense_block<J, Tl, B, TileOf<J, B>::BN, true>(a, sh, block_id());
+  dense_block<J, Tl, TileOf<J, B>::BM, TileOf<J, B>::BN, true>(a, sh, block_id());
 }
 // Two products in one launch: the first `first` blocks take the first.
 template <class J, class K, int B>
@@ -108,7 +108,7 @@ e3_status dense_bwd_products(DenseArgs x, DenseArgs w, float* part, hipStream_t 
   using JX = Job<T, kAlong, kAlong, KD, kFull, false>;
   using JW = Job<T, kAcross, kAcross, KX, KD, FLY>;
   const bool dx = x.y, dw = w.y, db = w.sums;
-  const Cut cx = dense_cut(t, x.rows, x.cols, x.red), cw = dense_cut(t, w.rows, w.cols, w.red);
+  const Cut cx = dense_cut(t, x.rows, x.cols, x.red, kDx), cw = dense_cut(t, w.rows, w.cols, w.red, kDw);
   const bool along = panel<T>(x.rows, x.cols, x.red);
   set_cut(x, cx, part);
   set_cut(w, cw, part + cut_bytes(cx, x.rows, x.cols) / sizeof(float), w.cols);
