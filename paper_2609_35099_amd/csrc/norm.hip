@@ -132,10 +132,14 @@ __global__ __launch_bounds__(kNormFwdThreads<L>) void k_norm_fwd(NormArgs a) {
 // row is worked on.  Workgroups are large and few, so that little is left for
 // the sum over them: 512 threads where a row takes at most a wave (1,024 leave
 // too few registers), one row where it takes more.
+// Which products are fused into sums is written out: left to the compiler, it
+// differs between the instances, and a gradient asked for alone (another instance
+// where dx streams) had other bits than beside dx.
 template <int L>
 constexpr int kNormBwdThreads = L <= kWave ? 512 : L;
 template <class T, int L, int J, bool Q, bool FAST>
 __global__ __launch_bounds__(kNormBwdThreads<L>) void k_norm_bwd(NormArgs a) {
+#pragma clang fp contract(off)
   constexpr int V = Elem<T>::V, NT = kNormBwdThreads<L>, R = NT / L;
   using In = RowsIn<T>;
   __shared__ float s[NT / kWave];
@@ -191,11 +195,11 @@ __global__ __launch_bounds__(kNormBwdThreads<L>) void k_norm_bwd(NormArgs a) {
       for (int i = 0; i < V; ++i) {
         // columns past the end have dy = 0: x there must not turn them into NaN
         x[j][i] = i < n ? (x[j][i] - m) * rs : 0.0f;
-        dg[j][i] += dy[j][i] * x[j][i];
+        dg[j][i] = fmaf(dy[j][i], x[j][i], dg[j][i]);
         db[j][i] += dy[j][i];
         if (gamma) dy[j][i] *= g[i];
         c0 += dy[j][i];
-        c1 += dy[j][i] * x[j][i];
+        c1 = fmaf(dy[j][i], x[j][i], c1);
       }
     }
     if (FAST || a.dx) {
@@ -205,7 +209,7 @@ __global__ __launch_bounds__(kNormBwdThreads<L>) void k_norm_bwd(NormArgs a) {
       for (int j = 0; j < J; ++j) {
         const int col = (j * L + lane) * V;
 #pragma unroll
-        for (int i = 0; i < V; ++i) dy[j][i] = rs * (dy[j][i] - c0 - x[j][i] * c1);
+        for (int i = 0; i < V; ++i) dy[j][i] = rs * fmaf(-x[j][i], c1, dy[j][i] - c0);
         st_piece<T>(static_cast<T*>(a.dx) + row * a.lddx + col, FAST ? V : cols - col, dy[j], FAST || a.nt);
       }
     }
