@@ -508,6 +508,16 @@ __global__ __launch_bounds__(WPB* kWave, 2) void k_dense_shared(DenseArgs a) {
     rows32_out<J, NC>(a, 0, block * 32, col0, 0, a.red, out[wave], acc);
   }
 }
+// What a product's kernels are called in timings: by tile, and by row walk.
+struct Names {
+  const char *t64, *t128, *t256, *panel, *shared;
+  const char* tile(int b) const { return b == 64 ? t64 : b == 128 ? t128 : t256; }
+};
+constexpr Names kNamesFwd{"dense_fwd_64", "dense_fwd_128", "dense_fwd_256", "dense_fwd_panel", "dense_fwd_shared"};
+constexpr Names kNamesDx{"dense_bwd_dx_64", "dense_bwd_dx_128", "dense_bwd_dx_256", "dense_bwd_dx_panel",
+                         "dense_bwd_dx_shared"};
+constexpr Names kNamesDw{"dense_bwd_dw_64", "dense_bwd_dw_128", "dense_bwd_dw_256", nullptr, nullptr};
+constexpr Names kNamesDb{"dense_bwd_db_64", "dense_bwd_db_128", "dense_bwd_db_256", nullptr, nullptr};
 // Whether a product goes that way: a reduction that fits the registers beside its
 // columns, and rows enough for the waves to walk.
 template <class T>
@@ -517,7 +527,7 @@ bool panel(int64_t rows, int64_t cols, int64_t red) {
   return red <= kPanel<T> && ((rows + 31) / 32) * ((cols + 63) / 64) >= 8192;
 }
 template <class J>
-e3_status dense_panel(DenseArgs a, const char* name, hipStream_t st) {
+e3_status dense_panel(DenseArgs a, const Names& names, hipStream_t st) {
   using T = typename J::T;
   if constexpr (sizeof(T) == 4) {
     // Shared row blocks: four waves, or two where the terms of B are few (more
@@ -531,7 +541,7 @@ e3_status dense_panel(DenseArgs a, const char* name, hipStream_t st) {
       const int64_t col = m.cols / (64 * wpb);
       m.splits = (int)std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 2048 / wpb / col));
       {
-        TimedLaunch t_(name, st);
+        TimedLaunch t_(names.shared, st);
         auto* k = wpb == 2 ? k_dense_shared<J, 32, 2> : a.red <= 32 ? k_dense_shared<J, 32, 4> : k_dense_shared<J, 64, 4>;
         hipLaunchKernelGGL(k, grid_of(m.splits * col), dim3(wpb * kWave), 0, st, m);
         E3_HIP(hipGetLastError());
@@ -541,14 +551,14 @@ e3_status dense_panel(DenseArgs a, const char* name, hipStream_t st) {
       a.b.p = static_cast<const T*>(a.b.p) + (J::FB == kAlong ? m.cols * a.b.ld : m.cols);
       a.y = static_cast<T*>(a.y) + m.cols;
       if (a.bias) a.bias = static_cast<const T*>(a.bias) + m.cols;
-      return dense_panel<J>(a, name, st);
+      return dense_panel<J>(a, names, st);
     }
   }
   // two workgroups per CU, each wave on row blocks of its own
   const int64_t groups = (a.cols + 63) / 64;
   a.splits = (int)std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 2048 / groups));
   const int64_t blocks = (a.splits * groups + 3) / 4;
-  TimedLaunch t_(name, st);
+  TimedLaunch t_(names.panel, st);
   auto go = [&](auto KK) {
     constexpr int kk = decltype(KK)::value;
     const bool fast = a.red == 16 * kk && a.cols % 64 == 0 && Tail<T>::plain(a);
@@ -684,8 +694,8 @@ e3_status dense_join(const DenseArgs& a, hipStream_t st) {
   return E3_OK;
 }
 template <class J>
-e3_status dense_launch(const DenseArgs& a, const Cut& c, const char* name, hipStream_t st) {
-  TimedLaunch t_(name, st);
+e3_status dense_launch(const DenseArgs& a, const Cut& c, const Names& names, hipStream_t st) {
+  TimedLaunch t_(names.tile(c.tile), st);
   const dim3 grid = grid_of(c.tiles * c.splits);
   if constexpr (sizeof(typename J::T) == 2) {
     if (c.tile == 256) {
@@ -704,11 +714,11 @@ e3_status dense_launch(const DenseArgs& a, const Cut& c, const char* name, hipSt
 constexpr e3_dtype dtype_of(const float*) { return E3_F32; }
 constexpr e3_dtype dtype_of(const __bf16*) { return E3_BF16; }
 template <class J>
-e3_status dense_product(DenseArgs a, float* part, const char* name, hipStream_t st) {
+e3_status dense_product(DenseArgs a, float* part, const Names& names, hipStream_t st) {
   const e3_dtype t = dtype_of(static_cast<const typename J::T*>(nullptr));
   const Cut c = dense_cut(t, a.rows, a.cols, a.red, kForward);
   set_cut(a, c, part);
-  const e3_status s = dense_launch<J>(a, c, name, st);
+  const e3_status s = dense_launch<J>(a, c, names, st);
   return s != E3_OK || c.splits == 1 ? s : dense_join<typename J::T>(a, st);
 }
 

@@ -205,8 +205,8 @@ e3_status dense_fwd(const DenseArgs& a, float* part, hipStream_t st) {
     return a.red <= 8 ? with(std::integral_constant<int, 8>{}) : with(std::integral_constant<int, kThin>{});
   }
   using J = Job<T, kAlong, kAcross, kFull, kFull, false>;
-  if (panel<T>(a.rows, a.cols, a.red)) return dense_panel<J>(a, "dense_fwd", st);
-  return dense_product<J>(a, part, "dense_fwd", st);
+  if (panel<T>(a.rows, a.cols, a.red)) return dense_panel<J>(a, kNamesFwd, st);
+  return dense_product<J>(a, part, kNamesFwd, st);
 }
 
 bool good_dims(e3_dtype t, int64_t M, int64_t K, int64_t N) {

@@ -119,12 +119,12 @@ e3_status dense_bwd_products(DenseArgs x, DenseArgs w, float* part, hipStream_t 
     hipLaunchKernelGGL((k_dense_two<JX, JW, 64>), grid_of(first + cw.tiles * cw.splits), dim3(256), 0, st, x, w, first);
     E3_HIP(hipGetLastError());
   } else {
-    if (dx) s = along ? dense_panel<JX>(x, "dense_bwd_dx", st) : dense_launch<JX>(x, cx, "dense_bwd_dx", st);
-    if (s == E3_OK && dw) s = dense_launch<JW>(w, cw, "dense_bwd_dw", st);
+    if (dx) s = along ? dense_panel<JX>(x, kNamesDx, st) : dense_launch<JX>(x, cx, kNamesDx, st);
+    if (s == E3_OK && dw) s = dense_launch<JW>(w, cw, kNamesDw, st);
   }
   if constexpr (FLY && KX == kFull) {
     if (s == E3_OK && db && !dw) {
-      TimedLaunch t_("dense_bwd_db", st);
+      TimedLaunch t_(kNamesDb.tile(cw.tile), st);
       const dim3 grid = grid_of((w.cols + cw.tile - 1) / cw.tile * (int64_t)cw.splits);
       auto go = [&](auto B) {
         constexpr int b = decltype(B)::value;

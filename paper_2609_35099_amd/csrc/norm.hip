@@ -389,15 +389,15 @@ e3_status norm_bwd(const NormArgs& a, hipStream_t st) {
   return norm_shape<T>(a.cols, [&](auto L, auto J) -> e3_status {
     constexpr int l = decltype(L)::value, j = decltype(J)::value;
     if constexpr (j > 0) {
-      TimedLaunch t_("layer_norm_bwd", st);
       const bool fast = a.dx && a.nt && a.cols == l * j * Elem<T>::V;
+      TimedLaunch t_(fast ? "layer_norm_bwd_stream" : "layer_norm_bwd", st);
       auto* k = a.x ? (fast ? k_norm_bwd<T, l, j, false, true> : k_norm_bwd<T, l, j, false, false>)
                     : (fast ? k_norm_bwd<T, l, j, true, true> : k_norm_bwd<T, l, j, true, false>);
       hipLaunchKernelGGL(k, dim3(a.blocks), dim3(kNormBwdThreads<l>), 0, st, a);
       E3_HIP(hipGetLastError());
     } else {
       if (a.dx) {
-        TimedLaunch t_("layer_norm_bwd", st);
+        TimedLaunch t_("layer_norm_bwd_wide", st);
         hipLaunchKernelGGL((k_norm_bwd_wide<T>), grid_of(a.rows), dim3(kNormThreads), 0, st, a);
         E3_HIP(hipGetLastError());
       }
