@@ -400,7 +400,8 @@ e3_status e3_unpack8(e3_dtype dtype, const int8_t* q, const uint8_t* c, void* x,
  *   y = (x - mean) rstd gamma + beta,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
  * gamma, beta [cols] (NULL: 1, 0); eps >= 0.  Optional outputs (NULL: not
  * stored): mean, rstd [rows] float32, which the backward takes; xq, xc: x in 8
- * bits; yq, yc: y as stored, in 8 bits. */
+ * bits; yq, yc: y as stored, in 8 bits.  y does not suffer from the mean's rounding
+ * to float32; the backward's (x - mean) rstd does, by up to 2^-24 |mean| rstd. */
 e3_status e3_layer_norm_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* gamma, const void* beta, float eps,
                             void* y, int64_t ldy, float* mean, float* rstd, int8_t* xq, uint8_t* xc, int8_t* yq,
                             uint8_t* yc, int64_t rows, int64_t cols, e3_stream stream);

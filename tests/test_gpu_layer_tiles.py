@@ -290,3 +290,18 @@ def test_checkpoints_past_the_caches(e3, dt, rows, cols):  # noqa: F811
     e3.unpack8(p, out=out)
     assert untouched() and torch.equal(out.double(), values(e3, p))
     assert torch.equal(e3.unpack8(p, out.dtype), out)
+
+
+@pytest.mark.parametrize("cols", [7, 32, 64, 100, 256, 515, 700, 1025, 2049, 4100, 8192, 20000])
+def test_layer_norm_of_a_large_mean(e3, cols):  # noqa: F811
+    """A mean 3,000 times the deviation: as a float32 it is off by up to 1e-4 deviations, which may not reach
+    y.  x less any float32 near its mean is exact, so what is left is the rounding of sums of deviations:
+    the bar of other inputs."""
+    import torch
+    x = (normal(40, cols, seed=cols) + 3000 * torch.linspace(1, 2, 40, device="cuda")[:, None]).contiguous()
+    print("[case] layer norm, large mean", cols, flush=True)
+    y, mean, rstd = e3.layer_norm_fwd(x, keep=("stats",))
+    d = x.double() - x.double().mean(1, keepdim=True)
+    r = 1 / torch.sqrt((d * d).mean(1) + 1e-5)
+    assert off(y, d * r[:, None]) < TOL["float32"]
+    assert off(mean, x.double().mean(1)) < 6e-8 and off(rstd, r) < 1e-6      # the mean: one rounding
