@@ -810,6 +810,7 @@ def unpack8(p: Packed8, dtype=None, out=None, stream=None):
 
 
 def _keep_of(keep, allowed):
+    keep = tuple(keep)
     for k in keep:
         if k not in allowed:
             raise ValueError(f"keep: {k!r} is none of {', '.join(allowed)}")
@@ -825,7 +826,7 @@ def layer_norm_fwd(x, gamma=None, beta=None, eps: float = 1e-5, keep=(), out=Non
     """
     code, dt = _layer_dtype(x, "x")
     m, n = shape = _matrix(x, "x")
-    _keep_of(keep, ("stats", "x8", "y8"))
+    keep = _keep_of(keep, ("stats", "x8", "y8"))
     y = x.new_empty(shape) if out is None else out
     got, mean, rstd, xp, yp = [y], None, None, (None, None), (None, None)
     if "stats" in keep:
@@ -860,7 +861,7 @@ def layer_norm_bwd(x, gamma, dy, mean, rstd, want=("dx", "dgamma", "dbeta"), dx=
     cotangents not in `want` are not computed (None).  gamma may be None (ones)."""
     code, dt = _layer_dtype(dy, "dy")
     m, n = shape = _matrix(dy, "dy")
-    _keep_of(want, ("dx", "dgamma", "dbeta"))
+    want = _keep_of(want, ("dx", "dgamma", "dbeta"))
     if "dx" in want and dx is None:
         dx = dy.new_empty(shape)
     dg = dy.new_empty((n,)) if "dgamma" in want else None
@@ -905,7 +906,7 @@ def dense_fwd(x, W, bias=None, res=None, act: str = "none", keep=(), out=None, w
     if _matrix(W, "W")[0] != K:
         raise ValueError(f"W has shape {tuple(W.shape)}, expected {K} rows")
     N = W.shape[1]
-    _keep_of(keep, ("z", "z8", "y8"))
+    keep = _keep_of(keep, ("z", "z8", "y8"))
     shape = (M, N)
     y = x.new_empty(shape) if out is None else out
     got, z, zp, yp = [y], None, (None, None), (None, None)
@@ -938,7 +939,7 @@ def dense_bwd(x, W, dy, z=None, act: str = "none", want=("dx", "dW", "db"), dx=N
     if _matrix(W, "W")[1] != N:
         raise ValueError(f"W has shape {tuple(W.shape)}, expected {N} columns")
     K = W.shape[0]
-    _keep_of(want, ("dx", "dW", "db"))
+    want = _keep_of(want, ("dx", "dW", "db"))
     if "dx" in want and dx is None:
         dx = dy.new_empty((M, K))
     dW = dy.new_empty((K, N)) if "dW" in want else None
