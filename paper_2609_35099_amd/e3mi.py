@@ -783,6 +783,19 @@ def _matrix(t, name):
     return shape
 
 
+def _scratch(ws):
+    """(pointer, bytes) of a workspace, the caller's or a call's own; None: none."""
+    if ws is None:
+        return None, 0
+    if not isinstance(ws, _torch().Tensor):
+        raise TypeError("ws must be a torch tensor")
+    if not ws.is_cuda:
+        raise ValueError("ws must be on the GPU")
+    if not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 @_on_stream
 def pack8(x, out=None, stream=None) -> Packed8:
     """x [rows, cols] (float32 or bfloat16) in 8 bits."""
@@ -873,8 +886,7 @@ def layer_norm_bwd(x, gamma, dy, mean, rstd, want=("dx", "dgamma", "dbeta"), dx=
                                    *_rows(dy, "dy", shape, dt), _ptr(mean, "mean", (m,)), _ptr(rstd, "rstd", (m,)),
                                    *((None, n) if dx is None else _rows(dx, "dx", shape, dt)),
                                    None if dg is None else dg.data_ptr(), None if db is None else db.data_ptr(),
-                                   None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), m, n,
-                                   _stream(stream)), "e3_layer_norm_bwd")
+                                   *_scratch(ws), m, n, _stream(stream)), "e3_layer_norm_bwd")
     return dx, dg, db
 
 
@@ -925,8 +937,8 @@ def dense_fwd(x, W, bias=None, res=None, act: str = "none", keep=(), out=None, w
     _check(lib().e3_dense_fwd(code, *_rows(x, "x", (M, K), dt), _ptr(W, "W", (K, N), dt),
                               None if bias is None else _ptr(bias, "bias", (N,), dt),
                               *((None, N) if res is None else _rows(res, "res", shape, dt)), _act_code(act),
-                              *_rows(y, "out", shape, dt), z, N, *zp, *yp, None if ws is None else ws.data_ptr(),
-                              0 if ws is None else ws.numel(), M, K, N, _stream(stream)), "e3_dense_fwd")
+                              *_rows(y, "out", shape, dt), z, N, *zp, *yp, *_scratch(ws), M, K, N, _stream(stream)),
+           "e3_dense_fwd")
     return tuple(got) if keep else y
 
 
@@ -951,7 +963,7 @@ def dense_bwd(x, W, dy, z=None, act: str = "none", want=("dx", "dW", "db"), dx=N
     _check(lib().e3_dense_bwd(code, xp, ldx, xq, xc, _ptr(W, "W", (K, N), dt), zp, ldz, zq, zc, _act_code(act),
                               *_rows(dy, "dy", shape, dt), *((None, K) if dx is None else _rows(dx, "dx", (M, K), dt)),
                               None if dW is None else dW.data_ptr(), None if db is None else db.data_ptr(),
-                              ws.data_ptr(), ws.numel(), M, K, N, _stream(stream)), "e3_dense_bwd")
+                              *_scratch(ws), M, K, N, _stream(stream)), "e3_dense_bwd")
     return dx, dW, db
 
 
