@@ -91,3 +91,48 @@ def test_dense_refusals(L):
     if b.value:
         assert bwd(nb=b.value - 1) == SMALL
         assert bwd(ws=None) == INVALID
+
+
+def _sizes(L, *args):
+    f, b = ct.c_size_t(), ct.c_size_t()
+    assert L.e3_dense_workspace_size(*args, ct.byref(f), ct.byref(b)) == OK
+    return f.value, b.value
+
+
+@pytest.mark.parametrize("dtype,M,K,N", [(F32, 16, 1000, 500), (BF16, 16, 1000, 500), (F32, 300, 4100, 300), (BF16, 3001, 4099, 2051)])
+def test_dense_forward_scratch_refusals(L, dtype, M, K, N):
+    """Sizes whose reduction is split: less scratch than asked for, none, or misaligned."""
+    need = _sizes(L, dtype, M, K, N)[0]
+    assert need >= 2 * M * N * 4                    # two splits at least
+
+    def fwd(ws, nb):
+        return L.e3_dense_fwd(dtype, P, K, P, None, None, N, 0, P, N, None, N, None, None, None, None, ws, nb, M, K, N, None)
+    assert fwd(P, need - 1) == SMALL and fwd(P, 0) == SMALL and fwd(None, 0) == SMALL
+    for ws in (None, ODD, HALF):
+        assert fwd(ws, need) == INVALID, ws
+
+
+@pytest.mark.parametrize("dtype,M,K,N", [(F32, 64, 300, 40), (BF16, 64, 300, 40), (F32, 5000, 64, 64), (BF16, 40000, 128, 256)])
+def test_dense_backward_scratch_refusals(L, dtype, M, K, N):
+    """Sizes that write dz (K = 300) or split the sum over rows."""
+    need = _sizes(L, dtype, M, K, N)[1]
+    assert need > 0
+
+    def bwd(ws, nb):
+        return L.e3_dense_bwd(dtype, P, K, None, None, P, P, N, None, None, 2, P, N, P, K, P, P, ws, nb, M, K, N, None)
+    assert bwd(P, need - 1) == SMALL and bwd(P, 0) == SMALL and bwd(None, 0) == SMALL
+    for ws in (None, ODD, HALF, ct.c_void_p(4096 + 8)):       # 16-byte alignment
+        assert bwd(ws, need) == INVALID, ws
+
+
+def test_dense_scratch_stays_near_the_tensors(L):
+    """No size asks for more than a small multiple of what it works on: 256 splits are taken only where the
+    outputs are few, dz is as large as dy."""
+    for dtype, e in ((F32, 4), (BF16, 2)):
+        for M in (1, 9, 100, 4097, 1_000_003):
+            for K in (1, 17, 300, 4099, 1 << 20):
+                for N in (1, 8, 65, 1027, 1 << 20):
+                    f, b = _sizes(L, dtype, M, K, N)
+                    tensors = e * (M * K + K * N + M * N)
+                    assert f <= 16 * tensors + (64 << 20), (dtype, M, K, N, f)
+                    assert b <= 16 * tensors + (64 << 20), (dtype, M, K, N, b)
