@@ -658,11 +658,23 @@ void set_cut(DenseArgs& a, const Cut& c, float* part, int64_t tail = 0) {
   a.chunk = c.chunk, a.splits = c.splits, a.part = c.splits > 1 ? part : nullptr, a.pitch = a.rows * a.cols + tail;
 }
 
-// The products of the backward form dz from dy and z on the way to LDS: once per
-// 128 columns of x, so up to this many; wider layers write dz once.  (Two rounds
-// of an activation's derivative cost less than dz's way to memory and back:
-// 100,003 x 128 x 256 float32 from 8 bits, 144 us against 162.)
+// Whether the products of the backward form dz from dy and z on the way to LDS:
+// once per 128 columns of x, so for up to 256; wider layers write dz once.  Formed
+// against written, silu, us: 60,003 x 64 x 256 float32 61 against 84, from 8 bits 56
+// against 72; x 256 x 1,024 560 against 612, 484 against 521; bfloat16 x 64 x 256 36
+// against 46, from 8 bits 38 against 45; x 256 x 256 82 against 86; x 256 x 1,024 201
+// against 224.  bfloat16 from 8 bits past 128 columns unpacks, differentiates and
+// rounds for every tile with too few registers for it in the largest: 60,003 x 256 x
+// 256 155 against 83, x 1,024 549 against 208 (120,011 rows 1,688 against 351), and
+// in the smaller ones 20,011 x 192 x 256 47 against 45, x 1,024 104 against 87; but
+// few columns of dz cost little (45,011 x 192 x 64 45 against 51), and small layers
+// save a launch (10,007 x 192 x 128 29 against 31, 3,000 x 200 x 300 22 against 29).
 constexpr int64_t kOnTheFly = 256;
+bool forms_dz(e3_dtype t, int64_t M, int64_t K, int64_t N, bool packed) {
+  if (K > kOnTheFly) return false;
+  if (!packed || t != E3_BF16 || K <= 128) return true;
+  return (N <= 64 || M * N < (1 << 21)) && dense_cut(t, M, K, N, kDx).tile < 256;
+}
 
 struct DenseBwdWs {
   size_t dz, db, part, total;
@@ -671,7 +683,7 @@ struct DenseBwdWs {
 DenseBwdWs dense_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   const size_t e = t == E3_F32 ? 4 : 2;
   DenseBwdWs w{};
-  if (K > kOnTheFly) {
+  if (!forms_dz(t, M, K, N, true)) {  // from z in full or packed
     w.db_blocks = std::max<int64_t>(1, std::min<int64_t>(512, (M + 63) / 64));
     w.db_rows = (M + w.db_blocks - 1) / w.db_blocks;
     w.dz = up256(M * N * e);
@@ -697,7 +709,9 @@ template <class J>
 e3_status dense_launch(const DenseArgs& a, const Cut& c, const Names& names, hipStream_t st) {
   TimedLaunch t_(names.tile(c.tile), st);
   const dim3 grid = grid_of(c.tiles * c.splits);
-  if constexpr (sizeof(typename J::T) == 2) {
+  // (packed gradient operands never get there: forms_dz; dW takes such tiles past
+  // 128 columns of dz and 1e8 values of it)
+  if constexpr (sizeof(typename J::T) == 2 && J::KA != kGradPacked && J::KB != kGradPacked) {
     if (c.tile == 256) {
       hipLaunchKernelGGL((k_dense<J, 256>), grid, dim3(TileOf<J, 256>::THREADS), 0, st, a);
       E3_HIP(hipGetLastError());

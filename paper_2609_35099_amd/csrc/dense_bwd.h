@@ -29,7 +29,7 @@ __global__ __launch_bounds__((TileOf<J, B>::THREADS), 2) void k_dense_two(DenseA
 // dz = dy act'(z) in the type of dy (a bfloat16 dz is an operand of the matrix
 // instructions, which take no more bits), and the column sums of its unrounded
 // values over the block's rows, for layers whose products would form dz too often
-// themselves (kOnTheFly).  Either output may be null.
+// themselves (forms_dz).  Either output may be null.
 template <class T>
 __global__ __launch_bounds__(256) void k_dense_dz(RowsIn<T> z, int act, const T* dy, int64_t lddy, T* dz, float* part,
                                                   int64_t rows, int cols, int64_t per) {
@@ -132,7 +132,7 @@ e3_status dense_bwd_products(DenseArgs x, DenseArgs w, float* part, hipStream_t 
       };
       if (cw.tile == 64) go(std::integral_constant<int, 64>{});
       else if (cw.tile == 128) go(std::integral_constant<int, 128>{});
-      else if constexpr (sizeof(T) == 2) go(std::integral_constant<int, 256>{});
+      else if constexpr (sizeof(T) == 2 && KD != kGradPacked) go(std::integral_constant<int, 256>{});
       E3_HIP(hipGetLastError());
     }
   }
@@ -158,7 +158,7 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
     return E3_OK;
   }
   const DenseBwdWs w = dense_bwd_ws(t, M, K, N);
-  const bool fly = K <= kOnTheFly;
+  const bool fly = forms_dz(t, M, K, N, act != E3_ACT_NONE && z.q);
   T* dz = reinterpret_cast<T*>(ws);
   float* dbp = reinterpret_cast<float*>(ws + w.dz);
   float* part = reinterpret_cast<float*>(ws + w.dz + w.db);
