@@ -15,9 +15,9 @@
 // float32 rows take up to 4% longer (20,000 x 1,024 29.2 us without, 30.3 with).
 // bfloat16 rows go without: their values have 8 bits, so where the mean is 256
 // times the deviation (m off by 1e-4 of it, y's last bit 4e-3) little else is left
-// of them.  The backward takes the mean as float32, whose rounding shifts its n.  L lanes share a row, J 16-byte pieces each; narrow rows take part
-// of a wave, wide ones a workgroup, and rows past the registers are read again
-// for each pass.
+// of them.  The backward takes the mean as float32, whose rounding shifts its n.
+// L lanes share a row, J 16-byte pieces each; narrow rows take part of a wave, wide
+// ones a workgroup, and rows past the registers are read again for each pass.
 //
 // One MI355X, 65,536 x 1,024 bfloat16: forward with statistics and x in 8 bits 76
 // us (4.4 TB/s), backward from x in 8 bits 60 us (5.6 TB/s) and 7 for the weight
@@ -378,8 +378,11 @@ __global__ __launch_bounds__(256) void k_unpack8(const int8_t* q, const uint8_t*
 
 // ------------------------------------------------------------ host
 // The narrowest arrangement that holds a row: lanes per row and pieces per
-// lane; J = 0 past the registers.
-template <class T, class F>
+// lane; J = 0 past the registers.  The backward's are full past two pieces of
+// bfloat16 in 512 lanes: four spilled 1 KB a lane, and reading the row again is
+// faster (2,003 x 10,001 92 us against 209, 2,003 x 16,384 130 against 175, from 8
+// bits 114 against 191); the forward's hold (2,003 x 16,384 29 against 39).
+template <class T, bool BWD, class F>
 auto norm_shape(int cols, F&& f) {
   constexpr int V = Elem<T>::V;
   const int pieces = (cols + V - 1) / V;
@@ -394,7 +397,7 @@ auto norm_shape(int cols, F&& f) {
   E3_SHAPE(256, 2);
   E3_SHAPE(256, 3);
   E3_SHAPE(512, 2);
-  E3_SHAPE(512, 4);
+  if constexpr (!BWD || V == 4) E3_SHAPE(512, 4);
 #undef E3_SHAPE
   return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 0>{});
 }
@@ -405,12 +408,12 @@ int norm_blocks(e3_dtype t, int64_t rows, int cols) {
     constexpr int l = decltype(L)::value, R = decltype(J)::value > 0 ? kNormBwdThreads<l> / l : 1;
     return (int)std::max<int64_t>(1, std::min<int64_t>(512, (rows + R - 1) / R));
   };
-  return t == E3_F32 ? norm_shape<float>(cols, of) : norm_shape<__bf16>(cols, of);
+  return t == E3_F32 ? norm_shape<float, true>(cols, of) : norm_shape<__bf16, true>(cols, of);
 }
 
 template <class T>
 e3_status norm_fwd(const NormArgs& a, hipStream_t st) {
-  return norm_shape<T>(a.cols, [&](auto L, auto J) -> e3_status {
+  return norm_shape<T, false>(a.cols, [&](auto L, auto J) -> e3_status {
     constexpr int l = decltype(L)::value, j = decltype(J)::value, R = kNormFwdThreads<l> / l;
     TimedLaunch t_("layer_norm_fwd", st);
     hipLaunchKernelGGL((k_norm_fwd<T, l, j>), grid_of((a.rows + R - 1) / R), dim3(kNormFwdThreads<l>), 0, st, a);
@@ -421,7 +424,7 @@ e3_status norm_fwd(const NormArgs& a, hipStream_t st) {
 
 template <class T>
 e3_status norm_bwd(const NormArgs& a, hipStream_t st) {
-  return norm_shape<T>(a.cols, [&](auto L, auto J) -> e3_status {
+  return norm_shape<T, true>(a.cols, [&](auto L, auto J) -> e3_status {
     constexpr int l = decltype(L)::value, j = decltype(J)::value;
     if constexpr (j > 0) {
       const bool fast = a.dx && a.nt && a.cols == l * j * Elem<T>::V;

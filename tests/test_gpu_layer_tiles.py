@@ -237,7 +237,8 @@ def test_float32_tiles_fall_back_for_large_operands(e3, M, K, N):  # noqa: F811
 # at widths that fill the registers' pieces exactly ("layer_norm_bwd_stream": loads and stores without
 # branches) and that do not, and rows past the registers
 NORM = [("bfloat16", 20001, 1024, 0, "layer_norm_bwd_stream"), ("bfloat16", 300001, 64, 0, "layer_norm_bwd_stream"),
-        ("bfloat16", 5001, 4096, 8, "layer_norm_bwd_stream"), ("bfloat16", 2003, 16384, 0, "layer_norm_bwd_stream"),
+        ("bfloat16", 5001, 4096, 8, "layer_norm_bwd_stream"), ("bfloat16", 2003, 16384, 0, "layer_norm_bwd_wide"),
+        ("bfloat16", 2503, 8192, 0, "layer_norm_bwd_stream"), ("bfloat16", 2003, 10001, 2, "layer_norm_bwd_wide"),
         ("bfloat16", 40001, 515, 3, "layer_norm_bwd"), ("bfloat16", 1100, 16390, 0, "layer_norm_bwd_wide"),
         ("float32", 70003, 128, 4, "layer_norm_bwd_stream"), ("float32", 9001, 1024, 0, "layer_norm_bwd_stream"),
         ("float32", 2501, 4096, 0, "layer_norm_bwd_stream"), ("float32", 2003, 8192, 0, "layer_norm_bwd_stream"),
