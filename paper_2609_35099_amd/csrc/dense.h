@@ -692,7 +692,8 @@ DenseBwdWs dense_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   // the partial sums of both products, side by side: one launch may make both
   const size_t dx = cut_bytes(dense_cut(t, M, K, N, kDx), M, K), dw = cut_bytes(dense_cut(t, K, N, M, kDw), K, N, N);
   w.part = dx + dw;
-  w.total = M == 0 ? 0 : w.dz + w.db + w.part;
+  // behind them, a W shorter than a piece
+  w.total = M == 0 ? 0 : w.dz + w.db + w.part + (K * N * e < 16 ? 256 : 0);
   return w;
 }
 

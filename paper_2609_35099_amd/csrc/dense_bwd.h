@@ -65,9 +65,8 @@ __global__ __launch_bounds__(256) void k_dense_dz(RowsIn<T> z, int act, const T*
   }
 }
 
-// Layers of which a matrix is shorter than a piece: a wave per value of dx, dW and
-// db, whose lanes take every 64th term.  (One row or column, or nearly; a long
-// reduction is slow here.)
+// Layers of which a matrix is shorter than a piece, and not many rows: a wave per
+// value of dx, dW and db, whose lanes take every 64th term.
 template <class T>
 __global__ __launch_bounds__(256) void k_dense_bwd_tiny(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy,
                                                         int64_t lddy, T* dx, int64_t lddx, T* dW, T* db, int64_t M,
@@ -98,6 +97,13 @@ __global__ __launch_bounds__(256) void k_dense_bwd_tiny(RowsIn<T> x, const T* W,
   }
   v = sum_lanes<kWave>(v);
   if (l == 0) *out = (T)v;
+}
+
+// A W shorter than a piece, so that whole pieces can be read.
+template <class T>
+__global__ __launch_bounds__(kWave) void k_dense_short(const T* W, int n, T* out) {
+  const int i = threadIdx.x;
+  if (i < Elem<T>::V) out[i] = i < n ? W[i] : (T)0.0f;
 }
 
 // ------------------------------------------------------------ host
@@ -149,7 +155,11 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
                     T* db, char* ws, int64_t M, int64_t K, int64_t N, hipStream_t st) {
   constexpr e3_dtype t = std::is_same_v<T, float> ? E3_F32 : E3_BF16;
   constexpr int V = Elem<T>::V;
-  if (M * N < V || M * K < V || K * N < V) {  // a matrix may be shorter than a piece
+  // x or dy shorter than a piece; a short W (copied to a whole piece below) where its
+  // launches would cost more than the wave's long sums: float32 silu, in one launch
+  // against tiles, us: 300 x 1 x 3 15 against 20, 6,000 20 and 20, 10,003 32 against
+  // 20, 1,000,003 5,410 against 235.
+  if (M * N < V || M * K < V || (K * N < V && M <= 4096)) {
     TimedLaunch t_("dense_bwd_tiny", st);
     const int64_t outs = M * K + K * N + N;
     hipLaunchKernelGGL(k_dense_bwd_tiny<T>, grid_of((outs + 3) / 4), dim3(256), 0, st, x, W, z, act, dy, lddy, dx, lddx,
@@ -174,11 +184,19 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
     const e3_status s = column_sums(t, dbp, (int)w.db_blocks, N, N, N, db, nullptr, st);
     if (s != E3_OK) return s;
   }
+  int64_t total = K * N;
+  if (dx && total < V) {
+    TimedLaunch t_("dense_short", st);
+    T* copy = reinterpret_cast<T*>(ws + w.dz + w.db + w.part);
+    hipLaunchKernelGGL(k_dense_short<T>, dim3(1), dim3(kWave), 0, st, W, (int)total, copy);
+    E3_HIP(hipGetLastError());
+    W = copy, total = V;
+  }
   DenseArgs ax{}, aw{};
   const int64_t ldd = own ? N : lddy, ldz = z.x ? z.ld : N, ldx = x.x ? x.ld : K;
   const Side d{own ? dz : dy, ldd, nullptr, nullptr, 0, (M - 1) * ldd + N};
   const Side pre{z.x, ldz, z.q, z.c, (N + kGroup - 1) / kGroup, (M - 1) * ldz + N};
-  ax.a = d, ax.b = {W, N, nullptr, nullptr, 0, K * N}, ax.pre = pre, ax.grad_act = act, ax.rows = M, ax.cols = (int)K, ax.red = N;
+  ax.a = d, ax.b = {W, N, nullptr, nullptr, 0, total}, ax.pre = pre, ax.grad_act = act, ax.rows = M, ax.cols = (int)K, ax.red = N;
   ax.y = dx, ax.ldy = lddx, ax.nt = streams(t, M, K);
   aw.a = {x.x, ldx, x.q, x.c, (K + kGroup - 1) / kGroup, (M - 1) * ldx + K}, aw.b = d, aw.pre = pre, aw.grad_act = act;
   aw.rows = K, aw.cols = (int)N, aw.red = M, aw.y = dW, aw.ldy = N, aw.sums = fly ? db : nullptr;

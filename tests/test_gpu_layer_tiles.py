@@ -333,3 +333,32 @@ def test_layer_norm_of_a_large_mean(e3, cols):  # noqa: F811
     r = 1 / torch.sqrt((d * d).mean(1) + 1e-5)
     assert off(y, d * r[:, None]) < TOL["float32"]
     assert off(mean, x.double().mean(1)) < 6e-8 and off(rstd, r) < 1e-6      # the mean: one rounding
+
+
+# W shorter than a load's 16 bytes (a layer of one or two columns to a few): few rows, many, ragged
+@pytest.mark.parametrize("dt", ["float32", "bfloat16"])
+@pytest.mark.parametrize("M,K,N,gap", [(9, 1, 1, 0), (40, 1, 3, 2), (1003, 3, 1, 0), (20011, 1, 2, 1), (300001, 1, 3, 0), (270001, 3, 1, 5)])
+@pytest.mark.parametrize("ckpt", [False, True])
+def test_dense_backward_of_a_short_matrix(e3, dt, M, K, N, gap, ckpt):  # noqa: F811
+    """The sums over many rows go through tiles and splits as those of wider layers do (a wave for each took
+    5 ms for a million rows).  A bfloat16 value is off by half a step, 2^-8 of it, at most."""
+    import torch
+    bar = 2e-6 if dt == "float32" else 1.001 * 2**-8
+    xd, Wd = rows_of(normal(M, K, seed=1) + 0.2, dt, gap), dev(normal(K, N, seed=2).cpu(), dt)
+    dyd, zd = rows_of(1e-3 * normal(M, N, seed=3), dt, gap), rows_of(normal(M, N, seed=4), dt, gap)
+    xin, zin = (e3.pack8(xd), e3.pack8(zd)) if ckpt else (xd, zd)
+    xr, zr, Wr, dyr = values(e3, xin), values(e3, zin), Wd.double(), dyd.double()
+    for act in ("none", "gelu"):
+        print("[case] dense_bwd, short W", dt, M, K, N, gap, ckpt, act, flush=True)
+        z = None if act == "none" else zin
+        dx, untouched = out_like((M, K), dt, gap, 1 if gap else 0)
+        got, names = ran(e3, lambda: e3.dense_bwd(xin, Wd, dyd, z, act=act, dx=dx))
+        assert ("dense_bwd_tiny" in names) == (M < 5000) and untouched()
+        dz = dyr if act == "none" else dyr * gelu_slope(zr)
+        dzr = rounded(dz, dt)
+        assert off(dx, rounded(dzr @ Wr.t().contiguous(), dt)) < TOL_BWD[dt]
+        for g, w, terms in ((got[1], xr.t().contiguous() @ dzr, (xr**2).t().contiguous() @ dzr**2), (got[2], dz.sum(0), (dz**2).sum(0))):
+            assert bool(((g.double() - w).abs() <= bar * (w.abs() + terms.sqrt())).all())
+        for k, w in enumerate(("dx", "dW", "db")):
+            one = e3.dense_bwd(xin if w == "dW" else None, Wd, dyd, z, act=act, want=(w,))
+            assert torch.equal(one[k], got[k]), (act, w)
