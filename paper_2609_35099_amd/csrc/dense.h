@@ -532,9 +532,15 @@ e3_status dense_panel(DenseArgs a, const Names& names, hipStream_t st) {
   if constexpr (sizeof(T) == 4) {
     // Shared row blocks: four waves, or two where the terms of B are few (more
     // would leave them without registers for two workgroups per CU); the columns
-    // past the last 256 in a launch of their own.
-    const int64_t four = a.cols / 256 * 256;
-    const int wpb = four == a.cols || (a.red > 32 && four > 0) ? 4 : a.red <= 32 && a.cols % 128 == 0 ? 2 : 0;
+    // past the last 256 in a launch of their own, which pays where there are many
+    // before them, or where the kernel above would run its loop with branches and
+    // they are not a few alone.  156,000 rows, in two launches against all above, us:
+    // x 64 x 320 88 against 75, x 576 118 against 115, x 832 153 against 160, x 1,664
+    // 266 against 304; x 40 x 300 109 against 89, x 320 84 against 88, x 640 127
+    // against 158.
+    const int64_t four = a.cols / 256 * 256, rest = a.cols - four;
+    const bool two = four > 0 && (a.red % 16 == 0 && a.cols % 64 == 0 ? four >= 768 : rest >= 64);
+    const int wpb = rest == 0 || (a.red > 32 && two) ? 4 : a.red <= 32 && a.cols % 128 == 0 ? 2 : 0;
     if (Tail<T>::plain(a) && wpb) {
       DenseArgs m = a;
       if (wpb == 4) m.cols = (int)four;

@@ -175,6 +175,21 @@ def test_dense_backward_tiles(e3, dt, M, K, N, gap, names, ckpt):  # noqa: F811
             assert torch.equal(one[k], got[k]), (act, w)
 
 
+@pytest.mark.parametrize("K,N,names", [(64, 320, {"dense_fwd_panel"}), (64, 832, {"dense_fwd_shared", "dense_fwd_panel"}),
+                                       (40, 300, {"dense_fwd_panel"}), (40, 400, {"dense_fwd_shared", "dense_fwd_panel"}),
+                                       (64, 512, {"dense_fwd_shared"}), (32, 384, {"dense_fwd_shared"}),
+                                       (32, 320, {"dense_fwd_panel"})])
+def test_columns_past_the_shared_ones(e3, K, N, names):  # noqa: F811
+    """Row blocks shared by four waves, and a second launch for the columns past the last 256 where that pays."""
+    import torch
+    xd, Wd, bd = normal(100003, K, seed=1), normal(K, N, seed=2) / K**0.5, normal(N, seed=3)
+    print("[case] dense_fwd, shared row blocks", K, N, flush=True)
+    y, launched = ran(e3, lambda: e3.dense_fwd(xd, Wd, bd, act="silu"))
+    assert launched == names
+    assert off(y, silu(xd.double() @ Wd.double() + bd.double())[0]) < TOL["float32"]
+    assert torch.equal(e3.dense_fwd(xd, Wd, bd, act="silu", keep=("z8",))[0], y)
+
+
 @pytest.mark.parametrize("dt,M,K,N,ckpt,once", [("bfloat16", 50021, 250, 1021, True, True), ("bfloat16", 50021, 250, 1021, False, False),
                                                 ("bfloat16", 8001, 200, 300, True, True), ("bfloat16", 3001, 200, 300, True, False), ("bfloat16", 60003, 160, 64, True, True),
                                                 ("bfloat16", 45011, 192, 64, True, False), ("bfloat16", 50021, 128, 1021, True, False),
@@ -203,7 +218,7 @@ def test_dz_is_written_where_forming_it_is_slow(e3, dt, M, K, N, ckpt, once):  #
                                            ("float32", 262149, 64, 64, "dense_fwd_panel"),
                                            ("bfloat16", 262149, 128, 64, "dense_fwd_panel"),
                                            ("float32", 70001, 32, 256, "dense_fwd_shared"),
-                                           ("float32", 70001, 64, 320, "dense_fwd_shared"),
+                                           ("float32", 70001, 64, 832, "dense_fwd_shared"),
                                            ("bfloat16", 45057, 250, 2051, "dense_fwd_256"),
                                            ("float32", 40003, 130, 256, "dense_fwd_128")])
 def test_outputs_beside_y_do_not_change_it(e3, dt, M, K, N, name):  # noqa: F811
