@@ -183,21 +183,23 @@ __device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_
   __builtin_amdgcn_wave_barrier();
 }
 
-// Tiles by type and size; what a library product reaches is 1,070 TFLOP/s in
-// bfloat16 and 143 in float32 (16,384 x 1,024 x 4,096).
+// Tiles by type and size, with us per call in turn with the other side.
 //   bfloat16, 256 x 256: 16 waves of 64 x 64, steps of 32, two buffers, one
-//     workgroup per CU: 1,083 (dx), 1,056 TFLOP/s (dW); 8 waves of 128 x 64 940,
-//     1,019.  The forward takes 256 x 128 by 8 waves, two workgroups per CU, so that
-//     one's activations run beside the other's product (902 for the bare product,
-//     942 with 256 x 256; with gelu and z in 8 bits 244 us against 261).
+//     workgroup per CU: 16,384 x 1,024 x 4,096 dx 142, dW 149 (the library's products
+//     100, 166).  The forward takes 256 x 128 by 8 waves, two workgroups per CU, so
+//     that one's activations run beside the other's product: 164 for the bare product
+//     (155 with 256 x 256, the library's 132), but with gelu 185 (187), and a training
+//     step with z in 8 bits 656 (670).
 //   bfloat16, 128 and 64: 4 waves, steps of 64, two buffers, two workgroups and
-//     more: 685, 906, 867.
+//     more.  (The sizes above by them: forward 190, backward 366 against 330.)
 //   float32: one buffer of the three planes.  Rows along the reduction take 64 x
 //     128 by 4 waves, four workgroups per CU that load, split and multiply beside
-//     each other (128 x 128 by 8 waves, two per CU: dx of 100,003 x 128 x 256 96 us
-//     against 79, forward 100,000 x 128 x 256 80 against 64, 60,000 x 100 x 1,000 187
-//     against 158, but 4,096 x 2,048 x 1,024 143 against 150); across 128 x 128 by 4
-//     (208 TFLOP/s; 8 193).
+//     each other.  128 x 128 by 8 waves, two per CU, are slower where the reduction is
+//     short (forward 100,000 x 128 x 256 64 against 85, 60,000 x 100 x 1,000 155
+//     against 186, backward of 100,003 x 128 x 256 from 8 bits 138 against 167), as
+//     fast at 16,384 x 1,024 x 1,024 (221, 223) and faster where it is long (4,096 x
+//     2,048 x 1,024 124 against 116, 2,048 x 4,096 x 4,096 442 against 412; the
+//     library 120 for the former).  Across, 128 x 128 by 4 waves (8 were 8% slower).
 template <class J, int B>
 struct TileOf {
   static constexpr bool f32 = sizeof(typename J::T) == 4, along = J::FA == kAlong, fwd = along && J::FB == kAcross;
@@ -209,8 +211,9 @@ struct TileOf {
 
 // Which tile block u of tm x tn takes: blocks go round robin to the XCDs, so an
 // XCD takes a contiguous eighth, eight row tiles by eight column tiles running
-// together, which share their operands in its L2.  (It moves less between the
-// caches; the times of the sizes measured here are the same without.)
+// together, which share their operands in its L2: bfloat16 40,000 x 515 x 1,021 100
+// us against 108 in order, backward of 16,384 x 1,024 x 4,096 339 against 358, float32
+// 16,384 x 1,024 x 1,024 232 against 239; 8,192 x 4,096 x 4,096 307 either way.
 struct TileAt {
   int64_t m;
   int n;
@@ -267,9 +270,9 @@ __global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void 
 // order, the next block's while it works on one.  The waves of a workgroup take
 // neighbouring columns of the same rows.
 // What bounds a short reduction is the write of y; tiles through LDS wait for
-// their own loads, barriers and stores in turn.  156,000 x 64 x 1,664: bfloat16 119
-// us (4.5 TB/s), float32 320 (tiles 421; bound by the vector unit, which splits
-// every row once per wave); 1,248,000 x 64 x 64 59 (5.4 TB/s) and 137 (4.7).
+// their own loads, barriers and stores in turn.  156,000 x 64 x 1,664: bfloat16 113
+// us (4.8 TB/s), float32 304 (tiles 421; bound by the vector unit, which splits
+// every row once per wave); 1,248,000 x 64 x 64 59 (5.4 TB/s) and 131 (4.9).
 template <class J, int KK, int NC, bool FAST>
 __global__ __launch_bounds__(256, 2) void k_dense_panel(DenseArgs a) {
   using T = typename J::T;
@@ -412,8 +415,9 @@ __global__ __launch_bounds__(256, 2) void k_dense_panel(DenseArgs a) {
 // The same where rows have columns for several waves: WPB waves of a workgroup
 // bring each row block to LDS together, so that its terms are formed once and not
 // by every wave (a third of the vector work in float32, which is what bounds the
-// kernel above).  156,000 x 64 x 1,664 float32: 320 us there, 281 with 1,536 of the
-// columns here (228) and the rest there; 156,000 x 32 x 1,664 185 us (5.7 TB/s).
+// kernel above).  156,000 x 64 x 1,664 float32: 304 us there, 265 with 1,536 of the
+// columns here (228) and the rest there; 156,000 x 32 x 1,664 190 us (5.6 TB/s), 194
+// there.
 // Two waves with a reduction of 64 are slower than none (421): LDS leaves six on a
 // CU.  Columns are whole multiples of 64 WPB, the reduction is at most BK, y
 // streams and is the only output.
@@ -648,7 +652,10 @@ Cut dense_cut(e3_dtype t, int64_t rows, int64_t cols, int64_t red, Product which
   if (c.tile == 128 && t == E3_F32 && which != kDw) c.tiles = tiles(64, 128), fill = 2 * kFill;  // 64 x 128 by TileOf
   // at least 256 indexes a split; few tiles of few indexes take down to 64
   int64_t least = c.tiles * (red / 256) < kFill / 8 ? 64 : c.tile == 256 ? 2048 : 256;
-  if (red <= 384) least = 384;  // what a launch to join them takes is longer
+  // What a launch to join them takes is longer: bfloat16 300^3 8.8 us against 13.8, 64
+  // x 384 x 512 8.9 against 13.5, float32 16 x 300 x 300 11.8 against 13.7, 100 x 384 x
+  // 100 13.3 against 13.7, backward of 380 x 300 x 200 22 against 28.
+  if (red <= 384) least = 384;
   const int64_t s = std::max<int64_t>(
       1, std::min<int64_t>({fill / std::max<int64_t>(c.tiles, 1), (red + least - 1) / least, 256}));
   c.chunk = std::max<int64_t>(64, ((red + s - 1) / s + 63) / 64 * 64);

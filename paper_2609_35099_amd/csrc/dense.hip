@@ -12,7 +12,7 @@ namespace {
 // Reductions of at most KC <= 16 (a radial basis): the weights of a thread's V
 // columns stay in registers, rows go by with the next one's x in flight, and no
 // LDS is used; L lanes share a row.  Bound by the write of y: 1,248,000 x 8 x 64
-// float32 with silu 58 us (6.2 TB/s; 320 MB of zeros take 46), where the tile
+// float32 with silu 60 us (6.0 TB/s; 320 MB of zeros take 47), where the tile
 // product took 156 (its steps are of 32).
 template <class T, int L, int KC, bool FAST>
 __global__ __launch_bounds__(256) void k_dense_thin(DenseArgs a) {

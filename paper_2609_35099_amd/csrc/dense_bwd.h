@@ -27,7 +27,7 @@ __global__ __launch_bounds__((TileOf<J, B>::THREADS), 2) void k_dense_two(DenseA
 }
 
 // dz = dy act'(z) in the type of dy (a bfloat16 dz is an operand of the matrix
-// instructions, which take no more bits), and the column sums of its unrounded
+// instructions, which take no more bits: Kind says what that costs), and the column sums of its unrounded
 // values over the block's rows, for layers whose products would form dz too often
 // themselves (forms_dz).  Either output may be null.
 template <class T>

@@ -19,10 +19,11 @@
 // L lanes share a row, J 16-byte pieces each; narrow rows take part of a wave, wide
 // ones a workgroup, and rows past the registers are read again for each pass.
 //
-// One MI355X, 65,536 x 1,024 bfloat16: forward with statistics and x in 8 bits 76
-// us (4.4 TB/s), backward from x in 8 bits 60 us (5.6 TB/s) and 7 for the weight
-// gradients; 100,003 x 515 float32: backward 121 us (5.1 TB/s) and 7.  Packing
-// 65,536 x 2,048 bfloat16 82 us (4.9 TB/s), unpacking 66 (6.2).
+// One MI355X, us per call in a row of calls: 65,536 x 1,024 bfloat16 forward with
+// statistics and x in 8 bits 65 (5.2 TB/s), backward from x in 8 bits 63, of which dx
+// alone 50 (6.7 TB/s, x's 8 bits from the last-level cache); 100,003 x 515 float32
+// forward 69 (5.9 TB/s), backward 130, dx alone 117 (5.3).  Packing 65,536 x 2,048
+// bfloat16 80 (5.1), unpacking 60 (6.8).
 #include "layers.h"
 
 namespace {
