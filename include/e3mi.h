@@ -438,6 +438,89 @@ e3_status e3_dense_bwd(e3_dtype dtype, const void* x, int64_t ldx, const int8_t*
                        int64_t lddy, void* dx, int64_t lddx, void* dW, void* db, void* ws, size_t ws_bytes, int64_t M,
                        int64_t K, int64_t N, e3_stream stream);
 
+/* Gated dense layer: [g | u] = x W + bias, y = act(g) u, with x [M, K], W [K, 2 N]
+ * (the columns of g, then those of u), bias [2 N] (NULL: none) and y [M, N]; N is at
+ * most 2^19.  With a dense layer after it, it is the feed-forward block of a
+ * transformer or of an edge network.  Optional outputs (NULL: not stored), for the
+ * backward and for the layer that reads y: z [M, 2 N], its rows g and u side by
+ * side; gq, gc and uq, uc: g and u in 8 bits, from their float32 values; yq, yc: y as
+ * stored, in 8 bits.
+ * ws: at least fwd_bytes of e3_gated_workspace_size (0 for most sizes). */
+e3_status e3_gated_workspace_size(e3_dtype dtype, int64_t M, int64_t K, int64_t N, size_t* fwd_bytes,
+                                  size_t* bwd_bytes);
+e3_status e3_gated_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* W, const void* bias, e3_act act, void* y,
+                       int64_t ldy, void* z, int64_t ldz, int8_t* gq, uint8_t* gc, int8_t* uq, uint8_t* uc, int8_t* yq,
+                       uint8_t* yc, void* ws, size_t ws_bytes, int64_t M, int64_t K, int64_t N, e3_stream stream);
+/* With dz = [dy u act'(g) | dy act(g)]: dx = dz W^T, dW = x^T dz, db = the column
+ * sums of dz (each may be NULL).  x (for dW) and z in full, or packed: xq, xc, and
+ * gq, gc and uq, uc.  dz is rounded as a dense backward's.  M = 0 gives dW = 0 and
+ * db = 0.  ws: bwd_bytes, 16-byte aligned. */
+e3_status e3_gated_bwd(e3_dtype dtype, const void* x, int64_t ldx, const int8_t* xq, const uint8_t* xc, const void* W,
+                       const void* z, int64_t ldz, const int8_t* gq, const uint8_t* gc, const int8_t* uq,
+                       const uint8_t* uc, e3_act act, const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dW,
+                       void* db, void* ws, size_t ws_bytes, int64_t M, int64_t K, int64_t N, e3_stream stream);
+
+/* Dropout: y = r + keep x / (1 - p), r [rows, cols] or NULL (0), p in [0, 1]; a
+ * dropped x is not looked at (an infinity or a NaN there does not reach y).
+ * The mask is never stored: the backward makes it again from what made it.  It is a
+ * function of seed, offset, row and column alone: Philox 4x32 with ten rounds
+ * (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3",
+ * 2011), key (seed mod 2^32, seed / 2^32), counter (row mod 2^32, row / 2^32 2^17 +
+ * col / 8, offset mod 2^32, offset / 2^32).  Of the 128 bits, lowest first, 16 from
+ * 16 (col mod 8) on are the column's; it is dropped where they are below t =
+ * 65536 p, rounded to the nearest integer (ties to even), and what stays is
+ * multiplied by 65536 / (65536 - t).  Calls that shall have other masks take
+ * another seed or offset.
+ * counter: device memory (8-byte aligned) whose value is added to offset when the
+ * kernel runs, or NULL; a captured graph draws another mask in each replay if the
+ * program counts it up in between (after the backward has run).
+ * y may be x or r itself (same ld).  dx = keep dy / (1 - p); dx may be dy. */
+e3_status e3_dropout_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* r, int64_t ldr, double p, uint64_t seed,
+                         uint64_t offset, const int64_t* counter, void* y, int64_t ldy, int64_t rows, int64_t cols,
+                         e3_stream stream);
+e3_status e3_dropout_bwd(e3_dtype dtype, const void* dy, int64_t lddy, double p, uint64_t seed, uint64_t offset,
+                         const int64_t* counter, void* dx, int64_t lddx, int64_t rows, int64_t cols, e3_stream stream);
+
+/* What stands between two blocks of a residual network, in one pass over rows: the
+ * norm after a block, dropout, gate, residual scale, the sum, and the norm before
+ * the next block,
+ *   s = r + scale gate drop(N1(h)),  y = N2(s).
+ * where: E3_NORM_AFTER (N1) and E3_NORM_BEFORE (N2; without it y is NULL), or-ed; a
+ * norm that is not named is left out, with its weights NULL.  E3_NORM_RMS: N(x) = x
+ * rstd gamma with rstd = 1 / sqrt(mean(x^2) + eps), no beta; E3_NORM_LAYER: the layer
+ * norm above.  gamma, beta [cols] (NULL: 1, 0); eps >= 0.  r [rows, cols] (NULL: 0).
+ * gate: NULL (1), [cols] (ldg = 0) or [rows, cols] (ldg at least cols).  Dropout as
+ * above (p = 0: none).  h alone with E3_NORM_AFTER and scale 1 is a norm by itself.
+ * Outputs: s (may be NULL with N2; may be r itself, same ld), y, and for the
+ * backward the statistics of N1 and N2, [rows] float32 (NULL: not stored; the means
+ * of a layer norm only).  N2 reads the sum's float32 values, not s as stored.
+ * Squares are summed in float32: a row whose values pass 1e19 has rstd 0. */
+typedef enum { E3_NORM_RMS = 0, E3_NORM_LAYER = 1 } e3_norm;
+#define E3_NORM_AFTER 1u
+#define E3_NORM_BEFORE 2u
+e3_status e3_residual_norm_fwd(e3_dtype dtype, e3_norm norm, unsigned where, const void* h, int64_t ldh, const void* r,
+                               int64_t ldr, const void* gate, int64_t ldg, float scale, double p, uint64_t seed,
+                               uint64_t offset, const int64_t* counter, const void* gamma1, const void* beta1,
+                               const void* gamma2, const void* beta2, float eps, void* s, int64_t lds, void* y,
+                               int64_t ldy, float* mean1, float* rstd1, float* mean2, float* rstd2, int64_t rows,
+                               int64_t cols, e3_stream stream);
+/* From the cotangents dy of y and ds of s (NULL: 0; without N2 dy is NULL and ds is
+ * there), the forward's h, s (with N2), gate, dropout and statistics: dr (s's whole
+ * cotangent, r's), dh, dgate (shape of gate; a vector's sums over the rows), and the
+ * gradients of the norms' weights, [cols].  Each may be NULL.  h may be NULL without
+ * N1 and dgate.  Sums over rows go through ws (at least
+ * e3_residual_norm_workspace_size bytes; not needed without them) in a fixed order;
+ * they are zero for rows = 0. */
+e3_status e3_residual_norm_workspace_size(e3_dtype dtype, int64_t rows, int64_t cols, size_t* bwd_bytes);
+e3_status e3_residual_norm_bwd(e3_dtype dtype, e3_norm norm, unsigned where, const void* h, int64_t ldh, const void* s,
+                               int64_t lds, const void* gate, int64_t ldg, float scale, double p, uint64_t seed,
+                               uint64_t offset, const int64_t* counter, const void* gamma1, const void* beta1,
+                               const void* gamma2, const float* mean1, const float* rstd1, const float* mean2,
+                               const float* rstd2, const void* dy, int64_t lddy, const void* ds, int64_t ldds, void* dr,
+                               int64_t lddr, void* dh, int64_t lddh, void* dgate, int64_t lddg, void* dgamma1,
+                               void* dbeta1, void* dgamma2, void* dbeta2, void* ws, size_t ws_bytes, int64_t rows,
+                               int64_t cols, e3_stream stream);
+
 /* Per-kernel timing (instrumentation).  While enabled, every kernel the
  * library launches is bracketed by two HIP events on the caller's stream.
  * e3_timing_read waits for the recorded events and returns, per kernel name

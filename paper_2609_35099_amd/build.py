@@ -9,7 +9,7 @@
 2. hipcc compiles the core unit (csrc/e3mi.hip: C ABI, graph, linear mixing,
    record tensor product, probes), the record convolution (csrc/convr.hip:
    layouts without a compiled unit), the invariant layers (csrc/dense*.hip,
-   csrc/norm.hip), every layout unit and the builder for gfx950, in parallel,
+   csrc/gated*.hip, csrc/norm.hip, csrc/residual.hip), every layout unit and the builder for gfx950, in parallel,
    and links libe3mi.so next to this file.
 
 Layouts beyond the defaults compiled into the generator (the benchmark and
@@ -94,7 +94,8 @@ def build(verbose: bool = True, extra=None) -> str:
     objdir = os.path.join(BUILD, "obj")
     os.makedirs(objdir, exist_ok=True)
     sources = [os.path.join(CSRC, "e3mi.hip"), os.path.join(CSRC, "convr.hip"),
-               *(os.path.join(CSRC, f) for f in ("dense.hip", "dense_bwd_f32.hip", "dense_bwd_bf16.hip", "norm.hip")),
+               *(os.path.join(CSRC, f) for f in ("dense.hip", "dense_bwd_f32.hip", "dense_bwd_bf16.hip", "gated.hip",
+                                              "gated_f32.hip", "gated_bf16.hip", "norm.hip", "residual.hip")),
                os.path.join(CSRC, "builder.cpp")] + \
               [os.path.join(GEN, u) for u in units]
     objs = []

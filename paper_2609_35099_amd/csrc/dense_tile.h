@@ -31,7 +31,10 @@ typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-enum Form { kAlong, kAcross };
+// Across in pairs: two halves of the columns side by side, of which the tile takes
+// 32 of the first and 32 of the second in turn, so that a wave's neighbouring blocks
+// of 32 hold the two of a pair (W of a gated layer; the output has a half's columns).
+enum Form { kAlong, kAcross, kPaired };
 
 constexpr float kTermScale = 0x1p24f, kTermBack = 0x1p-48f;
 
@@ -104,13 +107,16 @@ struct Fetch {
 
   static __device__ __forceinline__ int row_of(int i) { return threadIdx.x / PER + i * (THREADS / PER); }
   static __device__ __forceinline__ int col_of() { return threadIdx.x % PER * V; }
+  // Columns of the output that the tile spans, and the piece's among them.
+  static constexpr int SPAN = F == kPaired ? W / 2 : W;
+  static __device__ __forceinline__ int out_of(int col) { return F == kPaired ? col / 64 * 32 + col % 32 : col; }
   // The reduction index before which the tile's pieces are inside the matrix's
   // span: where rows or columns end within the tile (across), pieces past the end
   // hold values of the next row, which only reach results that are not stored.
   static __device__ __forceinline__ int64_t whole_until(const Side& s, int64_t r0, int64_t rows) {
     constexpr int64_t all = (int64_t)1 << 62;
-    if (F == kAlong || r0 + W <= rows) return all;
-    const int64_t room = s.total - r0 - W;
+    if (F == kAlong || r0 + SPAN <= rows) return all;
+    const int64_t room = s.total - (F == kPaired ? rows : 0) - r0 - SPAN;
     int64_t m = room < 0 ? 0 : room / s.ld + 1;
     if constexpr (Q) {
       const int64_t left = s.total / s.ld * s.ldc - r0 / kGroup - W / kGroup, mc = left < 0 ? 0 : left / s.ldc + 1;
@@ -135,7 +141,8 @@ struct Fetch {
     const E* p = (Q ? reinterpret_cast<const E*>(s.q) : static_cast<const E*>(s.p)) + (m0 * s.ld + c0);
     const uint8_t* pc = Q ? s.c + (m0 * s.ldc + c0 / kGroup) : nullptr;
     const int mlast = mend - m0 < 1024 ? (int)(mend - m0) - 1 : 1023;
-    const int lc = col_of();
+    // (rows: of a pair, the columns of a half)
+    const int oc = out_of(col_of()), lc = F == kPaired && col_of() / 32 % 2 ? oc + (int)rows : oc;
     if constexpr (WHOLE) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -147,7 +154,7 @@ struct Fetch {
     }
     const E* first = Q ? reinterpret_cast<const E*>(s.q) : static_cast<const E*>(s.p);
     const int left = cend - c0 < 1024 ? (int)(cend - c0) : 1024;  // columns from c0 on, at least one
-    const int n = left - lc < V ? (left - lc > 0 ? left - lc : 0) : V;
+    const int n = left - oc < V ? (left - oc > 0 ? left - oc : 0) : V;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const bool in = F == kAlong || row_of(i) <= mlast;
@@ -189,6 +196,7 @@ template <class T, Form F, int R, int BK, int THREADS, Kind KD>
 struct Loader {
   static constexpr int V = Elem<T>::V;
   static constexpr bool Q = KD == kPacked, G = KD >= kGradFull;
+  static_assert(F != kPaired || KD == kFull);
   static constexpr int P = sizeof(T) == 2 || Q ? 1 : 3;   // planes
   using Lds = Plane<F, R, BK, P>;
   using Main = Fetch<T, F, R, BK, THREADS, Q>;

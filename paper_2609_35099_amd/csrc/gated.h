@@ -1,0 +1,458 @@
+// Gated dense layers, for the type of the including unit.
+//
+//   [g | u] = x W + b,  y = act(g) u           W [K, 2 N]
+//   dz = [dy u act'(g) | dy act(g)],  dx = dz W^T, dW = x^T dz, db = sum_rows dz
+//
+// Forward: a tile takes the columns of both halves in turns of 32 (kPaired), so
+// that the two of a pair meet in one wave's staging and neither g nor u goes to
+// memory unless it is kept.  Backward: dz is written once, by the pass that sums db,
+// and the products are those of a dense layer of 2 N columns.
+#pragma once
+#include "dense.h"
+
+// A gated call, checked.
+struct GatedCall {
+  e3_dtype dtype;
+  const void *x, *W, *bias;
+  int64_t ldx;
+  int act;
+  void *y, *z;
+  int64_t ldy, ldz;
+  int8_t *gq, *uq, *yq;
+  uint8_t *gc, *uc, *yc;
+  // backward
+  const void *dy, *z_in;
+  const int8_t *xq, *gq_in, *uq_in;
+  const uint8_t *xc, *gc_in, *uc_in;
+  void *dx, *dW, *db;
+  int64_t lddy, lddx;
+  char* ws;
+  int64_t M, K, N;
+  hipStream_t st;
+};
+e3_status gated_fwd_f32(const GatedCall& c);
+e3_status gated_fwd_bf16(const GatedCall& c);
+
+namespace {
+
+struct GatedArgs {
+  Side a, b;  // x [rows, red], W [red, 2 cols]
+  int64_t rows, red;
+  int cols;   // of y
+  const void* bias;
+  int act;
+  void *y, *z;
+  int64_t ldy, ldz;
+  int8_t *gq, *uq, *yq;
+  uint8_t *gc, *uc, *yc;
+  int64_t chunks;  // row chunks of the panel
+  bool nt;
+};
+
+// What follows the sums of a piece of a row: columns col on of y.  The lanes of a
+// group of 32 columns take part together, also where rows (ok) or columns end.
+template <class T>
+struct GatedTail {
+  static constexpr int V = Elem<T>::V;
+  float bg[V], bu[V];
+  __device__ __forceinline__ GatedTail(const GatedArgs& a, int col) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) bg[i] = bu[i] = 0.0f;
+    if (!a.bias) return;
+    ld_piece<T>(static_cast<const T*>(a.bias) + col, a.cols - col, bg);
+    ld_piece<T>(static_cast<const T*>(a.bias) + a.cols + col, a.cols - col, bu);
+  }
+  // FAST: the piece is inside the row, y streams and is the only output (plain()).
+  template <bool FAST = false>
+  __device__ __forceinline__ void out(const GatedArgs& a, int64_t row, bool ok, int col, float (&g)[V],
+                                      float (&u)[V]) const {
+    const int n = FAST ? V : ok ? a.cols - col : 0;
+    const int64_t groups = (a.cols + kGroup - 1) / kGroup;
+    auto pack = [&](const float(&v)[V], int8_t* q, uint8_t* c) {
+      pack8_piece<V>(v, col, n, q + row * a.cols, c + row * groups);
+    };
+#pragma unroll
+    for (int i = 0; i < V; ++i) g[i] += bg[i], u[i] += bu[i];
+    if (!FAST && a.z) {
+      T* z = static_cast<T*>(a.z) + row * a.ldz + col;
+      st_piece<T>(z, n, g, a.nt);
+      st_piece<T>(z + a.cols, n, u, a.nt);
+    }
+    if (!FAST && a.gq) pack(g, a.gq, a.gc), pack(u, a.uq, a.uc);
+    act_piece(a.act, g);
+#pragma unroll
+    for (int i = 0; i < V; ++i) g[i] = Elem<T>::round(g[i] * u[i]);
+    T* y = static_cast<T*>(a.y) + row * a.ldy + col;
+    if constexpr (FAST) __builtin_nontemporal_store(Elem<T>::put(g), reinterpret_cast<typename Elem<T>::vec*>(y));
+    else st_piece<T>(y, n, g, a.nt);
+    if (!FAST && a.yq) pack(g, a.yq, a.yc);
+  }
+  static bool plain(const GatedArgs& a) { return a.nt && !a.z && !a.gq && !a.yq; }
+};
+
+// A sum again from memory, in float32 (half 0: g, 1: u).
+template <class T>
+__device__ __forceinline__ float gated_again(const GatedArgs& a, int64_t row, int col, int half) {
+  float sum = 0.0f;
+  const T* x = static_cast<const T*>(a.a.p) + row * a.a.ld;
+  const T* w = static_cast<const T*>(a.b.p) + (int64_t)half * a.cols + col;
+#pragma clang loop unroll(disable)
+  for (int64_t k = 0; k < a.red; ++k) sum = fmaf(Elem<T>::one(x[k]), Elem<T>::one(w[k * a.b.ld]), sum);
+  return sum;
+}
+
+// The results of rows row0 to row0 + 31 and 16 RN columns of y from col0 on: blocks
+// of 32 columns of g and of u in turn.
+template <class T, int RN, bool FAST = false>
+__device__ __forceinline__ void gated_rows32(const GatedArgs& a, int64_t row0, int col0, float (*out)[32 * RN + 4],
+                                             const f16v (&acc)[RN]) {
+  using R = Rows32<T, RN>;
+  constexpr int V = R::V, PER = 16 * RN / V, PASS = kWave / PER, N = 32 / PASS;
+  const int l = threadIdx.x % kWave, oc = l % PER * V, lr = l / PER, at = oc / 32 * 64 + oc % 32;
+  const GatedTail<T> tail(a, col0 + oc);
+  R::put(out, acc);
+  if constexpr (sizeof(T) == 4) {
+    if (R::bad(acc))
+      R::mend(out, [&](int r, int c) {
+        const int col = col0 + c / 64 * 32 + c % 32;
+        return row0 + r < a.rows && col < a.cols ? gated_again<T>(a, row0 + r, col, c / 32 % 2) : 0.0f;
+      });
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int r = i * PASS + lr;
+    float g[V], u[V];
+#pragma unroll
+    for (int e = 0; e < V; e += 4) {
+      *reinterpret_cast<f4v*>(&g[e]) = *reinterpret_cast<const f4v*>(&out[r][at + e]);
+      *reinterpret_cast<f4v*>(&u[e]) = *reinterpret_cast<const f4v*>(&out[r][at + 32 + e]);
+    }
+    tail.template out<FAST>(a, row0 + r, FAST || row0 + r < a.rows, col0 + oc, g, u);
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Tiles by type and size, as TileOf's; every wave has 64 columns of z, 32 of y.
+template <class T, int B>
+struct GatedTileOf {
+  static constexpr bool f32 = sizeof(T) == 4;
+  static constexpr int BM = f32 && B == 128 ? 64 : B, BN = B == 256 ? 128 : B;
+  static constexpr int WM = B == 256 ? 4 : 2, WN = BN / 64;
+  static constexpr int BK = f32 || B == 256 ? 32 : 64, THREADS = WM * WN * kWave, OCC = B == 256 ? 4 : 2;
+  using type = Tile<T, kAlong, kPaired, BM, BN, BK, WM, WN, kFull, kFull, false, f32 ? 1 : 2>;
+};
+template <class T, int B>
+__global__ __launch_bounds__((GatedTileOf<T, B>::THREADS), (GatedTileOf<T, B>::OCC)) void k_gated(GatedArgs a) {
+  using O = GatedTileOf<T, B>;
+  using Tl = typename O::type;
+  __shared__ __align__(16) typename Tl::Shared sh;
+  const int64_t tm = (a.rows + O::BM - 1) / O::BM, u = block_id();
+  const int tn = (a.cols + O::BN / 2 - 1) / (O::BN / 2);
+  if (u >= tm * tn) return;
+  const TileAt at = tile_at(u, tm, tn);
+  const int64_t r0 = at.m * O::BM;
+  const int c0 = at.n * (O::BN / 2);
+  Tl t;
+  t.template run<false>(sh, {a.a, a.b, {}, 0}, r0, a.rows, c0, a.cols, 0, a.red);
+  t.finish(sh, [&](int r, int c, auto out, auto& acc) { gated_rows32<T, Tl::RN>(a, r0 + r, c0 + c / 2, out, acc); });
+}
+
+// Short reductions over many rows, as k_dense_panel: a wave keeps the terms of 32
+// columns of g and of u and walks row blocks.
+template <class T, int KK, bool FAST>
+__global__ __launch_bounds__(256, 2) void k_gated_panel(GatedArgs a) {
+  using R = Rows32<T, 2>;
+  constexpr bool f32 = sizeof(T) == 4;
+  constexpr int V = Elem<T>::V, P = f32 ? 3 : 1, Q = 8 / V;
+  __shared__ __align__(16) float out[4][32][R::PITCH];
+  const int l = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), K = (int)a.red;
+  const int groups = (a.cols + 31) / 32;
+  const int64_t w = block_id() * 4 + wave, chunk = w / groups;
+  if (chunk >= a.chunks) return;
+  const int col0 = (int)(w % groups) * 32;
+  const int h = 8 * (l / 32);
+  bf8v wf[P][KK][2];
+#pragma unroll
+  for (int k = 0; k < KK; ++k)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int col = col0 + l % 32;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int at = 16 * k + h + e;
+        v[e] = at < K && col < a.cols ? Elem<T>::one(static_cast<const T*>(a.b.p)[at * a.b.ld + c * a.cols + col]) : 0.0f;
+        if (f32) v[e] *= kTermScale;
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        u4v t;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = term2(v[2 * e], v[2 * e + 1]);
+        wf[p][k][c] = __builtin_bit_cast(bf8v, t);
+      }
+    }
+  typename Elem<T>::vec x[KK][Q];
+  const T* xp = static_cast<const T*>(a.a.p);
+  auto load = [&](auto fast, int64_t block) {
+    constexpr bool F = decltype(fast)::value;
+    const int last = F ? 31 : a.rows - block * 32 < 32 ? (int)(a.rows - block * 32) - 1 : 31;
+    const int64_t m = imin(l % 32, last);
+#pragma unroll
+    for (int k = 0; k < KK; ++k)
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int at = 16 * k + h + q * V;
+        x[k][q] = ld_raw<T>(xp + block * 32 * a.a.ld + (m * a.a.ld + at), F ? V : K - at);
+      }
+  };
+  bf8v xf[P][KK];
+  auto terms = [&]() {
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      if constexpr (!f32) {
+        xf[0][k] = __builtin_bit_cast(bf8v, x[k][0]);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) Elem<T>::get(x[k][q], reinterpret_cast<float(&)[V]>(v[q * V]));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= kTermScale;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          u4v t;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t[e] = term2(v[2 * e], v[2 * e + 1]);
+          xf[p][k] = __builtin_bit_cast(bf8v, t);
+        }
+      }
+    }
+  };
+  auto product = [&](auto fast, int64_t block) {
+    f16v acc[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[c][e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KK; ++k)
+#pragma unroll
+      for (int s = 2 * P - 2 < 2 ? 2 * P - 2 : 2; s >= 0; --s)
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const int q = s - p;
+          if (q < 0 || q >= P) continue;
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[q][k][c], xf[p][k], acc[c], 0, 0, 0);
+        }
+    gated_rows32<T, 2, decltype(fast)::value>(a, block * 32, col0, out[wave], acc);
+  };
+  // FAST: whole row blocks by a loop without branches around loads and stores, and
+  // what is left of the rows after it
+  const int64_t blocks = FAST ? a.rows / 32 : (a.rows + 31) / 32;
+  const std::integral_constant<bool, FAST> fast;
+  if (chunk < blocks) {
+    // a round ends with loads and begins with stores, so that its wait for the
+    // loads of the one before leaves its own stores in flight; blocks past the
+    // end load the last one again
+    auto at = [&](int64_t b) { return b < blocks ? b : blocks - 1; };
+    load(fast, chunk);
+    terms();
+    load(fast, at(chunk + a.chunks));
+    for (int64_t block = chunk; block < blocks; block += a.chunks) {
+      product(fast, block);
+      terms();
+      load(fast, at(block + 2 * a.chunks));
+    }
+  }
+  if (FAST && a.rows % 32 && chunk == blocks % a.chunks) {
+    load(std::false_type{}, blocks);
+    terms();
+    product(std::false_type{}, blocks);
+  }
+}
+
+// At most MR <= 8 rows, as k_dense_few: W is read once, straight to registers, and
+// that is what bounds it.  A workgroup takes 32 columns of y.
+template <class T, int MR>
+__global__ __launch_bounds__(512) void k_gated_few(GatedArgs a) {
+  constexpr int V = Elem<T>::V, C = 32 / V, G = 512 / C, WAVES = 512 / kWave;
+  __shared__ float s[WAVES][2][MR][32];
+  const int cl = threadIdx.x % C, g = threadIdx.x / C, col = (int)blockIdx.x * 32 + cl * V, n = a.cols - col;
+  const int K = (int)a.red;
+  const T* W = static_cast<const T*>(a.b.p);
+  const T* x = static_cast<const T*>(a.a.p);
+  float v[2][MR][V] = {};
+  constexpr int U = MR > 4 ? 2 : 4;  // reduction indexes in flight
+  for (int k0 = g; k0 < K; k0 += G * U) {
+    typename Elem<T>::vec w[U][2];
+    float u[U][MR];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int k = k0 + j * G;
+      if (k < K) {
+        w[j][0] = ld_raw<T>(W + k * a.b.ld + col, n);
+        w[j][1] = ld_raw<T>(W + k * a.b.ld + a.cols + col, n);
+#pragma unroll
+        for (int m = 0; m < MR; ++m) u[j][m] = m < a.rows ? Elem<T>::one(x[m * a.a.ld + k]) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (k0 + j * G < K) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float t[V];
+          Elem<T>::get(w[j][h], t);
+#pragma unroll
+          for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[h][m][i] = fmaf(u[j][m], t[i], v[h][m][i]);
+        }
+      }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float t = sum_strided<C>(v[h][m][i]);
+        if (threadIdx.x % kWave < C) s[threadIdx.x / kWave][h][m][cl * V + i] = t;
+      }
+  __syncthreads();
+  if (threadIdx.x >= MR * C) return;
+  float t[2][V] = {};
+  for (int q = 0; q < WAVES; ++q)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < V; ++i) t[h][i] += s[q][h][g][cl * V + i];
+  GatedTail<T>(a, col).out(a, g, g < a.rows, col, t[0], t[1]);
+}
+
+// Partial sums of z from the splits of its reduction, in order, and the epilogue.
+template <class T>
+__global__ __launch_bounds__(256) void k_gated_join(GatedArgs a, const float* part, int splits) {
+  constexpr int V = Elem<T>::V;
+  const int per = (a.cols + kGroup - 1) / kGroup * (kGroup / V);
+  const int64_t i = block_id() * 256 + threadIdx.x, row = div_small(i, per);
+  const int col = (int)(i - row * per) * V;
+  const int n = row < a.rows ? a.cols - col : 0;
+  const int64_t pitch = a.rows * 2 * a.cols;
+  float v[2][V] = {};
+  const float* p = part + (row * 2 * a.cols + col);
+  for (int s = 0; s < splits; s += 4) {
+    float u[4][2][V];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < V; e += 4)
+          ld_piece<float>(p + (s + j) * pitch + (int64_t)h * a.cols + e, s + j < splits ? n - e : 0,
+                          reinterpret_cast<float(&)[4]>(u[j][h][e]));
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[h][e] += u[j][h][e];
+  }
+  GatedTail<T>(a, col).out(a, row, row < a.rows, col, v[0], v[1]);
+}
+
+// ------------------------------------------------------------ host
+constexpr int kGatedThin = 16, kGatedFew = 8;
+// How a forward goes.
+enum class GatedWay { few, panel, split, tile };
+GatedWay gated_way(e3_dtype t, int64_t M, int64_t K, int64_t N) {
+  if (M <= kGatedFew) return GatedWay::few;
+  // (a reduction this short has no whole piece to read in the tile's way)
+  const bool p = t == E3_F32 ? panel<float>(M, 2 * N, K) : panel<__bf16>(M, 2 * N, K);
+  if (p || K <= kGatedThin) return GatedWay::panel;
+  return dense_cut(t, M, 2 * N, K, kForward).splits > 1 ? GatedWay::split : GatedWay::tile;
+}
+size_t gated_fwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
+  if (M == 0 || gated_way(t, M, K, N) != GatedWay::split) return 0;
+  return cut_bytes(dense_cut(t, M, 2 * N, K, kForward), M, 2 * N);
+}
+
+template <class T>
+e3_status gated_panel(GatedArgs a, hipStream_t st) {
+  // two workgroups per CU, each wave on row blocks of its own
+  const int64_t groups = (a.cols + 31) / 32;
+  a.chunks = std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 2048 / groups));
+  const int64_t blocks = (a.chunks * groups + 3) / 4;
+  TimedLaunch t_("gated_fwd_panel", st);
+  auto go = [&](auto KK) {
+    constexpr int kk = decltype(KK)::value;
+    const bool fast = a.red == 16 * kk && a.cols % 32 == 0 && GatedTail<T>::plain(a);
+    auto* k = fast ? k_gated_panel<T, kk, true> : k_gated_panel<T, kk, false>;
+    hipLaunchKernelGGL(k, grid_of(blocks), dim3(256), 0, st, a);
+  };
+  if (a.red <= 16) go(std::integral_constant<int, 1>{});
+  else if (a.red <= 32) go(std::integral_constant<int, 2>{});
+  else if (sizeof(T) == 4 && a.red <= 48) go(std::integral_constant<int, 3>{});
+  else if (a.red <= 64) go(std::integral_constant<int, 4>{});
+  else if constexpr (sizeof(T) == 2) {
+    if (a.red <= 96) go(std::integral_constant<int, 6>{});
+    else go(std::integral_constant<int, 8>{});
+  }
+  E3_HIP(hipGetLastError());
+  return E3_OK;
+}
+
+template <class T>
+e3_status gated_fwd(const GatedCall& c) {
+  constexpr e3_dtype t = std::is_same_v<T, float> ? E3_F32 : E3_BF16;
+  GatedArgs a{};
+  a.a = {c.x, c.ldx, nullptr, nullptr, 0, (c.M - 1) * c.ldx + c.K};
+  a.b = {c.W, 2 * c.N, nullptr, nullptr, 0, c.K * 2 * c.N};
+  a.rows = c.M, a.red = c.K, a.cols = (int)c.N, a.bias = c.bias, a.act = c.act, a.y = c.y, a.z = c.z, a.ldy = c.ldy;
+  a.ldz = c.ldz, a.gq = c.gq, a.uq = c.uq, a.yq = c.yq, a.gc = c.gc, a.uc = c.uc, a.yc = c.yc;
+  a.nt = streams(t, c.M, c.N);
+  switch (gated_way(t, c.M, c.K, c.N)) {
+    case GatedWay::few: {
+      TimedLaunch t_("gated_fwd_few", c.st);
+      auto* k = c.M == 1 ? k_gated_few<T, 1> : c.M == 2 ? k_gated_few<T, 2> : c.M <= 4 ? k_gated_few<T, 4>
+                                                                                   : k_gated_few<T, kGatedFew>;
+      hipLaunchKernelGGL(k, dim3((unsigned)((c.N + 31) / 32)), dim3(512), 0, c.st, a);
+      break;
+    }
+    case GatedWay::panel: return gated_panel<T>(a, c.st);
+    case GatedWay::split: {
+      // z as a dense layer's partial sums
+      using J = Job<T, kAlong, kAcross, kFull, kFull, false>;
+      const Cut cut = dense_cut(t, c.M, 2 * c.N, c.K, kForward);
+      DenseArgs d{};
+      float* part = reinterpret_cast<float*>(c.ws);
+      d.a = a.a, d.b = a.b, d.rows = c.M, d.cols = (int)(2 * c.N), d.red = c.K;
+      set_cut(d, cut, part);
+      const e3_status s = dense_launch<J>(d, cut, {"gated_fwd_split_64", "gated_fwd_split_128", "gated_fwd_split_256"}, c.st);
+      if (s != E3_OK) return s;
+      TimedLaunch t_("gated_fwd_join", c.st);
+      const int64_t per = (c.N + kGroup - 1) / kGroup * (kGroup / Elem<T>::V);
+      hipLaunchKernelGGL(k_gated_join<T>, grid_of((c.M * per + 255) / 256), dim3(256), 0, c.st, a, part, cut.splits);
+      break;
+    }
+    case GatedWay::tile: {
+      const int b = dense_cut(t, c.M, 2 * c.N, c.K, kForward).tile;
+      TimedLaunch t_(b == 64 ? "gated_fwd_64" : b == 128 ? "gated_fwd_128" : "gated_fwd_256", c.st);
+      auto go = [&](auto B) {
+        using O = GatedTileOf<T, decltype(B)::value>;
+        const int64_t tiles = (c.M + O::BM - 1) / O::BM * ((c.N + O::BN / 2 - 1) / (O::BN / 2));
+        hipLaunchKernelGGL((k_gated<T, decltype(B)::value>), grid_of(tiles), dim3(O::THREADS), 0, c.st, a);
+      };
+      if (b == 64) go(std::integral_constant<int, 64>{});
+      else if (b == 128) go(std::integral_constant<int, 128>{});
+      else if constexpr (t == E3_BF16) go(std::integral_constant<int, 256>{});
+      break;
+    }
+  }
+  E3_HIP(hipGetLastError());
+  return E3_OK;
+}
+
+}  // namespace

@@ -44,6 +44,7 @@ _lib = None
 
 # name -> (restype, argtypes); mirrors include/e3mi.h
 _P, _I, _I64, _U, _D = ct.c_void_p, ct.c_int, ct.c_int64, ct.c_uint, ct.c_double
+_U64 = ct.c_uint64
 SIGNATURES = {
     "e3_plan_create": (_I, [ct.c_char_p, _I, _I, _U, ct.POINTER(_P)]),
     "e3_plan_query": (_I, [_P, ct.POINTER(PlanInfo)]),
@@ -101,6 +102,19 @@ SIGNATURES = {
                           _I64, _I64, _I64, _P]),
     "e3_dense_bwd": (_I, [_I, _P, _I64, _P, _P, _P, _P, _I64, _P, _P, _I, _P, _I64, _P, _I64, _P, _P, _P, ct.c_size_t,
                           _I64, _I64, _I64, _P]),
+    "e3_gated_workspace_size": (_I, [_I, _I64, _I64, _I64, ct.POINTER(ct.c_size_t), ct.POINTER(ct.c_size_t)]),
+    "e3_gated_fwd": (_I, [_I, _P, _I64, _P, _P, _I, _P, _I64, _P, _I64, _P, _P, _P, _P, _P, _P, _P, ct.c_size_t, _I64,
+                          _I64, _I64, _P]),
+    "e3_gated_bwd": (_I, [_I, _P, _I64, _P, _P, _P, _P, _I64, _P, _P, _P, _P, _I, _P, _I64, _P, _I64, _P, _P, _P,
+                          ct.c_size_t, _I64, _I64, _I64, _P]),
+    "e3_dropout_fwd": (_I, [_I, _P, _I64, _P, _I64, _D, _U64, _U64, _P, _P, _I64, _I64, _I64, _P]),
+    "e3_dropout_bwd": (_I, [_I, _P, _I64, _D, _U64, _U64, _P, _P, _I64, _I64, _I64, _P]),
+    "e3_residual_norm_fwd": (_I, [_I, _I, _U, _P, _I64, _P, _I64, _P, _I64, ct.c_float, _D, _U64, _U64, _P, _P, _P, _P, _P,
+                                  ct.c_float, _P, _I64, _P, _I64, _P, _P, _P, _P, _I64, _I64, _P]),
+    "e3_residual_norm_workspace_size": (_I, [_I, _I64, _I64, ct.POINTER(ct.c_size_t)]),
+    "e3_residual_norm_bwd": (_I, [_I, _I, _U, _P, _I64, _P, _I64, _P, _I64, ct.c_float, _D, _U64, _U64, _P, _P, _P, _P, _P,
+                                  _P, _P, _P, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _P, _P, _P, _P,
+                                  ct.c_size_t, _I64, _I64, _P]),
     "e3_probe_stream": (_I, [_P, ct.c_size_t, _P, ct.c_size_t, _I, _I, _I, _U, ct.POINTER(ct.c_size_t),
                              ct.POINTER(ct.c_size_t), _P]),
     "e3_timing_enable": (_I, [_I]),
@@ -141,7 +155,8 @@ def _torch():
     if _modules is None:
         import torch
         _modules = torch, {"float32": torch.float32, "float64": torch.float64, "int32": torch.int32,
-                           "bfloat16": torch.bfloat16, "int8": torch.int8, "uint8": torch.uint8}
+                           "bfloat16": torch.bfloat16, "int8": torch.int8, "uint8": torch.uint8,
+                           "int64": torch.int64}
     return _modules[0]
 
 
@@ -965,6 +980,315 @@ def dense_bwd(x, W, dy, z=None, act: str = "none", want=("dx", "dW", "db"), dx=N
                               None if dW is None else dW.data_ptr(), None if db is None else db.data_ptr(),
                               *_scratch(ws), M, K, N, _stream(stream)), "e3_dense_bwd")
     return dx, dW, db
+
+
+def _here(*tensors):
+    """Launches go to the current device: every tensor has to be there."""
+    global _current
+    if _current is None:
+        _stream(None)
+    device = _current[1]()
+    for t in tensors:
+        if t is None:
+            continue
+        try:
+            at = t.get_device()
+        except AttributeError:
+            raise TypeError(f"expected a torch tensor, got {type(t).__name__}") from None
+        if at != device:
+            raise ValueError("tensors must be on the GPU" if at < 0 else
+                             f"a tensor is on GPU {at}, the current device is {device}")
+
+
+# ---------------------------------------------------------------- gated dense layers
+@functools.lru_cache(maxsize=1024)
+def gated_workspace_size(M: int, K: int, N: int, dtype="float32"):
+    """Bytes of (forward, backward) of a gated dense layer with x [M, K] and W [K, 2 N]."""
+    f, b = ct.c_size_t(), ct.c_size_t()
+    _check(lib().e3_gated_workspace_size({"float32": 0, "bfloat16": 1}[dtype], M, K, N, ct.byref(f), ct.byref(b)),
+           "e3_gated_workspace_size")
+    return f.value, b.value
+
+
+def _gated_width(W, K):
+    """N of W [K, 2 N]."""
+    k, n2 = _matrix(W, "W")
+    if k != K or n2 % 2:
+        raise ValueError(f"W has shape {(k, n2)}, expected {K} rows and an even number of columns")
+    return n2 // 2
+
+
+@_on_stream
+def gated_fwd(x, W, bias=None, act: str = "silu", keep=(), out=None, ws=None, stream=None):
+    """y = act(g) u with [g | u] = x W + bias, x [M, K], W [K, 2 N], bias [2 N], y [M, N].
+
+    keep adds to the result, in this order: "z" (z [M, 2 N], its rows g and u side by side), "z8" (a
+    pair: g and u as a Packed8 each), "y8" (y as a Packed8).  z and the pair are what gated_bwd takes.
+    """
+    code, dt = _layer_dtype(x, "x")
+    M, K = _matrix(x, "x")
+    N = _gated_width(W, K)
+    keep = _keep_of(keep, ("z", "z8", "y8"))
+    shape = (M, N)
+    y = x.new_empty(shape) if out is None else out
+    _here(x, W, bias, y, ws)
+    got, z, zp, yp = [y], None, (None,) * 4, (None, None)
+    if "z" in keep:
+        got.append(x.new_empty((M, 2 * N)))
+        z = got[-1].data_ptr()
+    if "z8" in keep:
+        got.append((Packed8.empty(M, N), Packed8.empty(M, N)))
+        zp = (*_packed(got[-1][0], "z8", shape), *_packed(got[-1][1], "z8", shape))
+    if "y8" in keep:
+        got.append(Packed8.empty(M, N))
+        yp = _packed(got[-1], "y8", shape)
+    if ws is None:
+        nb = gated_workspace_size(M, K, N, dt)[0]
+        ws = workspace(nb) if nb else None
+    _check(lib().e3_gated_fwd(code, *_rows(x, "x", (M, K), dt), _ptr(W, "W", (K, 2 * N), dt),
+                              None if bias is None else _ptr(bias, "bias", (2 * N,), dt), _act_code(act),
+                              *_rows(y, "out", shape, dt), z, 2 * N, *zp, *yp, *_scratch(ws), M, K, N, _stream(stream)),
+           "e3_gated_fwd")
+    return tuple(got) if keep else y
+
+
+@_on_stream
+def gated_bwd(x, W, dy, z, act: str = "silu", want=("dx", "dW", "db"), dx=None, ws=None, stream=None):
+    """(dx, dW, db) of a gated dense layer from dy and the forward's x (a tensor or a Packed8) and z (a tensor
+    [M, 2 N], or the pair of "z8"); cotangents not in `want` are not computed (None).  x is needed for dW only."""
+    code, dt = _layer_dtype(dy, "dy")
+    M, N = shape = _matrix(dy, "dy")
+    K = _matrix(W, "W")[0]
+    if _gated_width(W, K) != N:
+        raise ValueError(f"W has shape {tuple(W.shape)}, expected {2 * N} columns")
+    want = _keep_of(want, ("dx", "dW", "db"))
+    if "dx" in want and dx is None:
+        dx = dy.new_empty((M, K))
+    dW = dy.new_empty((K, 2 * N)) if "dW" in want else None
+    db = dy.new_empty((2 * N,)) if "db" in want else None
+    if ws is None:
+        ws = workspace(gated_workspace_size(M, K, N, dt)[1])
+    xp = (None, K, None, None) if x is None else _kept(x, "x", (M, K), dt)
+    if isinstance(z, (tuple, list)):
+        if len(z) != 2:
+            raise ValueError("z must be a tensor or a pair of Packed8")
+        zp = (None, 2 * N, *_packed(z[0], "z[0]", shape), *_packed(z[1], "z[1]", shape))
+        _here(W, dy, dx, ws, x.q if isinstance(x, Packed8) else x, z[0].q, z[0].c, z[1].q, z[1].c)
+    else:
+        zp = (*_rows(z, "z", (M, 2 * N), dt), None, None, None, None)
+        _here(W, dy, dx, ws, x.q if isinstance(x, Packed8) else x, z)
+    _check(lib().e3_gated_bwd(code, *xp, _ptr(W, "W", (K, 2 * N), dt), *zp, _act_code(act), *_rows(dy, "dy", shape, dt),
+                              *((None, K) if dx is None else _rows(dx, "dx", (M, K), dt)),
+                              None if dW is None else dW.data_ptr(), None if db is None else db.data_ptr(),
+                              *_scratch(ws), M, K, N, _stream(stream)), "e3_gated_bwd")
+    return dx, dW, db
+
+
+# ---------------------------------------------------------------- dropout and residual norms
+class Dropout:
+    """What a dropout mask is made of: the probability p, a seed, an offset (both 0 to 2^64 - 1), and a counter,
+    an int64 tensor of one element on the GPU whose value is added to the offset when a kernel runs (None: 0).
+
+    The mask of a call is a function of these and of each value's row and column alone (the formula: e3_dropout_fwd
+    in e3mi.h), so that a backward with an equal Dropout has its forward's mask.  Calls that shall have masks of their
+    own take another seed or offset.  A captured graph draws another mask in each replay if the program counts the
+    counter up in between.
+    """
+
+    __slots__ = ("p", "seed", "offset", "counter")
+
+    def __init__(self, p: float, seed: int, offset: int = 0, counter=None):
+        if not 0.0 <= p <= 1.0:
+            raise ValueError(f"p must lie in [0, 1], got {p}")
+        for v, name in ((seed, "seed"), (offset, "offset")):
+            if not 0 <= v < 1 << 64:
+                raise ValueError(f"{name} must lie in [0, 2^64), got {v}")
+        self.p, self.seed, self.offset, self.counter = p, seed, offset, counter
+
+    def _args(self):
+        c = self.counter
+        if c is not None:
+            _here(c)
+            c = _ptr(c, "counter", (1,) if c.dim() else (), "int64")
+        return self.p, self.seed, self.offset, c
+
+
+_NO_DROP = (0.0, 0, 0, None)
+
+
+def _drop_args(drop):
+    if drop is None:
+        return _NO_DROP
+    if not isinstance(drop, Dropout):
+        raise TypeError("drop must be a Dropout")
+    return drop._args()
+
+
+@_on_stream
+def dropout_fwd(x, drop, res=None, out=None, stream=None):
+    """y = res + keep x / (1 - p) with the mask of drop (a Dropout), x and res [rows, cols]; out may be x or res."""
+    code, dt = _layer_dtype(x, "x")
+    m, n = shape = _matrix(x, "x")
+    if not isinstance(drop, Dropout):
+        raise TypeError("drop must be a Dropout")
+    y = x.new_empty(shape) if out is None else out
+    _here(x, res, y)
+    _check(lib().e3_dropout_fwd(code, *_rows(x, "x", shape, dt),
+                                *((None, n) if res is None else _rows(res, "res", shape, dt)), *drop._args(),
+                                *_rows(y, "out", shape, dt), m, n, _stream(stream)), "e3_dropout_fwd")
+    return y
+
+
+@_on_stream
+def dropout_bwd(dy, drop, dx=None, stream=None):
+    """dx = keep dy / (1 - p), from the Dropout of the forward; dx may be dy.  The residual's cotangent is dy."""
+    code, dt = _layer_dtype(dy, "dy")
+    m, n = shape = _matrix(dy, "dy")
+    if not isinstance(drop, Dropout):
+        raise TypeError("drop must be a Dropout")
+    dx = dy.new_empty(shape) if dx is None else dx
+    _here(dy, dx)
+    _check(lib().e3_dropout_bwd(code, *_rows(dy, "dy", shape, dt), *drop._args(), *_rows(dx, "dx", shape, dt), m, n,
+                                _stream(stream)), "e3_dropout_bwd")
+    return dx
+
+
+NORMS = {"rms": 0, "layer": 1}
+
+
+def _norm_code(norm):
+    code = NORMS.get(norm)
+    if code is None:
+        raise ValueError(f"norm: {norm!r} is none of {', '.join(NORMS)}")
+    return code
+
+
+def _norm_weights(w, name, norm, n, dt):
+    """(gamma, beta) pointers of a norm's weights: None (no norm) or a pair whose entries may be None."""
+    if w is None:
+        return None, None
+    if not isinstance(w, (tuple, list)) or len(w) != 2:
+        raise TypeError(f"{name} must be None or a pair (gamma, beta)")
+    g, b = w
+    if norm == "rms" and b is not None:
+        raise ValueError(f"{name}: an rms norm has no beta")
+    _here(g, b)
+    return (None if g is None else _ptr(g, name + " gamma", (n,), dt),
+            None if b is None else _ptr(b, name + " beta", (n,), dt))
+
+
+def _gate(gate, shape, dt):
+    """(pointer, row stride) of a gate: none, a vector (stride 0) or a matrix."""
+    if gate is None:
+        return None, 0
+    if isinstance(gate, _torch().Tensor) and gate.dim() == 1:
+        return _ptr(gate, "gate", (shape[1],), dt), 0
+    return _rows(gate, "gate", shape, dt)
+
+
+@_on_stream
+def residual_norm_fwd(h, res=None, gate=None, scale: float = 1.0, norm: str = "rms", post=None, pre=None,
+                      eps: float = 1e-5, drop=None, keep=(), out=None, y=None, stream=None):
+    """s = res + scale gate drop(N1(h)) and y = N2(s), in one pass over the rows of h [rows, cols].
+
+    post, pre: the weights (gamma, beta) of N1 (the norm after a block) and N2 (the one before the next); an
+    entry may be None (1, 0), and instead of a pair None leaves the norm out.  norm: "rms" (x / sqrt(mean x^2 +
+    eps) gamma, no beta) or "layer", for both.  gate: None, [cols] or [rows, cols].  drop: a Dropout.  out (s; may
+    be res) and y are written where they are given.
+
+    Returns s, with pre (s, y); keep=("stats",) adds the statistics that the backward takes, float32 rows of
+    [n, rows]: for each norm that is there its rstd, before it (layer) its mean.
+    """
+    code, dt = _layer_dtype(h, "h")
+    m, n = shape = _matrix(h, "h")
+    keep = _keep_of(keep, ("stats",))
+    kind = _norm_code(norm)
+    s = h.new_empty(shape) if out is None else out
+    if pre is None and y is not None:
+        raise ValueError("y is the output of the norm that pre names")
+    if pre is not None and y is None:
+        y = h.new_empty(shape)
+    _here(h, res, gate, s, y)
+    p = [None] * 4
+    stats = None
+    if keep:
+        stats = _empty(((1 + kind) * ((post is not None) + (pre is not None)), m))
+        at, step = stats.data_ptr(), 4 * m
+        for k, w in ((0, post), (2, pre)):
+            if w is not None and m:
+                if kind:
+                    p[k], at = at, at + step
+                p[k + 1], at = at, at + step
+    _check(lib().e3_residual_norm_fwd(
+        code, kind, (post is not None) + 2 * (pre is not None), *_rows(h, "h", shape, dt),
+        *((None, n) if res is None else _rows(res, "res", shape, dt)), *_gate(gate, shape, dt), scale, *_drop_args(drop),
+        *_norm_weights(post, "post", norm, n, dt), *_norm_weights(pre, "pre", norm, n, dt), eps,
+        *_rows(s, "out", shape, dt), *((None, n) if y is None else _rows(y, "y", shape, dt)), *p, m, n,
+        _stream(stream)), "e3_residual_norm_fwd")
+    got = (s,) if y is None else (s, y)
+    return (*got, stats) if keep else got if y is not None else s
+
+
+@functools.lru_cache(maxsize=1024)
+def residual_norm_workspace_size(rows: int, cols: int, dtype="float32") -> int:
+    b = ct.c_size_t()
+    _check(lib().e3_residual_norm_workspace_size({"float32": 0, "bfloat16": 1}[dtype], rows, cols, ct.byref(b)),
+           "e3_residual_norm_workspace_size")
+    return b.value
+
+
+@_on_stream
+def residual_norm_bwd(h, s, stats, dy=None, ds=None, gate=None, scale: float = 1.0, norm: str = "rms", post=None,
+                      pre=None, drop=None, want=("dres", "dh", "dgate", "dpost", "dpre"), dres=None, dh=None, ws=None,
+                      stream=None):
+    """(dres, dh, dgate, dpost, dpre) from the cotangents dy of y and ds of s (None: 0; with pre, dy is needed)
+    and the forward's h, s (needed with pre), statistics and arguments.  dpost and dpre are pairs (dgamma, dbeta);
+    what was not there (a gate, a norm, a weight that was None) or is not in `want` is None.  h is needed for
+    the norm after the block and for dgate."""
+    ref = dy if dy is not None else ds
+    if ref is None:
+        raise ValueError("dy or ds must be given")
+    if (dy is None) != (pre is None):
+        raise ValueError("dy is the cotangent of the norm that pre names")
+    code, dt = _layer_dtype(ref, "dy" if dy is not None else "ds")
+    m, n = shape = _matrix(ref, "dy" if dy is not None else "ds")
+    want = _keep_of(want, ("dres", "dh", "dgate", "dpost", "dpre"))
+    kind = _norm_code(norm)
+    if "dres" in want and dres is None:
+        dres = ref.new_empty(shape)
+    if "dh" in want and dh is None:
+        dh = ref.new_empty(shape)
+    dgate = ref.new_empty(gate.shape) if gate is not None and "dgate" in want else None
+    grads = []
+    for w, name in ((post, "dpost"), (pre, "dpre")):
+        wanted = w is not None and name in want
+        grads.append(tuple(ref.new_empty((n,)) if wanted and v is not None else None for v in (w or (None, None))))
+    vectors = [v for g in grads for v in g]
+    weights = (*_norm_weights(post, "post", norm, n, dt), *_norm_weights(pre, "pre", norm, n, dt))
+    if ws is None and (any(v is not None for v in vectors) or (dgate is not None and dgate.dim() == 1)):
+        ws = workspace(residual_norm_workspace_size(m, n, dt))
+    _here(h, s, stats, dy, ds, gate, dres, dh, ws)
+    count = (1 + kind) * ((post is not None) + (pre is not None))
+    p = [None] * 4
+    if count:
+        at, step = _ptr(stats, "stats", (count, m)), 4 * m
+        for k, w in ((0, post), (2, pre)):
+            if w is not None and m:
+                if kind:
+                    p[k], at = at, at + step
+                p[k + 1], at = at, at + step
+    none = (None, n)
+    _check(lib().e3_residual_norm_bwd(
+        code, kind, (post is not None) + 2 * (pre is not None), *(none if h is None else _rows(h, "h", shape, dt)),
+        *(none if s is None or pre is None else _rows(s, "s", shape, dt)), *_gate(gate, shape, dt), scale,
+        *_drop_args(drop), *weights[:3], *p, *(none if dy is None else _rows(dy, "dy", shape, dt)),
+        *(none if ds is None else _rows(ds, "ds", shape, dt)), *(none if dres is None else _rows(dres, "dres", shape, dt)),
+        *(none if dh is None else _rows(dh, "dh", shape, dt)), None if dgate is None else dgate.data_ptr(), n,
+        *(None if v is None else v.data_ptr() for v in vectors), *_scratch(ws), m, n, _stream(stream)),
+        "e3_residual_norm_bwd")
+    post_grads, pre_grads = (g if w is not None and name in want else None
+                             for g, w, name in ((grads[0], post, "dpost"), (grads[1], pre, "dpre")))
+    return dres, dh, dgate, post_grads, pre_grads
 
 
 # ---------------------------------------------------------------- instrumentation

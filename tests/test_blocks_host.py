@@ -1,0 +1,147 @@
+"""Argument checks of the gated layers', dropout's and the residual norms' C entry points: every refusal is made
+before device work."""
+import ctypes as ct
+
+import pytest
+
+from paper_2609_35099_amd import e3mi
+
+P = ct.c_void_p(4096)      # never dereferenced: the calls below are refused first
+ODD = ct.c_void_p(4097)
+HALF = ct.c_void_p(4098)   # aligned for bfloat16 only
+FOUR = ct.c_void_p(4100)
+F32, BF16 = 0, 1
+OK, INVALID, SMALL = 0, 1, 4
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module")
+def L():
+    return e3mi.lib()
+
+
+def _gated_sizes(L, *args):
+    f, b = ct.c_size_t(), ct.c_size_t()
+    assert L.e3_gated_workspace_size(*args, ct.byref(f), ct.byref(b)) == OK
+    return f.value, b.value
+
+
+def test_gated_refusals(L):
+    f, b = ct.c_size_t(), ct.c_size_t()
+    for args in ((3, 1, 1, 1), (F32, -1, 1, 1), (F32, 1, 0, 1), (F32, 1, 1, 0), (F32, 1, 1, (1 << 19) + 1),
+                 (F32, 1, (1 << 20) + 1, 1), (F32, (1 << 40) + 1, 1, 1)):
+        assert L.e3_gated_workspace_size(*args, ct.byref(f), ct.byref(b)) == INVALID, args
+    assert L.e3_gated_workspace_size(F32, 1, 1, 1, None, ct.byref(b)) == INVALID
+    assert L.e3_gated_workspace_size(F32, 1, 1, 1, ct.byref(f), None) == INVALID
+    assert _gated_sizes(L, BF16, 0, 64, 64) == (0, 0)
+
+    def fwd(dtype=F32, x=P, ldx=8, W=P, bias=P, act=2, y=P, ldy=8, z=None, ldz=16, gq=None, gc=None, uq=None, uc=None,
+            yq=None, yc=None, M=4, K=8, N=8):
+        return L.e3_gated_fwd(dtype, x, ldx, W, bias, act, y, ldy, z, ldz, gq, gc, uq, uc, yq, yc, P, 1 << 40, M, K, N, None)
+    for kw in ({"x": None}, {"W": None}, {"y": None}, {"ldx": 7}, {"ldy": 7}, {"z": P, "ldz": 15}, {"act": 4}, {"act": -1},
+               {"gq": P}, {"gc": P}, {"gq": P, "gc": P}, {"uq": P, "uc": P}, {"gq": P, "gc": P, "uq": P}, {"yq": P},
+               {"yc": P}, {"x": HALF}, {"W": ODD}, {"bias": HALF}, {"y": ODD}, {"z": HALF}, {"K": 0}, {"N": 0}, {"M": -1},
+               {"dtype": 7}, {"dtype": BF16, "x": ODD}):
+        assert fwd(**kw) == INVALID, kw
+    assert fwd(M=0, x=None, y=None, W=None) == OK
+
+    nb = _gated_sizes(L, F32, 4, 8, 8)[1]
+    assert nb >= 4 * 16 * 4          # dz
+
+    def bwd(dtype=F32, x=P, ldx=8, xq=None, xc=None, W=P, z=P, ldz=16, gq=None, gc=None, uq=None, uc=None, act=2, dy=P,
+            lddy=8, dx=P, lddx=8, dW=P, db=P, ws=P, nb=nb, M=4, K=8, N=8):
+        return L.e3_gated_bwd(dtype, x, ldx, xq, xc, W, z, ldz, gq, gc, uq, uc, act, dy, lddy, dx, lddx, dW, db, ws, nb, M,
+                              K, N, None)
+    pair = {"gq": P, "gc": P, "uq": P, "uc": P}
+    for kw in ({"x": None}, {"xq": P, "xc": P}, {"xq": P}, {"W": None}, {"z": None}, pair, {**pair, "z": None, "uc": None},
+               {"z": None, "gq": P, "gc": P}, {"dy": None}, {"act": 5}, {"ldx": 7}, {"ldz": 15}, {"lddy": 7}, {"lddx": 7},
+               {"dx": ODD}, {"dW": HALF}, {"db": HALF}, {"K": 0}, {"M": -1}, {"ws": None}, {"ws": ct.c_void_p(4104)}):
+        assert bwd(**kw) == INVALID, kw
+    assert bwd(nb=nb - 1) == SMALL
+    assert bwd(dx=None, dW=None, db=None, ws=None, nb=0) == OK       # nothing asked for
+    assert bwd(M=0, dx=None, dW=None, db=None, x=None, dy=None, z=None, ws=None, nb=0) == OK
+
+
+@pytest.mark.parametrize("dtype,M,K,N", [(F32, 16, 1000, 250), (BF16, 16, 1000, 250), (F32, 300, 4100, 150)])
+def test_gated_forward_scratch_refusals(L, dtype, M, K, N):
+    """Sizes whose reduction is split: less scratch than asked for, none, or misaligned."""
+    need = _gated_sizes(L, dtype, M, K, N)[0]
+    assert need >= 2 * M * 2 * N * 4                    # two splits at least
+
+    def fwd(ws, nb):
+        return L.e3_gated_fwd(dtype, P, K, P, None, 2, P, N, None, 2 * N, None, None, None, None, None, None, ws, nb, M, K,
+                              N, None)
+    assert fwd(P, need - 1) == SMALL and fwd(P, 0) == SMALL and fwd(None, 0) == SMALL
+    for ws in (None, ODD, HALF):
+        assert fwd(ws, need) == INVALID, ws
+
+
+def test_gated_scratch_stays_near_the_tensors(L):
+    for dtype, e in ((F32, 4), (BF16, 2)):
+        for M in (1, 9, 100, 4097, 1_000_003):
+            for K in (1, 17, 300, 4099, 1 << 20):
+                for N in (1, 8, 65, 1027, 1 << 19):
+                    f, b = _gated_sizes(L, dtype, M, K, N)
+                    tensors = e * (M * K + 2 * K * N + M * N)
+                    assert f <= 16 * tensors + (64 << 20), (dtype, M, K, N, f)
+                    assert b <= 20 * tensors + (64 << 20), (dtype, M, K, N, b)
+
+
+def test_dropout_refusals(L):
+    def fwd(dtype=F32, x=P, ldx=8, r=P, ldr=8, p=0.5, counter=P, y=P, ldy=8, rows=4, cols=8):
+        return L.e3_dropout_fwd(dtype, x, ldx, r, ldr, p, 1, 2, counter, y, ldy, rows, cols, None)
+
+    def bwd(dtype=F32, x=P, ldx=8, p=0.5, counter=P, y=P, ldy=8, rows=4, cols=8):
+        return L.e3_dropout_bwd(dtype, x, ldx, p, 1, 2, counter, y, ldy, rows, cols, None)
+    for call in (fwd, bwd):
+        for kw in ({"dtype": 2}, {"x": None}, {"y": None}, {"ldx": 7}, {"ldy": 7}, {"p": -0.1}, {"p": 1.1}, {"p": NAN},
+                   {"counter": FOUR}, {"x": HALF}, {"y": ODD}, {"rows": -1}, {"cols": 0}, {"cols": (1 << 20) + 1},
+                   {"rows": (1 << 40) + 1}):
+            assert call(**kw) == INVALID, kw
+        assert call(rows=0, x=None, y=None) == OK
+    assert fwd(ldr=7) == INVALID and fwd(r=HALF) == INVALID
+
+
+def test_residual_norm_refusals(L):
+    RMS, LAYER, AFTER, BEFORE = 0, 1, 1, 2
+
+    def fwd(dtype=F32, norm=LAYER, where=AFTER | BEFORE, h=P, ldh=8, r=P, ldr=8, gate=P, ldg=8, scale=1.0, p=0.1,
+            counter=None, g1=P, b1=P, g2=P, b2=P, eps=1e-5, s=P, lds=8, y=P, ldy=8, m1=P, r1=P, m2=P, r2=P, rows=4, cols=8):
+        return L.e3_residual_norm_fwd(dtype, norm, where, h, ldh, r, ldr, gate, ldg, scale, p, 1, 2, counter, g1, b1, g2, b2,
+                                      eps, s, lds, y, ldy, m1, r1, m2, r2, rows, cols, None)
+    for kw in ({"dtype": 3}, {"norm": 2}, {"norm": -1}, {"where": 4}, {"h": None}, {"y": None}, {"ldh": 7}, {"ldr": 7},
+               {"ldg": 7}, {"ldg": -1}, {"lds": 7}, {"ldy": 7}, {"eps": -1.0}, {"eps": NAN}, {"scale": NAN}, {"p": 2.0},
+               {"p": NAN}, {"counter": FOUR}, {"norm": RMS}, {"norm": RMS, "b1": None}, {"where": AFTER},
+               {"where": AFTER, "y": None}, {"where": BEFORE}, {"where": AFTER, "y": None, "g2": None, "b2": None, "s": None},
+               {"where": AFTER, "g2": None, "b2": None}, {"h": HALF}, {"r": ODD}, {"gate": HALF}, {"g1": ODD}, {"b1": HALF},
+               {"g2": HALF}, {"b2": ODD}, {"s": HALF}, {"y": HALF}, {"m1": HALF}, {"r1": ODD}, {"m2": HALF}, {"r2": HALF},
+               {"rows": -1}, {"cols": 0}):
+        assert fwd(**kw) == INVALID, kw
+    assert fwd(rows=0, h=None, s=None, y=None) == OK
+
+    n = ct.c_size_t()
+    assert L.e3_residual_norm_workspace_size(F32, 100, 33, ct.byref(n)) == OK and n.value >= 5 * 33 * 4
+    assert L.e3_residual_norm_workspace_size(F32, 0, 33, ct.byref(n)) == OK and n.value == 0
+    assert L.e3_residual_norm_workspace_size(F32, 1, 33, None) == INVALID
+    assert L.e3_residual_norm_workspace_size(F32, -1, 33, ct.byref(n)) == INVALID
+    L.e3_residual_norm_workspace_size(F32, 4, 8, ct.byref(n))
+
+    def bwd(dtype=F32, norm=LAYER, where=AFTER | BEFORE, h=P, ldh=8, s=P, lds=8, gate=P, ldg=8, scale=1.0, p=0.1,
+            counter=None, g1=P, b1=P, g2=P, m1=P, r1=P, m2=P, r2=P, dy=P, lddy=8, ds=P, ldds=8, dr=P, lddr=8, dh=P, lddh=8,
+            dgate=P, lddg=8, dg1=P, db1=P, dg2=P, db2=P, ws=P, nb=n.value, rows=4, cols=8):
+        return L.e3_residual_norm_bwd(dtype, norm, where, h, ldh, s, lds, gate, ldg, scale, p, 1, 2, counter, g1, b1, g2, m1,
+                                      r1, m2, r2, dy, lddy, ds, ldds, dr, lddr, dh, lddh, dgate, lddg, dg1, db1, dg2, db2,
+                                      ws, nb, rows, cols, None)
+    one = {"where": AFTER, "s": None, "g2": None, "dg2": None, "db2": None, "dy": None}
+    for kw in ({"dtype": 3}, {"norm": 5}, {"where": 7}, {"h": None}, {"s": None}, {"dy": None}, {"m1": None}, {"r1": None},
+               {"m2": None}, {"r2": None}, {"ldh": 7}, {"lds": 7}, {"ldg": 7}, {"lddy": 7}, {"ldds": 7}, {"lddr": 7},
+               {"lddh": 7}, {"lddg": 7}, {"gate": None}, {"norm": RMS}, {"norm": RMS, "b1": None, "db1": None}, {"where": AFTER},
+               {"where": BEFORE}, {**one, "ds": None}, {**one, "dy": P}, {"ws": None}, {"ws": HALF}, {"scale": NAN}, {"p": -1.0},
+               {"counter": FOUR}, {"h": HALF}, {"s": HALF}, {"gate": ODD}, {"dy": HALF}, {"ds": ODD}, {"dr": HALF}, {"dh": ODD},
+               {"dgate": HALF}, {"dg1": ODD}, {"db1": HALF}, {"dg2": HALF}, {"db2": ODD}, {"m2": HALF}, {"r1": ODD},
+               {"rows": -1}, {"cols": 0}):
+        assert bwd(**kw) == INVALID, kw
+    assert bwd(nb=n.value - 1) == SMALL
+    nothing = {"dr": None, "dh": None, "dgate": None, "dg1": None, "db1": None, "dg2": None, "db2": None, "ws": None, "nb": 0}
+    assert bwd(**nothing) == OK
+    assert bwd(rows=0, **nothing) == OK
