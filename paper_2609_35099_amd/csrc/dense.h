@@ -1,7 +1,7 @@
 // Dense layers, shared by their units: arguments, the epilogue, the tile kernel
 // and how a product is cut.
 #pragma once
-#include "dense_tile.h"
+#include "dense_direct.h"
 
 // A backward call, checked.
 struct DenseBwdCall {
@@ -262,6 +262,29 @@ __global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void 
   using Tl = typename TileOf<J, B>::type;
   __shared__ __align__(16) typename Tl::Shared sh;
   dense_block<J, Tl, TileOf<J, B>::BM, TileOf<J, B>::BN>(a, sh, block_id());
+}
+// bfloat16 with operands straight to LDS.
+template <class J>
+__global__ __launch_bounds__(512, 2) void k_dense_direct(DenseArgs a) {
+  using Tl = DirectTile<J::FA, J::FB>;
+  static_assert(sizeof(typename J::T) == 2 && J::KA == kFull && J::KB == kFull && !J::SUM);
+  __shared__ __align__(16) typename Tl::Buf s0, s1;
+  const int64_t tm = (a.rows + Tl::BM - 1) / Tl::BM;
+  const int tn = (a.cols + Tl::BN - 1) / Tl::BN;
+  int64_t u = block_id();
+  if (u >= tm * tn * a.splits) return;
+  const int split = (int)(u / (tm * tn));
+  u -= split * (tm * tn);
+  const TileAt at = tile_at(u, tm, tn);
+  const int64_t r0 = at.m * Tl::BM;
+  const int c0 = at.n * Tl::BN;
+  const int64_t k0 = split * a.chunk, end = k0 + a.chunk < a.red ? k0 + a.chunk : a.red;
+  Tl t;
+  t.run(s0, s1, a.a, a.b, r0, a.rows, c0, a.cols, k0, end);
+  auto* out = Tl::stage(s0, s1);
+  each_of([&](auto i) {
+    rows32_out<J, Tl::RN>(a, split, r0 + Tl::row0() + 32 * i, c0 + Tl::col0(), k0, end, out, t.acc[i]);
+  }, std::make_integer_sequence<int, Tl::RM>{});
 }
 // Short reductions (up to 16 KK) over many rows: no LDS and no barriers before the
 // epilogue.  A wave keeps the terms of its 32 NC columns of B in registers for
@@ -725,6 +748,16 @@ e3_status dense_launch(const DenseArgs& a, const Cut& c, const Names& names, hip
   const dim3 grid = grid_of(c.tiles * c.splits);
   // (packed gradient operands never get there: forms_dz; dW takes such tiles past
   // 128 columns of dz and 1e8 values of it)
+  if constexpr (sizeof(typename J::T) == 2 && J::KA == kFull && J::KB == kFull && !J::SUM) {
+    if (c.tile == 256 && a.red % 64 == 0 && direct_side(a.a, J::FA == kAlong ? 8 : a.rows) &&
+        direct_side(a.b, J::FB == kAlong ? 8 : a.cols)) {
+      using Tl = DirectTile<J::FA, J::FB>;
+      const int64_t tiles = (a.rows + Tl::BM - 1) / Tl::BM * ((a.cols + Tl::BN - 1) / Tl::BN);
+      hipLaunchKernelGGL(k_dense_direct<J>, grid_of(tiles * c.splits), dim3(Tl::THREADS), 0, st, a);
+      E3_HIP(hipGetLastError());
+      return E3_OK;
+    }
+  }
   if constexpr (sizeof(typename J::T) == 2 && J::KA != kGradPacked && J::KB != kGradPacked) {
     if (c.tile == 256) {
       hipLaunchKernelGGL((k_dense<J, 256>), grid, dim3(TileOf<J, 256>::THREADS), 0, st, a);

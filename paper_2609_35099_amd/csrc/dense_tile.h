@@ -60,8 +60,8 @@ struct Side {
 
 // LDS planes of R rows (or columns) by BK reduction indexes.  16-byte slots are
 // exchanged so that the lanes of one pass of a read cover all banks: along, by
-// the row's number among those that share the banks; across, the pairs of slots
-// of the four rows that one transposing read takes.
+// the row's number among those that share the banks; across, the four slots of each of
+// the four rows that half a wave's transposing read takes.
 template <Form F, int R, int BK, int P>
 struct Plane {
   static constexpr int W = F == kAlong ? BK : R;          // values of an LDS row
@@ -69,7 +69,7 @@ struct Plane {
   static constexpr int kShare = F == kAlong ? (S >= 16 ? 1 : 16 / S) : 1;  // rows over all banks
   unsigned short v[P][R * BK];
   static __device__ __forceinline__ int off(int row, int slot) {
-    const int x = F == kAlong ? (row / kShare) & (S - 1 < 15 ? S - 1 : 15) : (2 * (row & 3)) & (S - 1);
+    const int x = F == kAlong ? (row / kShare) & (S - 1 < 15 ? S - 1 : 15) : S >= 16 ? 4 * (row & 3) : 4 * (row / 2 & 1);
     return row * W + ((slot ^ x) * 8);
   }
   // The fragment of rows (columns) r0 + l % 32 at reduction indexes k0 + 8 (l / 32) on.

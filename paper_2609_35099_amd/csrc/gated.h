@@ -157,6 +157,23 @@ __global__ __launch_bounds__((GatedTileOf<T, B>::THREADS), (GatedTileOf<T, B>::O
   t.finish(sh, [&](int r, int c, auto out, auto& acc) { gated_rows32<T, Tl::RN>(a, r0 + r, c0 + c / 2, out, acc); });
 }
 
+// bfloat16 with operands straight to LDS.
+__global__ __launch_bounds__(512, 2) void k_gated_direct(GatedArgs a) {
+  using Tl = DirectTile<kAlong, kPaired>;
+  __shared__ __align__(16) Tl::Buf s0, s1;
+  const int64_t tm = (a.rows + Tl::BM - 1) / Tl::BM, u = block_id();
+  const int tn = (a.cols + Tl::BN / 2 - 1) / (Tl::BN / 2);
+  if (u >= tm * tn) return;
+  const TileAt at = tile_at(u, tm, tn);
+  const int64_t r0 = at.m * Tl::BM;
+  const int c0 = at.n * (Tl::BN / 2);
+  Tl t;
+  t.run(s0, s1, a.a, a.b, r0, a.rows, c0, a.cols, 0, a.red);
+  auto* out = Tl::stage(s0, s1);
+  each_of([&](auto i) { gated_rows32<__bf16, 2>(a, r0 + Tl::row0() + 32 * i, c0 + Tl::col0() / 2, out, t.acc[i]); },
+          std::make_integer_sequence<int, Tl::RM>{});
+}
+
 // Short reductions over many rows, as k_dense_panel: a wave keeps the terms of 32
 // columns of g and of u and walks row blocks.
 template <class T, int KK, bool FAST>
@@ -439,6 +456,15 @@ e3_status gated_fwd(const GatedCall& c) {
     }
     case GatedWay::tile: {
       const int b = dense_cut(t, c.M, 2 * c.N, c.K, kForward).tile;
+      if constexpr (t == E3_BF16) {
+        if (b == 256 && c.K % 64 == 0 && direct_side(a.a, 8) && direct_side(a.b, c.N)) {
+          using Tl = DirectTile<kAlong, kPaired>;
+          TimedLaunch t_("gated_fwd_direct", c.st);
+          const int64_t tiles = (c.M + Tl::BM - 1) / Tl::BM * ((c.N + Tl::BN / 2 - 1) / (Tl::BN / 2));
+          hipLaunchKernelGGL(k_gated_direct, grid_of(tiles), dim3(Tl::THREADS), 0, c.st, a);
+          break;
+        }
+      }
       TimedLaunch t_(b == 64 ? "gated_fwd_64" : b == 128 ? "gated_fwd_128" : "gated_fwd_256", c.st);
       auto go = [&](auto B) {
         using O = GatedTileOf<T, decltype(B)::value>;

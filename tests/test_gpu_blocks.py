@@ -128,7 +128,8 @@ def test_gated_backward(e3, dt, M, K, N, gap, shift, f32, bf16, ckpt):  # noqa: 
 LARGE = [("float32", 262149, 64, 16, 0, "panel"), ("float32", 131077, 33, 40, 3, "panel"), ("float32", 300007, 8, 64, 0, "panel"),
          ("bfloat16", 262149, 128, 16, 0, "panel"), ("bfloat16", 262176, 64, 32, 0, "panel"), ("bfloat16", 150001, 90, 33, 1, "panel"),
          ("float32", 16403, 100, 300, 0, "128"), ("float32", 4096, 1100, 257, 1, "split_128"), ("bfloat16", 40003, 130, 129, 0, "128"),
-         ("bfloat16", 16400, 300, 800, 0, "256"), ("bfloat16", 16001, 515, 1021, 6, "256")]
+         ("bfloat16", 16400, 300, 800, 0, "256"), ("bfloat16", 16400, 320, 800, 0, "direct"), ("bfloat16", 33000, 64, 328, 8, "panel"),
+         ("bfloat16", 16387, 192, 1000, 8, "direct"), ("bfloat16", 16400, 320, 804, 0, "256"), ("bfloat16", 16400, 320, 800, 4, "256"), ("bfloat16", 16001, 515, 1021, 6, "256")]
 
 
 @pytest.mark.parametrize("dt,M,K,N,gap,name", LARGE)
@@ -162,6 +163,29 @@ def test_gated_large(e3, dt, M, K, N, gap, name):  # noqa: F811
     close(db, dz.sum(0), dt)
     cols = np.unique(np.concatenate([np.arange(min(5, 2 * N)), np.linspace(0, 2 * N - 1, 12).astype(int)]))
     close(dW[:, torch.from_numpy(cols).cuda()], host(x).T @ dzr[:, cols], dt)
+
+
+@pytest.mark.parametrize("M,K,N", [(16387, 320, 1608), (40003, 256, 520), (8200, 1088, 2056)])
+def test_products_past_the_registers_have_the_same_bits(e3, M, K, N):  # noqa: F811
+    """Large bfloat16 products whose rows are whole aligned pieces take another way to the same sums."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(M)
+    def rows(m, n, gap):
+        return torch.empty(m, n + gap, dtype=torch.bfloat16, device="cuda")[:, :n]
+    def aligned_and_not(m, n):
+        a = torch.randn(m, n, generator=g, device="cuda").bfloat16()
+        return a, rows(m, n, 1).copy_(a)
+    x, dy = aligned_and_not(M, K), aligned_and_not(M, N)
+    W = (torch.randn(K, N, generator=g, device="cuda") / 30).bfloat16()
+    b = torch.randn(N, generator=g, device="cuda").bfloat16()
+    assert torch.equal(e3.dense_fwd(x[0], W, b, act="gelu"), e3.dense_fwd(x[1], W, b, act="gelu"))
+    for u, v in zip(e3.dense_bwd(x[0], W, dy[0]), e3.dense_bwd(x[1], W, dy[1])):
+        assert torch.equal(u, v)
+    assert torch.equal(e3.gated_fwd(x[0], W), e3.gated_fwd(x[1], W))
+    ref = host(dy[0][:64]) @ host(W).T
+    close(e3.dense_bwd(None, W, dy[0], want=("dx",))[0][:64], ref, "bfloat16")
+    cols = slice(0, N, 61)
+    close(e3.dense_bwd(x[0], W, dy[0], want=("dW",))[1][:, cols], host(x[0]).T @ host(dy[0][:, cols]), "bfloat16")
 
 
 @pytest.mark.parametrize("M,K,N", [(3, 40, 50), (40, 12, 40), (200, 130, 70), (20, 1000, 50), (100000, 64, 40)])
