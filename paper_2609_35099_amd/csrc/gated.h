@@ -32,6 +32,8 @@ struct GatedCall {
 };
 e3_status gated_fwd_f32(const GatedCall& c);
 e3_status gated_fwd_bf16(const GatedCall& c);
+e3_status gated_bwd_fused_f32(const GatedCall& c);
+e3_status gated_bwd_fused_bf16(const GatedCall& c);
 
 namespace {
 
@@ -394,6 +396,14 @@ GatedWay gated_way(e3_dtype t, int64_t M, int64_t K, int64_t N) {
 size_t gated_fwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   if (M == 0 || gated_way(t, M, K, N) != GatedWay::split) return 0;
   return cut_bytes(dense_cut(t, M, 2 * N, K, kForward), M, 2 * N);
+}
+
+// Backward in one pass over the rows (gated_bwd.h): layers whose dW fits the registers of
+// a workgroup, from z in full.  (dy and x hold a piece at least.)
+bool gated_fused(int64_t M, int64_t K, int64_t N) { return K <= 64 && N <= 128 && M * K >= 8 && M * N >= 8; }
+// Its workgroups: one per CU, or two where the LDS of bfloat16 allows.
+int gated_fused_groups(e3_dtype t, int64_t M, int64_t, int64_t) {
+  return (int)std::min<int64_t>((M + 31) / 32, 256);
 }
 
 template <class T>

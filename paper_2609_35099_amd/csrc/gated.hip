@@ -75,12 +75,15 @@ GatedBwdWs gated_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   w.db = up256((size_t)w.blocks * 2 * N * 4);
   w.products = dense_bwd_ws(t, M, K, 2 * N).total;
   w.total = w.dz + w.db + w.products;
+  if (gated_fused(M, K, N))  // from z in full or packed
+    w.total = std::max(w.total, up256((size_t)gated_fused_groups(t, M, K, N) * (K * 2 * N + 2 * N) * 4));
   return w;
 }
 
 template <class T>
 e3_status gated_bwd(const GatedCall& c) {
   constexpr e3_dtype t = std::is_same_v<T, float> ? E3_F32 : E3_BF16;
+  if (gated_fused(c.M, c.K, c.N) && c.z_in) return t == E3_F32 ? gated_bwd_fused_f32(c) : gated_bwd_fused_bf16(c);
   const GatedBwdWs w = gated_bwd_ws(t, c.M, c.K, c.N);
   T* dz = reinterpret_cast<T*>(c.ws);
   float* part = reinterpret_cast<float*>(c.ws + w.dz);
