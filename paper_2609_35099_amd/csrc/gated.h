@@ -64,8 +64,8 @@ struct GatedTail {
     ld_piece<T>(static_cast<const T*>(a.bias) + col, a.cols - col, bg);
     ld_piece<T>(static_cast<const T*>(a.bias) + a.cols + col, a.cols - col, bu);
   }
-  // FAST: the piece is inside the row, y streams and is the only output (plain()).
-  template <bool FAST = false>
+  // FAST: the piece is inside the row, y is the only output (plain()).
+  template <bool FAST = false, bool NT = true>
   __device__ __forceinline__ void out(const GatedArgs& a, int64_t row, bool ok, int col, float (&g)[V],
                                       float (&u)[V]) const {
     const int n = FAST ? V : ok ? a.cols - col : 0;
@@ -85,11 +85,12 @@ struct GatedTail {
 #pragma unroll
     for (int i = 0; i < V; ++i) g[i] = Elem<T>::round(g[i] * u[i]);
     T* y = static_cast<T*>(a.y) + row * a.ldy + col;
-    if constexpr (FAST) __builtin_nontemporal_store(Elem<T>::put(g), reinterpret_cast<typename Elem<T>::vec*>(y));
+    if constexpr (FAST && NT) __builtin_nontemporal_store(Elem<T>::put(g), reinterpret_cast<typename Elem<T>::vec*>(y));
+    else if constexpr (FAST) *reinterpret_cast<typename Elem<T>::vec*>(y) = Elem<T>::put(g);
     else st_piece<T>(y, n, g, a.nt);
     if (!FAST && a.yq) pack(g, a.yq, a.yc);
   }
-  static bool plain(const GatedArgs& a) { return a.nt && !a.z && !a.gq && !a.yq; }
+  static bool plain(const GatedArgs& a) { return !a.z && !a.gq && !a.yq; }
 };
 
 // A sum again from memory, in float32 (half 0: g, 1: u).
@@ -105,7 +106,7 @@ __device__ __forceinline__ float gated_again(const GatedArgs& a, int64_t row, in
 
 // The results of rows row0 to row0 + 31 and 16 RN columns of y from col0 on: blocks
 // of 32 columns of g and of u in turn.
-template <class T, int RN, bool FAST = false>
+template <class T, int RN, bool FAST = false, bool NT = true>
 __device__ __forceinline__ void gated_rows32(const GatedArgs& a, int64_t row0, int col0, float (*out)[32 * RN + 4],
                                              const f16v (&acc)[RN]) {
   using R = Rows32<T, RN>;
@@ -129,7 +130,7 @@ __device__ __forceinline__ void gated_rows32(const GatedArgs& a, int64_t row0, i
       *reinterpret_cast<f4v*>(&g[e]) = *reinterpret_cast<const f4v*>(&out[r][at + e]);
       *reinterpret_cast<f4v*>(&u[e]) = *reinterpret_cast<const f4v*>(&out[r][at + 32 + e]);
     }
-    tail.template out<FAST>(a, row0 + r, FAST || row0 + r < a.rows, col0 + oc, g, u);
+    tail.template out<FAST, NT>(a, row0 + r, FAST || row0 + r < a.rows, col0 + oc, g, u);
   }
   __builtin_amdgcn_wave_barrier();
 }
@@ -178,7 +179,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_direct(GatedArgs a) {
 
 // Short reductions over many rows, as k_dense_panel: a wave keeps the terms of 32
 // columns of g and of u and walks row blocks.
-template <class T, int KK, bool FAST>
+template <class T, int KK, bool FAST, bool NT>
 __global__ __launch_bounds__(256, 2) void k_gated_panel(GatedArgs a) {
   using R = Rows32<T, 2>;
   constexpr bool f32 = sizeof(T) == 4;
@@ -199,8 +200,10 @@ __global__ __launch_bounds__(256, 2) void k_gated_panel(GatedArgs a) {
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
+        // (loaded without a branch, so that all are in flight: 64 waits took 20 us)
         const int at = 16 * k + h + e;
-        v[e] = at < K && col < a.cols ? Elem<T>::one(static_cast<const T*>(a.b.p)[at * a.b.ld + c * a.cols + col]) : 0.0f;
+        const T u = static_cast<const T*>(a.b.p)[imin(at, K - 1) * a.b.ld + c * a.cols + imin(col, a.cols - 1)];
+        v[e] = at < K && col < a.cols ? Elem<T>::one(u) : 0.0f;
         if (f32) v[e] *= kTermScale;
       }
 #pragma unroll
@@ -265,7 +268,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_panel(GatedArgs a) {
           for (int c = 0; c < 2; ++c)
             acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[q][k][c], xf[p][k], acc[c], 0, 0, 0);
         }
-    gated_rows32<T, 2, decltype(fast)::value>(a, block * 32, col0, out[wave], acc);
+    gated_rows32<T, 2, decltype(fast)::value, NT>(a, block * 32, col0, out[wave], acc);
   };
   // FAST: whole row blocks by a loop without branches around loads and stores, and
   // what is left of the rows after it
@@ -401,9 +404,14 @@ size_t gated_fwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
 // Backward in one pass over the rows (gated_bwd.h): layers whose dW fits the registers of
 // a workgroup, from z in full.  (dy and x hold a piece at least.)
 bool gated_fused(int64_t M, int64_t K, int64_t N) { return K <= 64 && N <= 128 && M * K >= 8 && M * N >= 8; }
-// Its workgroups: one per CU, or two where the LDS of bfloat16 allows.
-int gated_fused_groups(e3_dtype t, int64_t M, int64_t, int64_t) {
-  return (int)std::min<int64_t>((M + 31) / 32, 256);
+// Rows of its blocks: such that the workgroup's threads have a piece each (156,000 x 64 x
+// 64 bfloat16 36 us with 64 rows, 44 with 32; 100,003 x 64 x 128 48 and 41, six blocks
+// a workgroup rounded up or twelve).
+constexpr int gated_fused_rows(bool f32, int64_t N) { return N <= (f32 ? 32 : 64) ? 64 : 32; }
+// Its workgroups: one per CU.
+int gated_fused_groups(e3_dtype t, int64_t M, int64_t N) {
+  const int rows = gated_fused_rows(t == E3_F32, N);
+  return (int)std::min<int64_t>((M + rows - 1) / rows, 256);
 }
 
 template <class T>
@@ -416,7 +424,7 @@ e3_status gated_panel(GatedArgs a, hipStream_t st) {
   auto go = [&](auto KK) {
     constexpr int kk = decltype(KK)::value;
     const bool fast = a.red == 16 * kk && a.cols % 32 == 0 && GatedTail<T>::plain(a);
-    auto* k = fast ? k_gated_panel<T, kk, true> : k_gated_panel<T, kk, false>;
+    auto* k = !fast ? k_gated_panel<T, kk, false, false> : a.nt ? k_gated_panel<T, kk, true, true> : k_gated_panel<T, kk, true, false>;
     hipLaunchKernelGGL(k, grid_of(blocks), dim3(256), 0, st, a);
   };
   if (a.red <= 16) go(std::integral_constant<int, 1>{});

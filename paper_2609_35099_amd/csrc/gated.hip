@@ -76,7 +76,7 @@ GatedBwdWs gated_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   w.products = dense_bwd_ws(t, M, K, 2 * N).total;
   w.total = w.dz + w.db + w.products;
   if (gated_fused(M, K, N))  // from z in full or packed
-    w.total = std::max(w.total, up256((size_t)gated_fused_groups(t, M, K, N) * (K * 2 * N + 2 * N) * 4));
+    w.total = std::max(w.total, up256((size_t)gated_fused_groups(t, M, N) * (K * 2 * N + 2 * N) * 4));
   return w;
 }
 

@@ -3,7 +3,7 @@
 //
 //   dz = [dy u act'(g) | dy act(g)],  dx = dz W^T, dW = x^T dz, db = sum_rows dz
 //
-// dz never goes to memory: a workgroup takes blocks of 32 rows, writes their dz and x to
+// dz never goes to memory: a workgroup takes blocks of 32 or 64 rows, writes their dz and x to
 // LDS as terms (dense_tile.h), and its eight waves multiply both products from there,
 // dx's with the terms of W in registers for good, dW's into registers that stay for
 // all blocks; what is left is to add the workgroups' dW and db in order.  The next
@@ -48,16 +48,17 @@ __device__ __forceinline__ float gated_dz_value(const FusedArgs<T>& a, int64_t r
 template <class T, int KB, int NB, bool XQ>
 struct Fused {
   static constexpr bool f32 = sizeof(T) == 4;
-  static constexpr int V = Elem<T>::V, P = f32 ? 3 : 1, R = 32, NC = 64 * NB, KC = 32 * KB, WAVES = 8, THREADS = 512;
+  static constexpr int V = Elem<T>::V, P = f32 ? 3 : 1, R = gated_fused_rows(f32, 32 * NB), RB = R / 32, NC = 64 * NB, KC = 32 * KB, WAVES = 8, THREADS = 512;
   static constexpr float kBack = f32 ? kTermBack : 1.0f;
   // pieces of a row and of a thread
   static constexpr int PR = 32 * NB / V, NP = (R * PR + THREADS - 1) / THREADS;
   static constexpr int XR = KC / V, NX = (R * XR + THREADS - 1) / THREADS;
-  // dx: a wave takes one of KB blocks over DS of the NC / 16 reduction steps
-  static constexpr int STEPS = NC / 16, DS = STEPS * KB >= WAVES ? STEPS * KB / WAVES : 1;
-  // dW: blocks of 32 x 32; a wave takes DB of them, or one over part of the two steps
+  // dx: a wave takes one of RB KB blocks over DS of the NC / 16 reduction steps
+  static constexpr int STEPS = NC / 16, UNITS = RB * KB, DS = STEPS * UNITS >= WAVES ? STEPS * UNITS / WAVES : 1;
+  // dW: blocks of 32 x 32; a wave takes DB of them, or one over half of the R / 16 steps
   static constexpr int BLOCKS = KB * 2 * NB, DB = BLOCKS >= WAVES ? BLOCKS / WAVES : 1;
   static constexpr int DW_SPLIT = BLOCKS >= WAVES ? 1 : 2, DW_WAVES = BLOCKS / DB * DW_SPLIT;
+  static constexpr int DW_STEPS = 2 * RB / DW_SPLIT;
   struct Shared {
     unsigned short dz[P][R * NC];
     unsigned short x[P][R * KC];
@@ -120,16 +121,19 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
   __shared__ __align__(16) typename F::Shared sh;
   const int tid = threadIdx.x, l = tid % kWave, w = uniform(tid / kWave), K = a.K, N = a.N;
   const int64_t blocks = (a.rows + F::R - 1) / F::R;
-  // the wave's part of dx: block kb of x's columns, reduction steps ks0 on
-  const int kb = w % KB, ks0 = w / KB * F::DS;
-  bf8v wf[F::DS][P];
+  // the wave's part of dx: rows rb, block kb of x's columns, reduction steps ks0 on
+  const int kb = w % KB, rb = w / KB % F::RB, ks0 = w / F::UNITS * F::DS;
+  bf8v wf[F::DS][P] = {};
+  if (a.dx)
 #pragma unroll
     for (int s = 0; s < F::DS; ++s) {
       const int j = (ks0 + s) * 16 + 8 * (l / 32), half = j / (32 * NB), n = j % (32 * NB), k = kb * 32 + l % 32;
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        v[e] = a.dx && ks0 + s < F::STEPS && k < K && n + e < N ? Elem<T>::one(a.W[(int64_t)k * 2 * N + half * N + n + e]) : 0.0f;
+        // (loaded without a branch, so that all are in flight)
+        const T u = a.W[(int64_t)imin(k, K - 1) * 2 * N + (half & 1) * N + imin(n + e, N - 1)];
+        v[e] = ks0 + s < F::STEPS && k < K && n + e < N ? Elem<T>::one(u) : 0.0f;
         if (F::f32) v[e] *= kTermScale;
       }
 #pragma unroll
@@ -140,7 +144,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
         wf[s][p] = __builtin_bit_cast(bf8v, t);
       }
     }
-  // and of dW: blocks db0 on, both steps of 16 rows or one of them
+  // and of dW: blocks db0 on, all steps of 16 rows or one half of them
   const int db0 = F::DW_SPLIT == 1 ? w * F::DB : w % F::BLOCKS, dstep = F::DW_SPLIT == 1 ? 0 : w / F::BLOCKS;
   f16v dw[F::DB];
 #pragma unroll
@@ -230,14 +234,14 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
       bf8v z[P];
 #pragma unroll
       for (int p = 0; p < P; ++p)
-        z[p] = *reinterpret_cast<const bf8v*>(&sh.dz[p][F::dz_off(l % 32, (ks0 + s) % F::STEPS * 2 + l / 32)]);
+        z[p] = *reinterpret_cast<const bf8v*>(&sh.dz[p][F::dz_off(rb * 32 + l % 32, (ks0 + s) % F::STEPS * 2 + l / 32)]);
       dx[s % CH] = F::products(wf[s], z, dx[s % CH]);
     }
 #pragma unroll
-    for (int t = 0; t < 2 / F::DW_SPLIT; ++t)
+    for (int t = 0; t < F::DW_STEPS; ++t)
 #pragma unroll
       for (int j = 0; j < F::DB; ++j) {
-        const int block = db0 + j, k0 = 16 * ((dstep + t) & 1);
+        const int block = db0 + j, k0 = 16 * ((dstep * F::DW_STEPS + t) % (2 * F::RB));
         bf8v x[P], z[P];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -267,7 +271,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
         for (int q = 0; q < SPLITS; ++q)
 #pragma unroll
           for (int e = 0; e < V; e += 4) {
-            const f4v t = *reinterpret_cast<const f4v*>(&sh.stage[q * KB + col / 32][r][col % 32 + e]);
+            const f4v t = *reinterpret_cast<const f4v*>(&sh.stage[q * F::UNITS + r / 32 * KB + col / 32][r % 32][col % 32 + e]);
             v[e] += t.x, v[e + 1] += t.y, v[e + 2] += t.z, v[e + 3] += t.w;
           }
         if constexpr (F::f32) {
@@ -381,7 +385,7 @@ e3_status gated_bwd_fused_of(const FusedArgs<T>& a, int groups, hipStream_t st) 
 template <class T>
 e3_status gated_bwd_fused(const GatedCall& c) {
   constexpr e3_dtype t = std::is_same_v<T, float> ? E3_F32 : E3_BF16;
-  const int groups = gated_fused_groups(t, c.M, c.K, c.N);
+  const int groups = gated_fused_groups(t, c.M, c.N);
   FusedArgs<T> a{};
   a.dy = static_cast<const T*>(c.dy), a.z = static_cast<const T*>(c.z_in), a.W = static_cast<const T*>(c.W);
   a.x = {static_cast<const T*>(c.x), c.ldx, c.xq, c.xc}, a.dx = static_cast<T*>(c.dx), a.lddy = c.lddy, a.ldz = c.ldz;
