@@ -309,8 +309,8 @@ __device__ __forceinline__ void row_means(float (&c)[2], float cols, float* s) {
 }
 // N1's part of a piece: d becomes t gate, x (h) becomes n1, and dgate's terms come out.
 template <int V, bool LAYER>
-__device__ __forceinline__ void first_piece(const ResArgs& a, const Dropper& drop, int64_t row, int col, int n, float mean,
-                                            float rstd, const float (&g1)[V], const float (&b1)[V], const float (&gate)[V],
+__device__ __forceinline__ void first_piece(const ResArgs& a, bool post, const Dropper& drop, int64_t row, int col, int n,
+                                            float mean, float rstd, const float (&g1)[V], const float (&b1)[V], const float (&gate)[V],
                                             float (&x)[V], float (&d)[V], float (&dgate)[V]) {
 #pragma clang fp contract(off)
   unsigned keep = ~0u;
@@ -321,7 +321,7 @@ __device__ __forceinline__ void first_piece(const ResArgs& a, const Dropper& dro
     const bool in = i < n && (keep >> i & 1);
     d[i] = in ? d[i] * k : 0.0f;
     float o = x[i];
-    if (a.post) {
+    if (post) {
       x[i] = i < n ? (LAYER ? (x[i] - mean) * rstd : x[i] * rstd) : 0.0f;
       o = fmaf(x[i], g1[i], b1[i]);
     }
@@ -332,9 +332,12 @@ __device__ __forceinline__ void first_piece(const ResArgs& a, const Dropper& dro
 
 // dr, dh, dgate of rows, and per workgroup the sums over its rows (rows blockIdx.x R
 // + i, then every gridDim.x R).  The next row's pieces are in flight while a row is
-// worked on.
-template <class T, int L, int J, bool LAYER>
-__global__ __launch_bounds__(kResThreads<L>) void k_res_bwd(ResArgs a) {
+// worked on; weights are kept in registers (their loads, issued after the next row's,
+// would wait for those).
+// FAST: both norms, ds, dr and dh, whole pieces, outputs that stream: no branch around
+// a load or store, so that the wait for the next row leaves this one's stores in flight.
+template <class T, int L, int J, bool LAYER, bool POST, bool FAST>
+__global__ __launch_bounds__(kResThreads<L>, FAST ? 2 : 1) void k_res_bwd(ResArgs a) {
 #pragma clang fp contract(off)
   constexpr int V = Elem<T>::V, NT = kResThreads<L>, R = NT / L;
   using Vec = typename Elem<T>::vec;
@@ -343,34 +346,43 @@ __global__ __launch_bounds__(kResThreads<L>) void k_res_bwd(ResArgs a) {
   const int lane = threadIdx.x % L, cols = a.cols;
   const Dropper drop(a.drop);
   const float width = (float)cols;
+  static_assert(POST || !FAST);
+  constexpr bool post = POST;
+  const bool pre = FAST || a.pre, full = !FAST && a.gate && a.ldg;
   float dg1[J][V] = {}, db1[J][V] = {}, dg2[J][V] = {}, db2[J][V] = {}, dgt[J][V] = {};
   const int64_t stride = (int64_t)gridDim.x * R;
-  const bool full = a.gate && a.ldg;
-  Vec hr[J], sr[J], yr[J], dr[J], gr[J];
+  Vec hr[J], sr[J], yr[J], dr[J], gr[J], w1[J], w2[J], o1[J];
   float m1 = 0.0f, r1 = 0.0f, m2 = 0.0f, r2 = 0.0f;
-#pragma unroll
-  for (int j = 0; j < J; ++j) hr[j] = sr[j] = yr[j] = dr[j] = gr[j] = Vec{};
-  if (a.gate && !full)
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-      gr[j] = ld_raw<T>(static_cast<const T*>(a.gate) + (j * L + lane) * V, cols - (j * L + lane) * V);
+  auto col_of = [&](int j) { return (j * L + lane) * V; };
+  auto left = [&](int j) { return FAST ? V : cols - col_of(j); };
   auto rows_of = [&](const void* p, int64_t ld, int64_t r, Vec(&to)[J]) {
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-      to[j] = ld_raw<T>(static_cast<const T*>(p) + r * ld + (j * L + lane) * V, cols - (j * L + lane) * V);
+    for (int j = 0; j < J; ++j) to[j] = ld_raw<T>(static_cast<const T*>(p) + r * ld + col_of(j), left(j));
   };
+  auto weights = [&](const void* p, float none, Vec(&to)[J]) {
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = none;
+#pragma unroll
+    for (int j = 0; j < J; ++j) to[j] = Elem<T>::put(v);
+    if (p) rows_of(p, 0, 0, to);
+  };
+#pragma unroll
+  for (int j = 0; j < J; ++j) hr[j] = sr[j] = yr[j] = dr[j] = gr[j] = Vec{};
+  weights(a.g1, 1.0f, w1), weights(a.g2, 1.0f, w2), weights(a.b1, 0.0f, o1);
+  if (a.gate && !full) rows_of(a.gate, 0, 0, gr);
   auto load = [&](int64_t r) {
     if (r >= a.rows) r = a.rows - 1;
-    if (a.pre) {
+    if (pre) {
       rows_of(a.s_in, a.lds, r, sr);
       rows_of(a.dy, a.ldy, r, yr);
       if (LAYER) m2 = a.mean2[r];
       r2 = a.rstd2[r];
     }
-    if (a.ds) rows_of(a.ds, a.ldd, r, dr);
-    if (a.h) rows_of(a.h, a.ldh, r, hr);
+    if (FAST || a.ds) rows_of(a.ds, a.ldd, r, dr);
+    if (FAST || a.h) rows_of(a.h, a.ldh, r, hr);
     if (full) rows_of(a.gate, a.ldg, r, gr);
-    if (a.post) {
+    if (post) {
       if (LAYER) m1 = a.mean1[r];
       r1 = a.rstd1[r];
     }
@@ -389,14 +401,13 @@ __global__ __launch_bounds__(kResThreads<L>) void k_res_bwd(ResArgs a) {
       Elem<T>::get(gr[j], gate[j]);
     }
     load(row + stride);
-    if (a.pre) {
+    if (pre) {
       float c[2] = {};
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        const int col = (j * L + lane) * V;
         float g[V];
-        ld_weight<T>(a.g2, col, cols - col, 1.0f, g);
-        second_piece<V, LAYER>(mean2, rstd2, g, cols - col, x[j], u[j], dg2[j], db2[j], c);
+        Elem<T>::get(w2[j], g);
+        second_piece<V, LAYER>(mean2, rstd2, g, left(j), x[j], u[j], dg2[j], db2[j], c);
       }
       row_means<L, LAYER>(c, width, sh);
 #pragma unroll
@@ -404,27 +415,25 @@ __global__ __launch_bounds__(kResThreads<L>) void k_res_bwd(ResArgs a) {
 #pragma unroll
         for (int i = 0; i < V; ++i) d[j][i] += through<LAYER>(rstd2, u[j][i], x[j][i], c);
     }
-    if (a.dr)
+    if (FAST || a.dr)
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const int col = (j * L + lane) * V;
-        st_piece<T>(static_cast<T*>(a.dr) + row * a.lddr + col, cols - col, d[j], a.nt);
-      }
+      for (int j = 0; j < J; ++j)
+        st_piece<T>(static_cast<T*>(a.dr) + row * a.lddr + col_of(j), left(j), d[j], FAST || a.nt);
     float e[2] = {};
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int col = (j * L + lane) * V, n = cols - col;
+      const int col = col_of(j), n = left(j);
       float g1[V], b1[V], t[V];
-      ld_weight<T>(a.g1, col, n, 1.0f, g1);
-      ld_weight<T>(a.b1, col, n, 0.0f, b1);
-      first_piece<V, LAYER>(a, drop, row, col, n, mean1, rstd1, g1, b1, gate[j], h[j], d[j], t);
+      Elem<T>::get(w1[j], g1);
+      Elem<T>::get(o1[j], b1);
+      first_piece<V, LAYER>(a, post, drop, row, col, n, mean1, rstd1, g1, b1, gate[j], h[j], d[j], t);
       if (full && a.dgate) {
         st_piece<T>(static_cast<T*>(a.dgate) + row * a.lddg + col, n, t, a.nt);
       } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) dgt[j][i] += t[i];
       }
-      if (a.post)
+      if (post)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           dg1[j][i] = fmaf(d[j][i], h[j][i], dg1[j][i]);
@@ -434,15 +443,14 @@ __global__ __launch_bounds__(kResThreads<L>) void k_res_bwd(ResArgs a) {
           if (LAYER) e[1] += d[j][i];
         }
     }
-    if (a.dh) {
-      if (a.post) row_means<L, LAYER>(e, width, sh);
+    if (FAST || a.dh) {
+      if (post) row_means<L, LAYER>(e, width, sh);
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        const int col = (j * L + lane) * V;
-        if (a.post)
+        if (post)
 #pragma unroll
           for (int i = 0; i < V; ++i) d[j][i] = through<LAYER>(rstd1, d[j][i], h[j][i], e);
-        st_piece<T>(static_cast<T*>(a.dh) + row * a.lddh + col, cols - col, d[j], a.nt);
+        st_piece<T>(static_cast<T*>(a.dh) + row * a.lddh + col_of(j), left(j), d[j], FAST || a.nt);
       }
     }
   }
@@ -513,7 +521,7 @@ __device__ __forceinline__ void wide_first(const ResArgs& a, const Dropper& drop
   for (int i = 0; i < V; ++i) h[i] = 0.0f;
   if (a.h) ld_piece<T>(static_cast<const T*>(a.h) + row * a.ldh + col, n, h);
   if (a.gate) ld_piece<T>(static_cast<const T*>(a.gate) + row * a.ldg + col, n, gate);
-  first_piece<V, LAYER>(a, drop, row, col, n, a.post && LAYER ? a.mean1[row] : 0.0f, a.post ? a.rstd1[row] : 0.0f, g1, b1,
+  first_piece<V, LAYER>(a, a.post, drop, row, col, n, a.post && LAYER ? a.mean1[row] : 0.0f, a.post ? a.rstd1[row] : 0.0f, g1, b1,
                         gate, h, d, t);
 }
 template <class T, bool LAYER>
@@ -662,8 +670,9 @@ __global__ __launch_bounds__(512) void k_res_sums(const float* part, int parts, 
 
 // ------------------------------------------------------------ host
 // The narrowest arrangement that holds a row: lanes per row and pieces per lane; J =
-// 0 past the registers.
-template <class T, class F>
+// 0 past the registers.  The backward keeps up to five sums a column: twelve float32
+// columns a lane fit (sixteen spilled 40 to 450 registers), sixteen of bfloat16.
+template <class T, bool BWD, class F>
 auto res_shape(int cols, F&& f) {
   constexpr int V = Elem<T>::V;
   const int pieces = (cols + V - 1) / V;
@@ -673,7 +682,15 @@ auto res_shape(int cols, F&& f) {
   E3_SHAPE(32, 1);
   E3_SHAPE(64, 1);
   E3_SHAPE(64, 2);
-  if constexpr (V == 4) {
+  if constexpr (V == 4 && BWD) {
+    E3_SHAPE(64, 3);
+    E3_SHAPE(128, 2);
+    E3_SHAPE(128, 3);
+    E3_SHAPE(256, 2);
+    E3_SHAPE(256, 3);
+    E3_SHAPE(512, 2);
+    E3_SHAPE(512, 3);
+  } else if constexpr (V == 4) {
     E3_SHAPE(64, 3);
     E3_SHAPE(64, 4);
     E3_SHAPE(128, 4);
@@ -693,15 +710,16 @@ int res_blocks(e3_dtype t, int64_t rows, int cols) {
     constexpr int l = decltype(L)::value, j = decltype(J)::value, nt = kResThreads<l>, R = j > 0 ? nt / l : 1;
     return (int)std::max<int64_t>(1, std::min<int64_t>(j > 0 ? 256 * 512 / nt : 256, (rows + R - 1) / R));
   };
-  return t == E3_F32 ? res_shape<float>(cols, of) : res_shape<__bf16>(cols, of);
+  return t == E3_F32 ? res_shape<float, true>(cols, of) : res_shape<__bf16, true>(cols, of);
 }
-bool res_wide(e3_dtype t, int cols) {
-  return cols > (t == E3_F32 ? 512 * 4 * 4 : 512 * 2 * 8);
+bool res_bwd_wide(e3_dtype t, int cols) {
+  auto of = [](auto, auto J) { return decltype(J)::value == 0; };
+  return t == E3_F32 ? res_shape<float, true>(cols, of) : res_shape<__bf16, true>(cols, of);
 }
 
 template <class T>
 e3_status res_fwd(const ResArgs& a, bool layer, hipStream_t st) {
-  return res_shape<T>(a.cols, [&](auto L, auto J) -> e3_status {
+  return res_shape<T, false>(a.cols, [&](auto L, auto J) -> e3_status {
     constexpr int l = decltype(L)::value, j = decltype(J)::value;
     if constexpr (j > 0) {
       constexpr int R = kResThreads<l> / l;
@@ -719,11 +737,15 @@ e3_status res_fwd(const ResArgs& a, bool layer, hipStream_t st) {
 }
 template <class T>
 e3_status res_bwd(const ResArgs& a, bool layer, hipStream_t st) {
-  return res_shape<T>(a.cols, [&](auto L, auto J) -> e3_status {
+  return res_shape<T, true>(a.cols, [&](auto L, auto J) -> e3_status {
     constexpr int l = decltype(L)::value, j = decltype(J)::value;
     if constexpr (j > 0) {
-      TimedLaunch t_("residual_norm_bwd", st);
-      auto* k = layer ? k_res_bwd<T, l, j, true> : k_res_bwd<T, l, j, false>;
+      const bool fast = a.pre && a.post && a.ds && a.h && a.dr && a.dh && !(a.gate && a.ldg) && a.nt &&
+                        a.cols == l * j * Elem<T>::V;
+      TimedLaunch t_(fast ? "residual_norm_bwd_stream" : "residual_norm_bwd", st);
+      auto* k = fast     ? (layer ? k_res_bwd<T, l, j, true, true, true> : k_res_bwd<T, l, j, false, true, true>)
+                : a.post ? (layer ? k_res_bwd<T, l, j, true, true, false> : k_res_bwd<T, l, j, false, true, false>)
+                         : (layer ? k_res_bwd<T, l, j, true, false, false> : k_res_bwd<T, l, j, false, false, false>);
       hipLaunchKernelGGL(k, dim3(a.blocks), dim3(kResThreads<l>), 0, st, a);
       E3_HIP(hipGetLastError());
     } else {
@@ -753,7 +775,7 @@ ResWs res_ws(e3_dtype t, int64_t rows, int64_t cols) {
   if (rows == 0) return w;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   w.part = up((size_t)res_blocks(t, rows, (int)cols) * 5 * cols * sizeof(float));
-  w.total = w.part + (res_wide(t, (int)cols) ? up((size_t)rows * 2 * sizeof(float)) : 0);
+  w.total = w.part + (res_bwd_wide(t, (int)cols) ? up((size_t)rows * 2 * sizeof(float)) : 0);
   return w;
 }
 
