@@ -323,18 +323,26 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
           dw[0][4 * g] += t.x, dw[0][4 * g + 1] += t.y, dw[0][4 * g + 2] += t.z, dw[0][4 * g + 3] += t.w;
         }
     }
+    __syncthreads();
+    // by way of the wave's staging, so that rows are written in runs of 128 bytes
     if (dstep == 0)
 #pragma unroll
       for (int j = 0; j < F::DB; ++j) {
-        const int block = db0 + j, nb = block % (2 * NB), half = nb / NB, k = block / (2 * NB) * 32 + l % 32;
+        const int block = db0 + j, nb = block % (2 * NB), half = nb / NB;
+        asm volatile("" ::: "memory");
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int n = nb % NB * 32 + 8 * g + 4 * (l / 32);
-          float v[4];
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f4v*>(&sh.stage[w][l % 32][8 * g + 4 * (l / 32)]) =
+              f4v{dw[j][4 * g], dw[j][4 * g + 1], dw[j][4 * g + 2], dw[j][4 * g + 3]} * F::kBack;
+        Rows32<float, 1>::wait();
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[e] = dw[j][4 * g + e] * F::kBack;
-            if constexpr (F::f32) {
+        for (int i = 0; i < 4; ++i) {
+          const int r = 8 * i + l / 8, k = block / (2 * NB) * 32 + r, n = nb % NB * 32 + 4 * (l % 8);
+          const f4v s = *reinterpret_cast<const f4v*>(&sh.stage[w][r][4 * (l % 8)]);
+          float v[4] = {s.x, s.y, s.z, s.w};
+          if constexpr (F::f32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
               if (v[e] * 0.0f != 0.0f && k < K && n + e < N) {
                 v[e] = 0.0f;
 #pragma clang loop unroll(disable)
@@ -343,10 +351,10 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
                   for (int64_t row = b * F::R; row < (b + 1) * F::R && row < a.rows; ++row)
                     v[e] = fmaf(a.x.value(row, k, K), gated_dz_value(a, row, half * N + n + e), v[e]);
               }
-            }
           }
           if (k < K) st_piece<float>(part + (int64_t)k * 2 * N + half * N + n, N - n, v);
         }
+        Rows32<float, 1>::wait();
       }
   }
   // db: the threads of a piece, in order
