@@ -69,7 +69,9 @@ struct GatedBwdWs {
 GatedBwdWs gated_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   GatedBwdWs w{};
   if (M == 0) return w;
-  w.blocks = std::max<int64_t>(1, std::min<int64_t>(512, (M + 63) / 64));
+  // 4,096 workgroups with the column tiles: more would leave more partial sums of db
+  const int64_t tiles = (N + 16 * (t == E3_F32 ? 4 : 8) - 1) / (16 * (t == E3_F32 ? 4 : 8));
+  w.blocks = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512, std::max<int64_t>(64, 4096 / tiles)), (M + 63) / 64));
   w.rows = (M + w.blocks - 1) / w.blocks;
   w.dz = up256((size_t)M * 2 * N * (t == E3_F32 ? 4 : 2));
   w.db = up256((size_t)w.blocks * 2 * N * 4);

@@ -984,10 +984,7 @@ def dense_bwd(x, W, dy, z=None, act: str = "none", want=("dx", "dW", "db"), dx=N
 
 def _here(*tensors):
     """Launches go to the current device: every tensor has to be there."""
-    global _current
-    if _current is None:
-        _stream(None)
-    device = _current[1]()
+    device = None
     for t in tensors:
         if t is None:
             continue
@@ -995,9 +992,14 @@ def _here(*tensors):
             at = t.get_device()
         except AttributeError:
             raise TypeError(f"expected a torch tensor, got {type(t).__name__}") from None
+        if at < 0:
+            raise ValueError("tensors must be on the GPU")
+        if device is None:
+            if _current is None:
+                _stream(None)
+            device = _current[1]()
         if at != device:
-            raise ValueError("tensors must be on the GPU" if at < 0 else
-                             f"a tensor is on GPU {at}, the current device is {device}")
+            raise ValueError(f"a tensor is on GPU {at}, the current device is {device}")
 
 
 # ---------------------------------------------------------------- gated dense layers

@@ -145,3 +145,29 @@ def test_residual_norm_refusals(L):
     nothing = {"dr": None, "dh": None, "dgate": None, "dg1": None, "db1": None, "dg2": None, "db2": None, "ws": None, "nb": 0}
     assert bwd(**nothing) == OK
     assert bwd(rows=0, **nothing) == OK
+
+
+def test_dropout_arguments():
+    d = e3mi.Dropout(0.25, (1 << 64) - 1, 7)
+    assert (d.p, d.seed, d.offset, d.counter) == (0.25, (1 << 64) - 1, 7, None)
+    for args in ((-0.1, 0), (1.5, 0), (NAN, 0), (0.5, -1), (0.5, 1 << 64), (0.5, 0, -1), (0.5, 0, 1 << 64)):
+        with pytest.raises(ValueError):
+            e3mi.Dropout(*args)
+
+
+def test_calls_refuse_tensors_that_are_not_on_the_gpu():
+    torch = pytest.importorskip("torch")
+    x, W, w = torch.zeros(4, 8), torch.zeros(8, 12), torch.zeros(8)
+    drop = e3mi.Dropout(0.5, 1)
+    if torch.cuda.is_available():
+        pytest.skip("checked on the host")
+    for call in (lambda: e3mi.dropout_fwd(x, 0.5), lambda: e3mi.dropout_bwd(x, None), lambda: e3mi.gated_fwd(x.double(), W),
+                 lambda: e3mi.residual_norm_fwd(x.half(), pre=(None, None))):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: e3mi.gated_fwd(x, W[:, :11]), lambda: e3mi.gated_fwd(x, W[:7]), lambda: e3mi.gated_fwd(x, W, act="tanh"),
+                 lambda: e3mi.gated_bwd(x, W, x, x), lambda: e3mi.residual_norm_fwd(x, norm="batch"),
+                 lambda: e3mi.gated_fwd(x, W), lambda: e3mi.dropout_fwd(x, drop), lambda: e3mi.residual_norm_fwd(x, pre=(w, None)),
+                 lambda: e3mi.residual_norm_bwd(x, x, None), lambda: e3mi.residual_norm_bwd(x, x, None, dy=x)):
+        with pytest.raises(ValueError):
+            call()

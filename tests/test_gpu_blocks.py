@@ -533,6 +533,94 @@ def test_residual_norm_gradient_equals_differences(e3):  # noqa: F811
         assert abs(num - (host(got) * step).sum()) < 1e-5 * np.linalg.norm(host(got)) * np.sqrt(step.size), i
 
 
+@pytest.mark.parametrize("M,K,N", [(17_000_003, 8, 64), (9_000_007, 8, 130)])
+def test_gated_past_two_billion_values(e3, M, K, N):  # noqa: F811
+    """z (and dz, where it is written) has more than 2^31 values: rows of both ends."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(M, K, generator=g, device="cuda").bfloat16()
+    W = torch.randn(K, 2 * N, generator=g, device="cuda").bfloat16()
+    dy = torch.randn(M, N, generator=g, device="cuda").bfloat16()
+    print("[case] gated large", M, K, N, flush=True)
+    y, z = e3.gated_fwd(x, W, keep=("z",))
+    dx = e3.gated_bwd(None, W, dy, z, want=("dx",))[0]
+    rows = torch.cat([torch.arange(100), torch.arange(M - 100, M), torch.arange((1 << 31) // (2 * N) - 50, (1 << 31) // (2 * N) + 50)]).cuda()
+    ref, zr = ob.gated_fwd(host(x[rows]), host(W))
+    close(y[rows], ref, "bfloat16")
+    close(z[rows], zr, "bfloat16")
+    dz = rounded(ob.gated_dz(host(dy[rows]), host(z[rows])), "bfloat16")
+    close(dx[rows], dz @ host(W).T, "bfloat16")
+    # the sums over rows: those of the last rows alone reach dW and db
+    dy[:-100] = 0
+    dW, db = e3.gated_bwd(x, W, dy, z, want=("dW", "db"))[1:]
+    last = torch.arange(M - 100, M).cuda()
+    dz = ob.gated_dz(host(dy[last]), host(z[last]))
+    close(dW, host(x[last]).T @ rounded(dz, "bfloat16"), "bfloat16")
+    close(db, dz.sum(0), "bfloat16")
+
+
+def test_residual_norm_past_two_billion_values(e3):  # noqa: F811
+    import torch
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB")
+    M, K = 2_100_007, 1024
+    g = torch.Generator(device="cuda").manual_seed(2)
+    h, r, dy, ds = (torch.randn(M, K, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(4))
+    w = ((1 + 0.2 * torch.randn(K, generator=g, device="cuda")).bfloat16(), None)
+    drop = e3.Dropout(0.3, 5, 9)
+    print("[case] residual_norm large", M, K, flush=True)
+    s, y, st = e3.residual_norm_fwd(h, r, None, 0.5, "rms", w, w, drop=drop, keep=("stats",))
+    dr, dh, _, _, _ = e3.residual_norm_bwd(h, s, st, dy, ds, None, 0.5, "rms", w, w, drop, want=("dres", "dh"))
+    rows = np.concatenate([np.arange(40), np.arange((1 << 31) // K - 20, (1 << 31) // K + 20), np.arange(M - 40, M)])
+    pick = torch.from_numpy(rows).cuda()
+    wh, f = (host(w[0]), None), ob.factors(rows, K, 0.3, 5, 9)
+    rs, ry, first, last = ob.residual_norm_fwd(host(h[pick]), host(r[pick]), None, 0.5, "rms", wh, wh, 1e-5, f)
+    close(s[pick], rs, "bfloat16")
+    close(y[pick], ry, "bfloat16")
+    got = host(st[:, pick])
+    ref = ob.residual_norm_bwd(host(h[pick]), host(s[pick]), (None, got[0]), (None, got[1]), host(dy[pick]), host(ds[pick]), None,
+                               0.5, "rms", wh, wh, f)
+    close(dr[pick], ref[0], "bfloat16")
+    close(dh[pick], ref[1], "bfloat16")
+
+
+@pytest.mark.parametrize("M,K,N", [(1000, 64, 128), (700, 24, 20), (40, 64, 33), (900, 100, 60)])
+def test_gated_backward_bad_values_stay_in_their_rows_and_columns(e3, M, K, N):  # noqa: F811
+    """float32: an infinity in x reaches its row of dW, a NaN in dy its row of dx and its columns of dW and db."""
+    import torch
+    x, W, b, dy = _gated_inputs(M, K, N)
+    z = ob.gated_fwd(x, W, b)[1]
+    x[M // 2, 3], dy[M - 1, 5] = np.inf, np.nan
+    dx, dW, db = e3.gated_bwd(dev(x, "float32"), dev(W, "float32"), dev(dy, "float32"), dev(z, "float32"))
+    clean = dy.copy()
+    clean[M - 1, 5] = 0
+    dz = ob.gated_dz(clean, z)
+    rows = [i for i in range(M) if i != M - 1]
+    close(dx[torch.tensor(rows).cuda()], dz[rows] @ W.T, "float32")
+    assert bool(torch.isnan(dx[M - 1]).all())
+    ks, js = [k for k in range(K) if k != 3], [j for j in range(2 * N) if j not in (5, N + 5)]
+    close(dW[torch.tensor(ks).cuda()][:, torch.tensor(js).cuda()], (x[:, ks].T @ dz)[:, js], "float32")
+    assert not bool(torch.isfinite(dW[3]).any()) and bool(torch.isnan(dW[:, 5]).all()) and bool(torch.isnan(dW[:, N + 5]).all())
+    close(db[torch.tensor(js).cuda()], dz.sum(0)[js], "float32")
+    assert bool(torch.isnan(db[5])) and bool(torch.isnan(db[N + 5]))
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e12, 1e18])
+@pytest.mark.parametrize("M,K,N", [(500, 64, 100), (500, 70, 100)])
+def test_gated_backward_float32_range(e3, scale, M, K, N):  # noqa: F811
+    """Operands whose scaled terms or sums leave the matrix cores' range."""
+    x, W, b, dy = _gated_inputs(M, K, N)
+    xd, Wd, zd, dyd = dev(x * scale, "float32"), dev(W, "float32"), dev(ob.gated_fwd(x, W, b)[1], "float32"), dev(dy, "float32")
+    dz = ob.gated_dz(host(dyd), host(zd))
+    dx, dW, db = e3.gated_bwd(xd, Wd, dyd, zd)
+    close(dx, dz @ host(Wd).T, "float32")
+    close(dW, host(xd).T @ dz, "float32")
+    dx = e3.gated_bwd(None, Wd, dev(dy * scale, "float32"), zd, want=("dx",))[0]
+    close(dx, ob.gated_dz(host(dev(dy * scale, "float32")), host(zd)) @ host(Wd).T, "float32")
+
+
 # ---------------------------------------------------------------- as they are used
 def _block(e3, dt, packs, M=900, D=96, F=160):  # noqa: F811
     """Two residual blocks, forward and backward call by call, against float64 automatic differentiation."""
