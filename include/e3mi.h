@@ -453,8 +453,9 @@ e3_status e3_gated_fwd(e3_dtype dtype, const void* x, int64_t ldx, const void* W
                        uint8_t* yc, void* ws, size_t ws_bytes, int64_t M, int64_t K, int64_t N, e3_stream stream);
 /* With dz = [dy u act'(g) | dy act(g)]: dx = dz W^T, dW = x^T dz, db = the column
  * sums of dz (each may be NULL).  x (for dW) and z in full, or packed: xq, xc, and
- * gq, gc and uq, uc.  dz is rounded as a dense backward's.  M = 0 gives dW = 0 and
- * db = 0.  ws: bwd_bytes, 16-byte aligned. */
+ * gq, gc and uq, uc.  A bfloat16 dz is rounded as a dense backward's, but for K up to
+ * 64 and N up to 128 from z in full, where it never goes to memory.  M = 0 gives dW
+ * = 0 and db = 0.  ws: bwd_bytes, 16-byte aligned. */
 e3_status e3_gated_bwd(e3_dtype dtype, const void* x, int64_t ldx, const int8_t* xq, const uint8_t* xc, const void* W,
                        const void* z, int64_t ldz, const int8_t* gq, const uint8_t* gc, const int8_t* uq,
                        const uint8_t* uc, e3_act act, const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dW,

@@ -3,7 +3,7 @@
 //
 //   dz = [dy u act'(g) | dy act(g)],  dx = dz W^T, dW = x^T dz, db = sum_rows dz
 //
-// dz never goes to memory: a workgroup takes blocks of 32 or 64 rows, writes their dz and x to
+// dz never goes to memory and is rounded nowhere (two bfloat16 terms hold 16 bits of it): a workgroup takes blocks of 32 or 64 rows, writes their dz and x to
 // LDS as terms (dense_tile.h), and its eight waves multiply both products from there,
 // dx's with the terms of W in registers for good, dW's into registers that stay for
 // all blocks; what is left is to add the workgroups' dW and db in order.  The next
@@ -48,7 +48,7 @@ __device__ __forceinline__ float gated_dz_value(const FusedArgs<T>& a, int64_t r
 template <class T, int KB, int NB, bool XQ>
 struct Fused {
   static constexpr bool f32 = sizeof(T) == 4;
-  static constexpr int V = Elem<T>::V, P = f32 ? 3 : 1, R = gated_fused_rows(f32, 32 * NB), RB = R / 32, NC = 64 * NB, KC = 32 * KB, WAVES = 8, THREADS = 512;
+  static constexpr int V = Elem<T>::V, P = f32 ? 3 : 1, PZ = f32 ? 3 : 2, R = gated_fused_rows(f32, 32 * NB), RB = R / 32, NC = 64 * NB, KC = 32 * KB, WAVES = 8, THREADS = 512;
   static constexpr float kBack = f32 ? kTermBack : 1.0f;
   // pieces of a row and of a thread
   static constexpr int PR = 32 * NB / V, NP = (R * PR + THREADS - 1) / THREADS;
@@ -60,7 +60,7 @@ struct Fused {
   static constexpr int DW_SPLIT = BLOCKS >= WAVES ? 1 : 2, DW_WAVES = BLOCKS / DB * DW_SPLIT;
   static constexpr int DW_STEPS = 2 * RB / DW_SPLIT;
   struct Shared {
-    unsigned short dz[P][R * NC];
+    unsigned short dz[PZ][R * NC];
     unsigned short x[P][R * KC];
     float stage[WAVES][32][36];
   };
@@ -86,26 +86,29 @@ struct Fused {
     u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + off(k + 4, col / 8) + col % 8));
     return u.f;
   }
-  // The terms of V values to every plane.
-  static __device__ __forceinline__ void put(unsigned short* p, int plane, const float (&v)[V]) {
-    if constexpr (f32) {
-      float a = v[0] * kTermScale, b = v[1] * kTermScale, c = v[2] * kTermScale, d = v[3] * kTermScale;
+  // The first N terms of V values, to N planes.
+  template <int N>
+  static __device__ __forceinline__ void put(unsigned short* p, int plane, float (&v)[V]) {
+    if constexpr (f32)
 #pragma unroll
-      for (int t = 0; t < 3; ++t) {
-        const unsigned x = term2(a, b), y = term2(c, d);
-        *reinterpret_cast<u2v*>(p + t * plane) = u2v{x, y};
-      }
-    } else {
-      *reinterpret_cast<u4v*>(p) = u4v{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+      for (int k = 0; k < V; ++k) v[k] *= kTermScale;
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+      unsigned b[V / 2];
+#pragma unroll
+      for (int k = 0; k < V / 2; ++k) b[k] = term2(v[2 * k], v[2 * k + 1]);
+      if constexpr (V == 4) *reinterpret_cast<u2v*>(p + t * plane) = u2v{b[0], b[1]};
+      else *reinterpret_cast<u4v*>(p + t * plane) = u4v{b[0], b[1], b[2], b[3]};
     }
   }
   // Pairs of terms, smallest products first.
-  static __device__ __forceinline__ f16v products(const bf8v (&y)[P], const bf8v (&x)[P], f16v acc) {
+  template <int PY, int PX>
+  static __device__ __forceinline__ f16v products(const bf8v (&y)[PY], const bf8v (&x)[PX], f16v acc) {
 #pragma unroll
-    for (int s = 2 * P - 2 < 2 ? 2 * P - 2 : 2; s >= 0; --s)
+    for (int s = PY + PX - 2 < 2 ? PY + PX - 2 : 2; s >= 0; --s)
 #pragma unroll
-      for (int p = 0; p < P; ++p)
-        if (s - p >= 0 && s - p < P) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[s - p], x[p], acc, 0, 0, 0);
+      for (int p = 0; p < PX; ++p)
+        if (s - p >= 0 && s - p < PY) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[s - p], x[p], acc, 0, 0, 0);
     return acc;
   }
 };
@@ -204,8 +207,8 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
         sum[0][k] += u[k], sum[1][k] += e[k];
       }
       if (r < F::R) {
-        F::put(&sh.dz[0][F::dz_off(r, col / 8) + col % 8], F::R * F::NC, u);
-        F::put(&sh.dz[0][F::dz_off(r, (col + 32 * NB) / 8) + col % 8], F::R * F::NC, e);
+        F::template put<F::PZ>(&sh.dz[0][F::dz_off(r, col / 8) + col % 8], F::R * F::NC, u);
+        F::template put<F::PZ>(&sh.dz[0][F::dz_off(r, (col + 32 * NB) / 8) + col % 8], F::R * F::NC, e);
       }
     }
     if (a.dw)
@@ -217,7 +220,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
         const bool in = r < count && col < K;
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = in ? v[k] : 0.0f;
-        if (r < F::R) F::put(&sh.x[0][F::x_off(r, col / 8) + col % 8], F::R * F::KC, v);
+        if (r < F::R) F::template put<P>(&sh.x[0][F::x_off(r, col / 8) + col % 8], F::R * F::KC, v);
       }
   };
   // Both products of a block.  dx's sum runs over its steps in two chains, so that with
@@ -231,9 +234,9 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
       for (int e = 0; e < 16; ++e) dx[c][e] = 0.0f;
 #pragma unroll
     for (int s = 0; s < F::DS; ++s) {
-      bf8v z[P];
+      bf8v z[F::PZ];
 #pragma unroll
-      for (int p = 0; p < P; ++p)
+      for (int p = 0; p < F::PZ; ++p)
         z[p] = *reinterpret_cast<const bf8v*>(&sh.dz[p][F::dz_off(rb * 32 + l % 32, (ks0 + s) % F::STEPS * 2 + l / 32)]);
       dx[s % CH] = F::products(wf[s], z, dx[s % CH]);
     }
@@ -242,12 +245,11 @@ __global__ __launch_bounds__(512, 2) void k_gated_bwd(FusedArgs<T> a) {
 #pragma unroll
       for (int j = 0; j < F::DB; ++j) {
         const int block = db0 + j, k0 = 16 * ((dstep * F::DW_STEPS + t) % (2 * F::RB));
-        bf8v x[P], z[P];
+        bf8v x[P], z[F::PZ];
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          x[p] = F::across(sh.x[p], F::x_off, block / (2 * NB) * 32, k0);
-          z[p] = F::across(sh.dz[p], F::dz_off, block % (2 * NB) * 32, k0);
-        }
+        for (int p = 0; p < P; ++p) x[p] = F::across(sh.x[p], F::x_off, block / (2 * NB) * 32, k0);
+#pragma unroll
+        for (int p = 0; p < F::PZ; ++p) z[p] = F::across(sh.dz[p], F::dz_off, block % (2 * NB) * 32, k0);
         dw[j] = F::products(z, x, dw[j]);
       }
 #pragma unroll
