@@ -297,6 +297,120 @@ __global__ __launch_bounds__(256, 2) void k_gated_panel(GatedArgs a) {
   }
 }
 
+// The same in float32 for whole pieces and y alone: the terms of W lie in LDS for the
+// workgroup's waves, and each forms a row block's terms, a third of the vector work,
+// once for NG groups of 32 columns of y instead of once for each.  Against the kernel
+// above, us: 156,000 x 64 x 64 24 and 30, 624,000 70 and 92, 1,248,000 x 32 x 128 194 and
+// 223; bfloat16, which has no terms to form, 17 and 14, 42 and 37.
+template <class T, int KK, int NG, bool NT>
+__global__ __launch_bounds__(512, 2) void k_gated_walk(GatedArgs a) {
+  using R = Rows32<T, 2>;
+  constexpr bool f32 = sizeof(T) == 4;
+  constexpr int V = Elem<T>::V, P = f32 ? 3 : 1, Q = 8 / V, WAVES = 8;
+  __shared__ __align__(16) bf8v wf[NG][KK][2][P][kWave];
+  __shared__ __align__(16) float out[WAVES][32][R::PITCH];
+  const int l = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), h = 8 * (l / 32);
+  const int col0 = (int)blockIdx.y * 32 * NG;
+  for (int f = wave; f < NG * KK * 2; f += WAVES) {
+    const int c = f % 2, k = f / 2 % KK, g = f / 2 / KK;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = Elem<T>::one(static_cast<const T*>(a.b.p)[(16 * k + h + e) * a.b.ld + c * a.cols + col0 + 32 * g + l % 32]);
+      if (f32) v[e] *= kTermScale;
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      u4v t;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = term2(v[2 * e], v[2 * e + 1]);
+      wf[g][k][c][p][l] = __builtin_bit_cast(bf8v, t);
+    }
+  }
+  __syncthreads();
+  typename Elem<T>::vec x[KK][Q];
+  const T* xp = static_cast<const T*>(a.a.p);
+  auto load = [&](auto fast, int64_t block) {
+    constexpr bool F = decltype(fast)::value;
+    const int last = F ? 31 : (int)(a.rows - block * 32) - 1;
+    const int64_t m = imin(l % 32, last);
+#pragma unroll
+    for (int k = 0; k < KK; ++k)
+#pragma unroll
+      for (int q = 0; q < Q; ++q) x[k][q] = ld_raw<T>(xp + block * 32 * a.a.ld + (m * a.a.ld + 16 * k + h + q * V), V);
+  };
+  bf8v xf[P][KK];
+  auto terms = [&]() {
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      if constexpr (!f32) {
+        xf[0][k] = __builtin_bit_cast(bf8v, x[k][0]);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) Elem<T>::get(x[k][q], reinterpret_cast<float(&)[V]>(v[q * V]));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= kTermScale;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          u4v t;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t[e] = term2(v[2 * e], v[2 * e + 1]);
+          xf[p][k] = __builtin_bit_cast(bf8v, t);
+        }
+      }
+    }
+  };
+  auto product = [&](auto fast, int64_t block) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      f16v acc[2];
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[c][e] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < KK; ++k) {
+        bf8v y[2][P];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int p = 0; p < P; ++p) y[c][p] = wf[g][k][c][p][l];
+#pragma unroll
+        for (int s = 2 * P - 2 < 2 ? 2 * P - 2 : 2; s >= 0; --s)
+#pragma unroll
+          for (int p = 0; p < P; ++p) {
+            const int q = s - p;
+            if (q < 0 || q >= P) continue;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[c][q], xf[p][k], acc[c], 0, 0, 0);
+          }
+      }
+      gated_rows32<T, 2, decltype(fast)::value, NT>(a, block * 32, col0 + 32 * g, out[wave], acc);
+    }
+  };
+  const int64_t blocks = a.rows / 32, stride = (int64_t)gridDim.x * WAVES;
+  const std::true_type fast;
+  const int64_t first = (int64_t)blockIdx.x * WAVES + wave;
+  if (first < blocks) {
+    // rounds as k_gated_panel's
+    auto at = [&](int64_t b) { return b < blocks ? b : blocks - 1; };
+    load(fast, first);
+    terms();
+    load(fast, at(first + stride));
+    for (int64_t block = first; block < blocks; block += stride) {
+      product(fast, block);
+      terms();
+      load(fast, at(block + 2 * stride));
+    }
+  }
+  if (a.rows % 32 && first == blocks % stride) {
+    load(std::false_type{}, blocks);
+    terms();
+    product(std::false_type{}, blocks);
+  }
+}
+
 // At most MR <= 8 rows, as k_dense_few: W is read once, straight to registers, and
 // that is what bounds it.  A workgroup takes 32 columns of y.
 template <class T, int MR>
@@ -416,8 +530,27 @@ int gated_fused_groups(e3_dtype t, int64_t M, int64_t N) {
   return (int)std::min<int64_t>((M + rows - 1) / rows, 256);
 }
 
+// Whether k_gated_walk takes it: whole steps and groups of columns.
+bool gated_walks(const GatedArgs& a) {
+  return a.rows >= 32 && GatedTail<float>::plain(a) && (a.red == 32 || a.red == 64) && a.cols % 64 == 0;
+}
+template <int KK, int NG>
+e3_status gated_walk(const GatedArgs& a, hipStream_t st) {
+  TimedLaunch t_("gated_fwd_walk", st);
+  const unsigned tiles = (unsigned)(a.cols / (32 * NG));  // of columns; a workgroup per CU among them
+  const int64_t rows = std::min<int64_t>((a.rows + 255) / 256, std::max<int64_t>(1, 256 / tiles));
+  auto* k = a.nt ? k_gated_walk<float, KK, NG, true> : k_gated_walk<float, KK, NG, false>;
+  hipLaunchKernelGGL(k, dim3((unsigned)rows, tiles), dim3(512), 0, st, a);
+  E3_HIP(hipGetLastError());
+  return E3_OK;
+}
+
 template <class T>
 e3_status gated_panel(GatedArgs a, hipStream_t st) {
+  if constexpr (sizeof(T) == 4) {
+    if (gated_walks(a))
+      return a.red == 64 ? gated_walk<4, 2>(a, st) : a.cols % 128 == 0 ? gated_walk<2, 4>(a, st) : gated_walk<2, 2>(a, st);
+  }
   // two workgroups per CU, each wave on row blocks of its own
   const int64_t groups = (a.cols + 31) / 32;
   a.chunks = std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 2048 / groups));

@@ -130,7 +130,9 @@ def test_gated_backward(e3, dt, M, K, N, gap, shift, f32, bf16, ckpt):  # noqa: 
 
 
 # M, K, N and the kernel, past the sizes above: tiles and row walks
-LARGE = [("float32", 262149, 64, 16, 0, "panel"), ("float32", 131077, 33, 40, 3, "panel"), ("float32", 300007, 8, 64, 0, "panel"),
+LARGE = [("float32", 262149, 64, 64, 0, "walk"), ("float32", 140000, 32, 128, 0, "walk"), ("float32", 131111, 32, 64, 8, "walk"),
+         ("float32", 90001, 64, 192, 0, "walk"), ("float32", 140001, 64, 72, 0, "panel"), ("bfloat16", 262149, 64, 64, 0, "panel"),
+         ("float32", 262149, 64, 16, 0, "panel"), ("float32", 131077, 33, 40, 3, "panel"), ("float32", 300007, 8, 64, 0, "panel"),
          ("bfloat16", 262149, 128, 16, 0, "panel"), ("bfloat16", 262176, 64, 32, 0, "panel"), ("bfloat16", 150001, 90, 33, 1, "panel"),
          ("float32", 16403, 100, 300, 0, "128"), ("float32", 4096, 1100, 257, 1, "split_128"), ("bfloat16", 40003, 130, 129, 0, "128"),
          ("bfloat16", 16400, 300, 800, 0, "256"), ("bfloat16", 16400, 320, 800, 0, "direct"), ("bfloat16", 33000, 64, 328, 8, "panel"),
