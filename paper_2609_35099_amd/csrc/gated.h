@@ -48,6 +48,8 @@ struct GatedArgs {
   int8_t *gq, *uq, *yq;
   uint8_t *gc, *uc, *yc;
   int64_t chunks;  // row chunks of the panel
+  float* part;     // partial sums of z, [splits][rows][2 cols], instead of the epilogue
+  int red_chunk;   // reduction indexes of a split
   bool nt;
 };
 
@@ -418,37 +420,54 @@ __global__ __launch_bounds__(512) void k_gated_few(GatedArgs a) {
   constexpr int V = Elem<T>::V, C = 32 / V, G = 512 / C, WAVES = 512 / kWave;
   __shared__ float s[WAVES][2][MR][32];
   const int cl = threadIdx.x % C, g = threadIdx.x / C, col = (int)blockIdx.x * 32 + cl * V, n = a.cols - col;
-  const int K = (int)a.red;
+  const int kbegin = (int)blockIdx.y * a.red_chunk, K = imin(kbegin + a.red_chunk, (int)a.red);
   const T* W = static_cast<const T*>(a.b.p);
   const T* x = static_cast<const T*>(a.a.p);
   float v[2][MR][V] = {};
-  constexpr int U = MR > 4 ? 2 : 4;  // reduction indexes in flight
-  for (int k0 = g; k0 < K; k0 += G * U) {
-    typename Elem<T>::vec w[U][2];
-    float u[U][MR];
+  constexpr int U = MR > 4 ? 4 : 8;       // reduction indexes in flight
+  // several rows of x by way of LDS (loaded value by value beside W, eight took a third of
+  // the time: 1,024 to 4,096 bfloat16 21 us against 29; one row is faster without, 10.5, 11.5)
+  constexpr bool STAGE = MR > 1;
+  constexpr int KX = STAGE ? 8192 / MR : 1 << 30;
+  __shared__ float xs[MR][STAGE ? KX : 1];
+  for (int kc = kbegin; kc < K; kc = STAGE ? kc + KX : K) {
+    const int ke = STAGE ? imin(kc + KX, K) : K;
+    if constexpr (STAGE) {
+      if (kc != kbegin) __syncthreads();
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int k = k0 + j * G;
-      if (k < K) {
-        w[j][0] = ld_raw<T>(W + k * a.b.ld + col, n);
-        w[j][1] = ld_raw<T>(W + k * a.b.ld + a.cols + col, n);
-#pragma unroll
-        for (int m = 0; m < MR; ++m) u[j][m] = m < a.rows ? Elem<T>::one(x[m * a.a.ld + k]) : 0.0f;
-      }
+      for (int m = 0; m < MR; ++m)
+        for (int k = threadIdx.x; k < ke - kc; k += 512) xs[m][k] = m < a.rows ? Elem<T>::one(x[m * a.a.ld + kc + k]) : 0.0f;
+      __syncthreads();
     }
+    for (int k0 = kc + g; k0 < ke; k0 += G * U) {
+      typename Elem<T>::vec w[U][2];
+      T own[U];
 #pragma unroll
-    for (int j = 0; j < U; ++j)
-      if (k0 + j * G < K) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float t[V];
-          Elem<T>::get(w[j][h], t);
-#pragma unroll
-          for (int m = 0; m < MR; ++m)
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[h][m][i] = fmaf(u[j][m], t[i], v[h][m][i]);
+      for (int j = 0; j < U; ++j) {
+        const int k = k0 + j * G;
+        if (k < ke) {
+          if (!STAGE) own[j] = x[k];
+          w[j][0] = ld_raw<T>(W + k * a.b.ld + col, n);
+          w[j][1] = ld_raw<T>(W + k * a.b.ld + a.cols + col, n);
         }
       }
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+        if (k0 + j * G < ke) {
+          float u[MR];
+#pragma unroll
+          for (int m = 0; m < MR; ++m) u[m] = STAGE ? xs[m][k0 + j * G - kc] : Elem<T>::one(own[j]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float t[V];
+            Elem<T>::get(w[j][h], t);
+#pragma unroll
+            for (int m = 0; m < MR; ++m)
+#pragma unroll
+              for (int i = 0; i < V; ++i) v[h][m][i] = fmaf(u[m], t[i], v[h][m][i]);
+          }
+        }
+    }
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h)
@@ -467,6 +486,16 @@ __global__ __launch_bounds__(512) void k_gated_few(GatedArgs a) {
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < V; ++i) t[h][i] += s[q][h][g][cl * V + i];
+  if (a.part) {
+    if (g >= a.rows) return;
+    float* p = a.part + ((int64_t)blockIdx.y * a.rows + g) * 2 * a.cols + col;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < V; e += 4)
+        st_piece<float>(p + (int64_t)h * a.cols + e, n - e, reinterpret_cast<float(&)[4]>(t[h][e]));
+    return;
+  }
   GatedTail<T>(a, col).out(a, g, g < a.rows, col, t[0], t[1]);
 }
 
@@ -512,8 +541,20 @@ GatedWay gated_way(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   if (p || K <= kGatedThin) return GatedWay::panel;
   return dense_cut(t, M, 2 * N, K, kForward).splits > 1 ? GatedWay::split : GatedWay::tile;
 }
+// Splits of a long reduction where a few rows' columns leave most of the card idle (one
+// row of 4,096 to 1,024 bfloat16 13 us with eight, join included, 32 without; 1,024 to
+// 1,024 float32 7 either way).
+int gated_few_splits(int64_t K, int64_t N) {
+  const int64_t tiles = (N + 31) / 32;
+  return tiles > 64 || K < 2048 ? 1 : (int)std::min<int64_t>({256 / tiles, K / 256, 32});
+}
 size_t gated_fwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
-  if (M == 0 || gated_way(t, M, K, N) != GatedWay::split) return 0;
+  if (M == 0) return 0;
+  if (M <= kGatedFew) {
+    const int s = gated_few_splits(K, N);
+    return s > 1 ? up256((size_t)s * M * 2 * N * sizeof(float)) : 0;
+  }
+  if (gated_way(t, M, K, N) != GatedWay::split) return 0;
   return cut_bytes(dense_cut(t, M, 2 * N, K, kForward), M, 2 * N);
 }
 
@@ -575,6 +616,14 @@ e3_status gated_panel(GatedArgs a, hipStream_t st) {
 }
 
 template <class T>
+e3_status gated_join(const GatedArgs& a, const float* part, int splits, hipStream_t st) {
+  TimedLaunch t_("gated_fwd_join", st);
+  const int64_t per = (a.cols + kGroup - 1) / kGroup * (kGroup / Elem<T>::V);
+  hipLaunchKernelGGL(k_gated_join<T>, grid_of((a.rows * per + 255) / 256), dim3(256), 0, st, a, part, splits);
+  E3_HIP(hipGetLastError());
+  return E3_OK;
+}
+template <class T>
 e3_status gated_fwd(const GatedCall& c) {
   constexpr e3_dtype t = std::is_same_v<T, float> ? E3_F32 : E3_BF16;
   GatedArgs a{};
@@ -585,10 +634,16 @@ e3_status gated_fwd(const GatedCall& c) {
   a.nt = streams(t, c.M, c.N);
   switch (gated_way(t, c.M, c.K, c.N)) {
     case GatedWay::few: {
+      const int splits = gated_few_splits(c.K, c.N);
+      a.red_chunk = (int)((c.K + splits - 1) / splits);
+      a.part = splits > 1 ? reinterpret_cast<float*>(c.ws) : nullptr;
+      {
       TimedLaunch t_("gated_fwd_few", c.st);
       auto* k = c.M == 1 ? k_gated_few<T, 1> : c.M == 2 ? k_gated_few<T, 2> : c.M <= 4 ? k_gated_few<T, 4>
                                                                                    : k_gated_few<T, kGatedFew>;
-      hipLaunchKernelGGL(k, dim3((unsigned)((c.N + 31) / 32)), dim3(512), 0, c.st, a);
+      hipLaunchKernelGGL(k, dim3((unsigned)((c.N + 31) / 32), (unsigned)splits), dim3(512), 0, c.st, a);
+      }
+      if (splits > 1) return gated_join<T>(a, a.part, splits, c.st);
       break;
     }
     case GatedWay::panel: return gated_panel<T>(a, c.st);
@@ -602,10 +657,7 @@ e3_status gated_fwd(const GatedCall& c) {
       set_cut(d, cut, part);
       const e3_status s = dense_launch<J>(d, cut, {"gated_fwd_split_64", "gated_fwd_split_128", "gated_fwd_split_256"}, c.st);
       if (s != E3_OK) return s;
-      TimedLaunch t_("gated_fwd_join", c.st);
-      const int64_t per = (c.N + kGroup - 1) / kGroup * (kGroup / Elem<T>::V);
-      hipLaunchKernelGGL(k_gated_join<T>, grid_of((c.M * per + 255) / 256), dim3(256), 0, c.st, a, part, cut.splits);
-      break;
+      return gated_join<T>(a, part, cut.splits, c.st);
     }
     case GatedWay::tile: {
       const int b = dense_cut(t, c.M, 2 * c.N, c.K, kForward).tile;

@@ -62,7 +62,7 @@ def test_gated_refusals(L):
     assert bwd(M=0, dx=None, dW=None, db=None, x=None, dy=None, z=None, ws=None, nb=0) == OK
 
 
-@pytest.mark.parametrize("dtype,M,K,N", [(F32, 16, 1000, 250), (BF16, 16, 1000, 250), (F32, 300, 4100, 150)])
+@pytest.mark.parametrize("dtype,M,K,N", [(F32, 16, 1000, 250), (BF16, 16, 1000, 250), (F32, 300, 4100, 150), (BF16, 1, 4096, 100)])
 def test_gated_forward_scratch_refusals(L, dtype, M, K, N):
     """Sizes whose reduction is split: less scratch than asked for, none, or misaligned."""
     need = _gated_sizes(L, dtype, M, K, N)[0]

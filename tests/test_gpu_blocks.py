@@ -53,7 +53,8 @@ def names_of(e3, f):  # noqa: F811
 
 # ---------------------------------------------------------------- gated dense layers
 # M, K, N, gap, shift, and the kernel of the forward in float32 and in bfloat16
-GATED = [(1, 1, 1, 0, 0, "few", "few"), (1, 1024, 100, 0, 0, "few", "few"), (2, 33, 31, 1, 1, "few", "few"),
+GATED = [(1, 1, 1, 0, 0, "few", "few"), (1, 4100, 40, 0, 0, "few", "few"), (7, 9001, 65, 1, 1, "few", "few"), (3, 2048, 2050, 0, 0, "few", "few"),
+         (8, 2049, 3, 0, 0, "few", "few"), (8, 1500, 500, 4, 0, "few", "few"), (1, 1024, 100, 0, 0, "few", "few"), (2, 33, 31, 1, 1, "few", "few"),
          (3, 7, 64, 0, 0, "few", "few"), (8, 515, 129, 3, 0, "few", "few"), (5, 130, 8, 0, 3, "few", "few"),
          (9, 1, 1, 0, 0, "panel", "panel"), (300, 8, 33, 0, 0, "panel", "panel"), (1000, 16, 7, 5, 1, "panel", "panel"),
          (9, 17, 3, 0, 0, "64", "64"), (64, 64, 32, 0, 0, "64", "64"), (130, 100, 65, 2, 1, "64", "64"),
