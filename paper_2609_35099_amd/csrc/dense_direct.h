@@ -36,19 +36,19 @@ struct Feed {
       }
     }
   }
-  // The next step's loads.  In asm, so that the compiler, which cannot tell the buffers'
+  // A half of the next step's loads (0, then 1).  In asm, so that the compiler, which cannot tell the buffers'
   // loads apart across the loop, does not wait for all of them at the first read;
   // DirectTile waits.  Nothing is loaded to registers; m0 is set before each use, here and
   // by the compiler.
-  __device__ __forceinline__ void next(Lds& to) {
+  __device__ __forceinline__ void next(Lds& to, int half) {
     typedef __attribute__((address_space(3))) unsigned short* lds;
     const unsigned first = (unsigned)(uintptr_t)(lds)&to.v[0][at];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = half * N / 2; i < (half + 1) * N / 2; ++i)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(first + i * 1024), "v"(off[i]),
                    "s"(base)
                    : "memory");
-    base += step;
+    if (half) base += step;
   }
 };
 
@@ -57,13 +57,16 @@ struct Feed {
 // them passes through registers.  Whole pieces of 16 aligned bytes only
 // (direct_side), reductions in multiples of 64.  Sums run over the reduction in the
 // order of the other tiles: the same bits.
-// A product of 8,192 x 4,096 x 8,192 takes 465 us in a gated layer, 1.18 PFLOP/s (the
-// library's bare one 409); tiles of 256 x 128 by four waves, two to a CU, steps of 32
-// in three buffers 578; steps of 32 in four buffers 478; four waves of 128 x 128,
-// whose reads nothing hides, 643; the two waves of a SIMD in turns, one's products
-// beside the other's reads, 490; steps of 32 in five buffers with the next fragments
-// read beside the products 500.  16,384 x 1,024 by 4,096 columns of reduction takes 132
-// (91): its products alone, without loads, 105, its loads alone 74.
+// The loads are issued in two halves behind the first reads of LDS, which they would
+// hold up: 16,384 x 1,024 by 4,096 columns of reduction takes 135 us so, 144 with all
+// of them first, 150 with all of them behind the first reads (the library 95).
+// Other tiles, measured with the loads first: a product of 8,192 x 4,096 x 8,192 in a
+// gated layer took 465 us (the library's bare one 409); tiles of 256 x 128 by four
+// waves, two to a CU, steps of 32 in three buffers 578; steps of 32 in four buffers
+// 478; four waves of 128 x 128 643, and 540 with the next fragments read beside the
+// products; the two waves of a SIMD in turns, one's products beside the other's reads,
+// 490; steps of 32 in five buffers with the next fragments read beside the products
+// 500.  Of the 16,384 x 1,024 the products alone took 105 us, the loads alone 74.
 template <Form FA, Form FB>
 struct DirectTile {
   static constexpr int BM = 256, BN = 256, BK = 64, WM = 2, WN = 4, THREADS = WM * WN * kWave;
@@ -80,7 +83,9 @@ struct DirectTile {
   // Where the wave's part of the tile begins.
   static __device__ __forceinline__ int row0() { return uniform(threadIdx.x / kWave) / WN * (32 * RM); }
   static __device__ __forceinline__ int col0() { return uniform(threadIdx.x / kWave) % WN * (32 * RN); }
-  __device__ __forceinline__ void multiply(const Buf& s) {
+  // between(i): after the reads of the i-th 16 indexes, before their products
+  template <class Fn>
+  __device__ __forceinline__ void multiply(const Buf& s, Fn&& between) {
 #pragma unroll
     for (int k = 0; k < BK; k += 16) {
       bf8v x[RM], y[RN];
@@ -88,6 +93,7 @@ struct DirectTile {
       for (int j = 0; j < RN; ++j) y[j] = s.b.frag(0, col0() + 32 * j, k);
 #pragma unroll
       for (int i = 0; i < RM; ++i) x[i] = s.a.frag(0, row0() + 32 * i, k);
+      between(k / 16);
 #pragma unroll
       for (int i = 0; i < RM; ++i)
 #pragma unroll
@@ -107,13 +113,14 @@ struct DirectTile {
     A fa(sa, r0, rows, k0);
     B fb(sb, c0, cols, k0);
     const int n = (int)((end - k0) / BK);
-    fa.next(s0.a), fb.next(s0.b);
+    for (int h = 0; h < 2; ++h) fa.next(s0.a, h), fb.next(s0.b, h);
     // past the barrier every wave's loads are there, and every wave is done with the
     // buffer that is filled next
     auto step = [&](int s, Buf& now, Buf& next) {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (s + 1 < n) fa.next(next.a), fb.next(next.b);
-      multiply(now);
+      multiply(now, [&](int i) {
+        if (i < 2 && s + 1 < n) fa.next(next.a, i), fb.next(next.b, i);
+      });
     };
     for (int s = 0; s < n; s += 2) {
       step(s, s0, s1);
