@@ -14,7 +14,7 @@ import numpy as np
 import pytest
 
 from gpu_util import rel_l2
-from oracle import blocks as ob
+from oracle import blocks as ob, layers as ol
 from test_gpu_layers import dev, e3, host, near_steps, out_like, packed, rounded  # noqa: F401 (e3: a fixture)
 
 pytestmark = pytest.mark.gpu
@@ -130,14 +130,63 @@ def test_gated_backward(e3, dt, M, K, N, gap, shift, f32, bf16, ckpt):  # noqa: 
             assert torch.equal(alone[i], got[i]) and all(v is None for j, v in enumerate(alone) if j != i)
 
 
+@pytest.mark.parametrize("act,res,bias,keep", [("none", False, False, ()), ("gelu", False, True, ("z8",)),
+                                               ("silu", True, True, ("z", "y8")), ("relu", True, False, ())])
+def test_dense_forward_direct(e3, act, res, bias, keep):  # noqa: F811
+    """Wide bfloat16 products whose operands go straight to LDS have the bits of those by way of registers,
+    which rows of x at odd strides take; rows and columns end inside a tile."""
+    import torch
+    M, K, N = 16003, 1536, 1000
+    g = torch.Generator(device="cuda").manual_seed(17)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    x, W = normal(M, K), (normal(K, N) / K ** 0.5)
+    r, b = (normal(M, N) if res else None), (normal(N) if bias else None)
+    odd = torch.zeros(M, K + 3, device="cuda").bfloat16()
+    odd[:, :K] = x
+    assert names_of(e3, lambda: e3.dense_fwd(x, W, b, r, act, keep)) == {"dense_fwd_256"}
+    one, two = (e3.dense_fwd(v, W, b, r, act, keep) for v in (x, odd[:, :K]))
+    pairs = zip(one, two) if keep else [(one, two)]
+    for u, v in pairs:
+        for p, q in ([(u.q, v.q), (u.c, v.c)] if isinstance(u, e3.Packed8) else [(u, v)]):
+            assert torch.equal(p, q)
+    rows = torch.tensor([0, 1, 255, 256, 8191, M - 20, M - 1], device="cuda")
+    z = host(x[rows]) @ host(W) + (host(b) if bias else 0.0)
+    y = ol.act(act, z)[0] + (host(r[rows]) if res else 0.0)
+    close((one[0] if keep else one)[rows], y, "bfloat16")
+
+
+@pytest.mark.parametrize("M,K,N", [(16384, 1000, 2048), (8000, 1992, 2112)])
+def test_dense_backward_direct(e3, M, K, N):  # noqa: F811
+    """The same of dW (x at odd strides), and dx against the definition; the reduction of dW split."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(M)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    x, W, dy, z = normal(M, K), normal(K, N) / K ** 0.5, normal(M, N), normal(M, N)
+    odd = torch.zeros(M, K + 3, device="cuda").bfloat16()
+    odd[:, :K] = x
+    assert {"dense_dz", "dense_bwd_dx_256", "dense_bwd_dw_256"} <= names_of(e3, lambda: e3.dense_bwd(x, W, dy, z, act="silu"))
+    one, two = (e3.dense_bwd(v, W, dy, z, act="silu")[:3] for v in (x, odd[:, :K]))
+    for u, v in zip(one, two):
+        assert torch.equal(u, v)
+    zz = host(z)
+    dz = host(torch.from_numpy(host(dy) * ol.act("silu", zz)[1]).float().bfloat16())
+    rows = [0, 1, 255, 256, M - 20, M - 1]
+    close(one[0][rows], dz[rows] @ host(W).T, "bfloat16")
+    cols = [0, 1, 255, 256, N - 1]
+    close(one[1][:, cols], host(x).T @ dz[:, cols], "bfloat16")
+
+
 # M, K, N and the kernel, past the sizes above: tiles and row walks
 LARGE = [("float32", 262149, 64, 64, 0, "walk"), ("float32", 140000, 32, 128, 0, "walk"), ("float32", 131111, 32, 64, 8, "walk"),
          ("float32", 90001, 64, 192, 0, "walk"), ("float32", 140001, 64, 72, 0, "panel"), ("bfloat16", 262149, 64, 64, 0, "panel"),
          ("float32", 262149, 64, 16, 0, "panel"), ("float32", 131077, 33, 40, 3, "panel"), ("float32", 300007, 8, 64, 0, "panel"),
          ("bfloat16", 262149, 128, 16, 0, "panel"), ("bfloat16", 262176, 64, 32, 0, "panel"), ("bfloat16", 150001, 90, 33, 1, "panel"),
          ("float32", 16403, 100, 300, 0, "128"), ("float32", 4096, 1100, 257, 1, "split_128"), ("bfloat16", 40003, 130, 129, 0, "128"),
-         ("bfloat16", 16400, 300, 800, 0, "256"), ("bfloat16", 16400, 320, 800, 0, "direct"), ("bfloat16", 33000, 64, 328, 8, "panel"),
-         ("bfloat16", 16387, 192, 1000, 8, "direct"), ("bfloat16", 16400, 320, 804, 0, "256"), ("bfloat16", 16400, 320, 800, 4, "256"), ("bfloat16", 16001, 515, 1021, 6, "256")]
+         ("bfloat16", 16400, 300, 800, 0, "256"), ("bfloat16", 16400, 320, 800, 0, "256"), ("bfloat16", 16400, 576, 800, 0, "direct"),
+         ("bfloat16", 33000, 64, 328, 8, "panel"),
+         ("bfloat16", 16387, 192, 1000, 8, "256"), ("bfloat16", 16387, 512, 1000, 8, "direct"), 
+         ("bfloat16", 16400, 576, 804, 0, "256"), ("bfloat16", 16400, 576, 800, 4, "256"),
+         ("bfloat16", 16400, 320, 804, 0, "256"), ("bfloat16", 16400, 320, 800, 4, "256"), ("bfloat16", 16001, 515, 1021, 6, "256")]
 
 
 @pytest.mark.parametrize("dt,M,K,N,gap,name", LARGE)
