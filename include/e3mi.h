@@ -509,9 +509,10 @@ e3_status e3_residual_norm_fwd(e3_dtype dtype, e3_norm norm, unsigned where, con
  * there), the forward's h, s (with N2), gate, dropout and statistics: dr (s's whole
  * cotangent, r's), dh, dgate (shape of gate; a vector's sums over the rows), and the
  * gradients of the norms' weights, [cols].  Each may be NULL.  h may be NULL without
- * N1 and dgate.  Sums over rows go through ws (at least
- * e3_residual_norm_workspace_size bytes; not needed without them) in a fixed order;
- * they are zero for rows = 0. */
+ * N1 and dgate.  dr and dh may each be ds, dy, s or h itself, and a matrix dgate the
+ * gate (same ld); outputs may not overlap inputs or each other in any other way.
+ * Sums over rows go through ws (at least e3_residual_norm_workspace_size bytes; not
+ * needed without them) in a fixed order; they are zero for rows = 0. */
 e3_status e3_residual_norm_workspace_size(e3_dtype dtype, int64_t rows, int64_t cols, size_t* bwd_bytes);
 e3_status e3_residual_norm_bwd(e3_dtype dtype, e3_norm norm, unsigned where, const void* h, int64_t ldh, const void* s,
                                int64_t lds, const void* gate, int64_t ldg, float scale, double p, uint64_t seed,

@@ -566,8 +566,12 @@ __global__ __launch_bounds__(512) void k_res_bwd_wide(ResArgs a) {
   for (int col = lane * V; col < cols; col += L * V) {
     const int n = cols - col;
     wide_total<T, LAYER>(a, row, col, n, c, x, dy, d);
-    if (a.dr) st_piece<T>(static_cast<T*>(a.dr) + row * a.lddr + col, n, d, a.nt);
+    float total[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) total[i] = d[i];
     wide_first<T, LAYER>(a, drop, row, col, n, g1, h, d, t);
+    // (an output may lie where an input does: all of the piece has been read)
+    if (a.dr) st_piece<T>(static_cast<T*>(a.dr) + row * a.lddr + col, n, total, a.nt);
     if (a.dgate && a.ldg) st_piece<T>(static_cast<T*>(a.dgate) + row * a.lddg + col, n, t, a.nt);
     if (!a.dh) continue;
     if (a.post)
@@ -719,6 +723,19 @@ bool res_bwd_wide(e3_dtype t, int cols) {
   return t == E3_F32 ? res_shape<float, true>(cols, of) : res_shape<__bf16, true>(cols, of);
 }
 
+// Whether the spans of a backward's outputs and inputs meet.
+bool inputs_written(const ResArgs& a, size_t e) {
+  struct Span {
+    const void* p;
+    int64_t ld;
+  };
+  auto end = [&](const Span& s) { return reinterpret_cast<uintptr_t>(s.p) + ((a.rows - 1) * s.ld + a.cols) * e; };
+  for (const Span& o : {Span{a.dr, a.lddr}, Span{a.dh, a.lddh}, Span{a.ldg ? a.dgate : nullptr, a.lddg}})
+    for (const Span& i : {Span{a.ds, a.ldd}, Span{a.dy, a.ldy}, Span{a.s_in, a.lds}, Span{a.h, a.ldh}, Span{a.gate, a.ldg}})
+      if (o.p && i.p && reinterpret_cast<uintptr_t>(o.p) < end(i) && reinterpret_cast<uintptr_t>(i.p) < end(o)) return true;
+  return false;
+}
+
 template <class T>
 e3_status res_fwd(const ResArgs& a, bool layer, hipStream_t st) {
   return res_shape<T, false>(a.cols, [&](auto L, auto J) -> e3_status {
@@ -751,12 +768,22 @@ e3_status res_bwd(const ResArgs& a, bool layer, hipStream_t st) {
       hipLaunchKernelGGL(k, dim3(a.blocks), dim3(kResThreads<l>), 0, st, a);
       E3_HIP(hipGetLastError());
     } else {
-      {
+      auto over_rows = [&](const ResArgs& of) {
         TimedLaunch t_("residual_norm_bwd_wide", st);
         auto* k = layer ? k_res_bwd_wide<T, true> : k_res_bwd_wide<T, false>;
-        hipLaunchKernelGGL(k, grid_of(a.rows), dim3(512), 0, st, a);
-        E3_HIP(hipGetLastError());
+        hipLaunchKernelGGL(k, grid_of(of.rows), dim3(512), 0, st, of);
+      };
+      // The sums read the inputs again: where outputs may lie on these, a pass for the
+      // means alone (two more reads) lets the sums come first.
+      const bool sums_first = a.part && inputs_written(a, sizeof(T));
+      if (!sums_first) {
+        over_rows(a);
+      } else if (a.pre) {
+        ResArgs means = a;
+        means.dr = means.dh = means.dgate = nullptr;
+        over_rows(means);
       }
+      E3_HIP(hipGetLastError());
       if (a.part) {
         TimedLaunch t_("residual_norm_bwd_cols", st);
         const int per = 256 * Elem<T>::V;
@@ -764,6 +791,8 @@ e3_status res_bwd(const ResArgs& a, bool layer, hipStream_t st) {
         hipLaunchKernelGGL(k, dim3(a.blocks, (a.cols + per - 1) / per), dim3(256), 0, st, a);
         E3_HIP(hipGetLastError());
       }
+      if (sums_first) over_rows(a);
+      E3_HIP(hipGetLastError());
     }
     return E3_OK;
   });

@@ -1246,7 +1246,8 @@ def residual_norm_bwd(h, s, stats, dy=None, ds=None, gate=None, scale: float = 1
     """(dres, dh, dgate, dpost, dpre) from the cotangents dy of y and ds of s (None: 0; with pre, dy is needed)
     and the forward's h, s (needed with pre), statistics and arguments.  dpost and dpre are pairs (dgamma, dbeta);
     what was not there (a gate, a norm, a weight that was None) or is not in `want` is None.  h is needed for
-    the norm after the block and for dgate."""
+    the norm after the block and for dgate.  dres and dh are written where they are given; each may be ds, dy, s
+    or h itself (the same rows), but not the other."""
     ref = dy if dy is not None else ds
     if ref is None:
         raise ValueError("dy or ds must be given")

@@ -1,0 +1,58 @@
+"""How the gated layers, dropout and the residual norms are called: outputs in the memory of inputs, and the kernels
+that sizes and alignments choose."""
+import numpy as np
+import pytest
+
+from oracle import blocks as ob
+from test_gpu_blocks import DTS, _host_pair, _pair, _residual_inputs, close
+from test_gpu_layers import dev, e3, host  # noqa: F401 (e3: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- outputs in the memory of inputs
+# (float32 rows stay in registers up to 6,144 columns, bfloat16 rows up to 8,192)
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("cols", [24, 64, 515, 6144, 6147, 20000])
+@pytest.mark.parametrize("norm,after,before,gate", [("rms", True, True, "row"), ("layer", True, True, "full"),
+                                                   ("layer", True, False, "row"), ("rms", False, True, "row")])
+def test_residual_norm_backward_in_place(e3, dt, cols, norm, after, before, gate):  # noqa: F811
+    """Gradients written where a cotangent, h or s was are those written apart, and so are the sums over rows."""
+    import torch
+    h, r, g, post, pre, ds, dy = _residual_inputs(33, cols, norm, after, before, gate, True)
+    hd, rd, gd, dsd, dyd = (dev(v, dt) for v in (h, r, g, ds, dy))
+    post, pre = _pair(post, dt, 0), _pair(pre, dt, 0)
+    drop, f = e3.Dropout(0.2, 3), ob.factors(33, cols, 0.2, 3)
+    out = e3.residual_norm_fwd(hd, rd, gd, 0.5, norm, post, pre, 1e-5, drop, keep=("stats",))
+    s, st = out[0], out[-1]
+
+    def run(dres=None, dh=None, **at):
+        a = {k: v if k not in at else at[k] for k, v in (("h", hd), ("s", s), ("dy", dyd if before else None), ("ds", dsd))}
+        got = e3.residual_norm_bwd(a["h"], a["s"], st, a["dy"], a["ds"], gd, 0.5, norm, post, pre, drop, dres=dres, dh=dh)
+        return [v for o in got for v in (o if isinstance(o, tuple) else (o,)) if v is not None]
+    want = run()
+    count, stats = 1 + (norm == "layer"), list(host(st))
+    firsts = tuple(stats[:count]) if after else None
+    lasts = tuple(stats[-count:]) if before else None
+    firsts, lasts = (v if v is None or count == 2 else (None, v[0]) for v in (firsts, lasts))
+    ref = ob.residual_norm_bwd(host(hd), host(s), firsts, lasts, host(dyd) if before else None, host(dsd), host(gd), 0.5,
+                               norm, _host_pair(post), _host_pair(pre), f)
+    there = [True, True, True, *(v is not None for w in (post, pre) if w for v in w)]
+    ref = [v for o in ref if o is not None for v in (o if isinstance(o, tuple) else (o,))]
+    ref = [v for v, t in zip(ref, there, strict=True) if t]
+    assert len(ref) == len(want)
+    for got, v in zip(want, ref):
+        close(got, v, dt)
+    places = {"ds": dsd, "h": hd, **({"dy": dyd, "s": s} if before else {})}
+    for a in places:
+        for b in places:
+            print("[case] in place", dt, cols, norm, after, before, gate, a, b, flush=True)
+            here = {k: v.clone() for k, v in places.items()}
+            pairs = [(here[a], None), (None, here[a])] if a == b else [(here[a], here[b])]
+            for dres, dh in pairs:
+                for k, v in places.items():
+                    here[k].copy_(v)
+                got = run(dres, dh, **here)
+                assert len(got) == len(want)
+                for u, v in zip(got, want):
+                    assert torch.equal(u, v), (a, b)
