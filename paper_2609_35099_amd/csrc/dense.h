@@ -463,7 +463,7 @@ __global__ __launch_bounds__(256, 2) void k_dense_panel(DenseArgs a) {
 template <class J, int BK, int WPB>
 __global__ __launch_bounds__(WPB* kWave, 2) void k_dense_shared(DenseArgs a) {
   using T = typename J::T;
-  using LA = Loader<T, kAlong, 32, BK, WPB * kWave, J::KA>;
+  using LA = Loader<T, kAlong, 32, BK, WPB * kWave, J::KA, false>;
   constexpr int NC = 2, KK = BK / 16, P = LA::P;
   static_assert(J::FA == kAlong && J::KA != kPacked && J::KB == kFull && !J::SUM);
   __shared__ __align__(16) typename LA::Lds in[2];

@@ -9,7 +9,7 @@ namespace {
 template <Form F, int R, int BK, int WAVES>
 struct Feed {
   static constexpr int N = R * BK * 2 / 1024 / WAVES;  // instructions of a wave and step
-  using Lds = Plane<F, R, BK, 1>;
+  using Lds = Plane<F, R, BK, 1, true>;
   const char* base;  // of the next step
   int64_t step;      // bytes
   unsigned off[N];   // of the lane's pieces

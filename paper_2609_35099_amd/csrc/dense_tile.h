@@ -60,16 +60,23 @@ struct Side {
 
 // LDS planes of R rows (or columns) by BK reduction indexes.  16-byte slots are
 // exchanged so that the lanes of one pass of a read cover all banks: along, by
-// the row's number among those that share the banks; across, the four slots of each of
-// the four rows that half a wave's transposing read takes.
-template <Form F, int R, int BK, int P>
+// the row's number among those that share the banks; across, the pairs of slots of the
+// four rows that one transposing read takes, or (FOURS) the four slots of each of the four
+// rows that half a wave's read takes.  The forwards' tiles and the direct ones have FOURS:
+// float32 16,384 x 1,024 x 1,024 219 us against 223, bfloat16 16,387 x 515 x 1,021 49 against
+// 50.  dW's largest tiles lack the registers for it: with an operand formed on the way they
+// spilled 136 for 9, the backward of 60,003 x 192 x 2,048 with silu 978 us against 328.
+template <Form F, int R, int BK, int P, bool FOURS>
 struct Plane {
   static constexpr int W = F == kAlong ? BK : R;          // values of an LDS row
   static constexpr int S = W / 8;                         // slots of one
   static constexpr int kShare = F == kAlong ? (S >= 16 ? 1 : 16 / S) : 1;  // rows over all banks
   unsigned short v[P][R * BK];
   static __device__ __forceinline__ int off(int row, int slot) {
-    const int x = F == kAlong ? (row / kShare) & (S - 1 < 15 ? S - 1 : 15) : S >= 16 ? 4 * (row & 3) : 4 * (row / 2 & 1);
+    const int x = F == kAlong ? (row / kShare) & (S - 1 < 15 ? S - 1 : 15)
+                  : !FOURS    ? (2 * (row & 3)) & (S - 1)
+                  : S >= 16   ? 4 * (row & 3)
+                              : 4 * (row / 2 & 1);
     return row * W + ((slot ^ x) * 8);
   }
   // The fragment of rows (columns) r0 + l % 32 at reduction indexes k0 + 8 (l / 32) on.
@@ -192,13 +199,13 @@ struct Fetch {
 enum Kind { kFull, kPacked, kGradFull, kGradPacked };
 
 // One operand's way from memory to LDS.
-template <class T, Form F, int R, int BK, int THREADS, Kind KD>
+template <class T, Form F, int R, int BK, int THREADS, Kind KD, bool FOURS>
 struct Loader {
   static constexpr int V = Elem<T>::V;
   static constexpr bool Q = KD == kPacked, G = KD >= kGradFull;
   static_assert(F != kPaired || KD == kFull);
   static constexpr int P = sizeof(T) == 2 || Q ? 1 : 3;   // planes
-  using Lds = Plane<F, R, BK, P>;
+  using Lds = Plane<F, R, BK, P, FOURS>;
   using Main = Fetch<T, F, R, BK, THREADS, Q>;
   using Pre = Fetch<T, F, R, BK, THREADS, KD == kGradPacked>;
   static constexpr int N = Main::N;
@@ -265,8 +272,9 @@ struct Loader {
 template <class T, Form FA, Form FB, int BM, int BN, int BK, int WM, int WN, Kind KA, Kind KB, bool SUM, int BUFS>
 struct Tile {
   static constexpr int THREADS = WM * WN * kWave, TM = BM / WM, TN = BN / WN, RM = TM / 32, RN = TN / 32;
-  using LA = Loader<T, FA, BM, BK, THREADS, KA>;
-  using LB = Loader<T, FB, BN, BK, THREADS, KB>;
+  static constexpr bool FOURS = FA == kAlong && FB != kAlong;  // a forward's (Plane)
+  using LA = Loader<T, FA, BM, BK, THREADS, KA, FOURS>;
+  using LB = Loader<T, FB, BN, BK, THREADS, KB, FOURS>;
   union Shared {
     struct {
       typename LA::Lds a;
