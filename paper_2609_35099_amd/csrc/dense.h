@@ -765,11 +765,13 @@ e3_status dense_launch(const DenseArgs& a, const Cut& c, const Names& names, hip
   // (packed gradient operands never get there: forms_dz; dW takes such tiles past
   // 128 columns of dz and 1e8 values of it)
   if constexpr (sizeof(typename J::T) == 2 && J::KA == kFull && J::KB == kFull && !J::SUM) {
-    // A forward's short reduction is faster by two workgroups per CU, one's results stored
-    // beside the other's products: 16,384 x K x 8,192, us: K = 512 232 direct, 208 by
-    // those, 1,024 349 and 332, 1,536 435 and 451, 2,048 530 and 598, 8,192 x 4,096 x 8,192
-    // 465 and 561.
-    constexpr int64_t least = J::FA == kAlong && J::FB == kAcross ? 1536 : 0;
+    // Short reductions are faster by the tiles whose workgroups run two to a CU or whose
+    // steps are shorter.  Direct and those, us: forward 16,384 x K x 8,192 K = 512 232 and
+    // 208, 1,024 349 and 332, 1,536 435 and 451, 2,048 530 and 598, 8,192 x 4,096 x 8,192 465
+    // and 561; dx of 65,536 x 512 columns from 512 59 and 49, 1,024 83 and 79, 1,536 107 and
+    // 111, 2,048 132 and 152; dW 4,096 x 4,096 from 512 rows 32 and 26, 1,024 45 and 41, 2,048
+    // 70 and 71, 4,096 123 and 132.
+    constexpr int64_t least = 1536;
     if (c.tile == 256 && a.red >= least && a.red % 64 == 0 && direct_side(a.a, J::FA == kAlong ? 8 : a.rows) &&
         direct_side(a.b, J::FB == kAlong ? 8 : a.cols)) {
       using Tl = DirectTile<J::FA, J::FB>;

@@ -56,3 +56,55 @@ def test_residual_norm_backward_in_place(e3, dt, cols, norm, after, before, gate
                 assert len(got) == len(want)
                 for u, v in zip(got, want):
                     assert torch.equal(u, v), (a, b)
+
+
+# ---------------------------------------------------------------- which kernels run
+def launched(f):
+    """The (mangled) names of the kernels that f launches."""
+    import torch
+    from torch.profiler import ProfilerActivity, profile
+    f()
+    torch.cuda.synchronize()
+    with profile(activities=[ProfilerActivity.CUDA]) as p:
+        f()
+        torch.cuda.synchronize()
+    names = {e.name for e in p.events() if e.device_type == torch.autograd.DeviceType.CUDA}
+    assert names
+    return names
+
+
+def direct(f):
+    """Whether f's dense products read their operands straight to LDS."""
+    names = launched(f)
+    some = {"k_dense_direct" in n for n in names if "k_dense" in n and "join" not in n and "k_dense_dz" not in n}
+    assert len(some) == 1, names
+    return some.pop()
+
+
+def bf16(seed, *shape, gap=0):
+    """Normal values; gap: elements between a row's end and the next one's start."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    v = torch.randn(*shape, generator=g, device="cuda").bfloat16()
+    if not gap:
+        return v
+    wide = torch.zeros(shape[0], shape[1] + gap, dtype=v.dtype, device="cuda")
+    wide[:, :shape[1]] = v
+    return wide[:, :shape[1]]
+
+
+@pytest.mark.parametrize("M,N,red,want", [(16384, 1024, 512, False), (65536, 512, 512, False), (65536, 512, 1024, False),
+                                          (16384, 2048, 1536, True), (65536, 512, 2048, True)])
+def test_dx_goes_direct_from_long_reductions_only(e3, M, N, red, want):  # noqa: F811
+    """(Short ones are up to a fifth faster the other way.)  M x N values of dx from `red` columns of dy."""
+    W, dy = bf16(1, N, red), bf16(2, M, red)
+    assert direct(lambda: e3.dense_bwd(None, W, dy, want=("dx",))) == want
+    assert not direct(lambda: e3.dense_bwd(None, W, bf16(2, M, red, gap=1), want=("dx",)))
+
+
+@pytest.mark.parametrize("K,N,M,want", [(4096, 4096, 512, False), (4096, 4096, 1024, False), (2048, 8192, 1024, False),
+                                        (4096, 4096, 2048, True), (1024, 4096, 16384, True)])
+def test_dw_goes_direct_from_many_rows_only(e3, K, N, M, want):  # noqa: F811
+    x, W, dy = bf16(1, M, K), bf16(2, K, N), bf16(3, M, N)
+    assert direct(lambda: e3.dense_bwd(x, W, dy, want=("dW",))) == want
+    assert not direct(lambda: e3.dense_bwd(bf16(1, M, K, gap=1), W, dy, want=("dW",)))
