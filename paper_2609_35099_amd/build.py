@@ -94,8 +94,8 @@ def build(verbose: bool = True, extra=None) -> str:
     objdir = os.path.join(BUILD, "obj")
     os.makedirs(objdir, exist_ok=True)
     sources = [os.path.join(CSRC, "e3mi.hip"), os.path.join(CSRC, "convr.hip"),
-               *(os.path.join(CSRC, f) for f in ("dense.hip", "dense_bwd_f32.hip", "dense_bwd_bf16.hip", "gated.hip",
-                                              "gated_f32.hip", "gated_bf16.hip", "gated_bwd_f32.hip",
+               *(os.path.join(CSRC, f) for f in ("dense.hip", "dense_direct.hip", "dense_bwd_f32.hip", "dense_bwd_bf16.hip",
+                                              "gated.hip", "gated_f32.hip", "gated_bf16.hip", "gated_bwd_f32.hip",
                                               "gated_bwd_bf16.hip", "norm.hip", "residual.hip")),
                os.path.join(CSRC, "builder.cpp")] + \
               [os.path.join(GEN, u) for u in units]

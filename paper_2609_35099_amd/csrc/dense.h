@@ -18,8 +18,6 @@ struct DenseBwdCall {
 e3_status dense_bwd_f32(const DenseBwdCall& c);
 e3_status dense_bwd_bf16(const DenseBwdCall& c);
 
-namespace {
-
 struct DenseArgs {
   Side a, b, pre;  // rows of A by columns of B over the reduction; the z of one that is a gradient
   int grad_act;
@@ -39,6 +37,13 @@ struct DenseArgs {
   int act;
   bool nt;  // y (and z) streams
 };
+// bfloat16 products with operands straight to LDS, in a unit of their own
+// (dense_direct.hip): x W, dz W^T and x^T dz.
+e3_status dense_direct_fwd(const DenseArgs& a, hipStream_t st);
+e3_status dense_direct_dx(const DenseArgs& a, hipStream_t st);
+e3_status dense_direct_dw(const DenseArgs& a, hipStream_t st);
+
+namespace {
 
 // What follows the sums of one piece of a row, row0 + lr with row0 uniform (so
 // that a thread multiplies by a row stride once, not per piece).  The lanes of a
@@ -270,37 +275,6 @@ __global__ __launch_bounds__((TileOf<J, B>::THREADS), (TileOf<J, B>::OCC)) void 
   using Tl = typename TileOf<J, B>::type;
   __shared__ __align__(16) typename Tl::Shared sh;
   dense_block<J, Tl, TileOf<J, B>::BM, TileOf<J, B>::BN>(a, sh, block_id());
-}
-// bfloat16 with operands straight to LDS.
-template <class J>
-__global__ __launch_bounds__(512, 2) void k_dense_direct(DenseArgs a) {
-  using Tl = DirectTile<J::FA, J::FB>;
-  static_assert(sizeof(typename J::T) == 2 && J::KA == kFull && J::KB == kFull && !J::SUM);
-  __shared__ __align__(16) typename Tl::Buf s0, s1;
-  const int64_t tm = (a.rows + Tl::BM - 1) / Tl::BM;
-  const int tn = (a.cols + Tl::BN - 1) / Tl::BN;
-  int64_t u = block_id();
-  if (u >= tm * tn * a.splits) return;
-  const int split = (int)(u / (tm * tn));
-  u -= split * (tm * tn);
-  const TileAt at = tile_at(u, tm, tn);
-  const int64_t r0 = at.m * Tl::BM;
-  const int c0 = at.n * Tl::BN;
-  const int64_t k0 = split * a.chunk, end = k0 + a.chunk < a.red ? k0 + a.chunk : a.red;
-  // Without loads between its stores the end waits for none of them (a load's wait is
-  // one for every store before it).
-  const Tail<typename J::T> tail(a, c0 + Tl::col0() + Rows32<typename J::T, Tl::RN>::col());
-  Tl t;
-  t.run(s0, s1, a.a, a.b, r0, a.rows, c0, a.cols, k0, end);
-  auto* out = Tl::stage(s0, s1);
-  auto store = [&](auto bare) {
-    each_of([&](auto i) {
-      rows32_out<J, Tl::RN, false, decltype(bare)::value>(a, tail, split, r0 + Tl::row0() + 32 * i, c0 + Tl::col0(), k0, end,
-                                                          out, t.acc[i]);
-    }, std::make_integer_sequence<int, Tl::RM>{});
-  };
-  if (a.res || a.part) store(std::false_type{});
-  else store(std::true_type{});
 }
 // Short reductions (up to 16 KK) over many rows: no LDS and no barriers before the
 // epilogue.  A wave keeps the terms of its 32 NC columns of B in registers for
@@ -774,11 +748,9 @@ e3_status dense_launch(const DenseArgs& a, const Cut& c, const Names& names, hip
     constexpr int64_t least = 1536;
     if (c.tile == 256 && a.red >= least && a.red % 64 == 0 && direct_side(a.a, J::FA == kAlong ? 8 : a.rows) &&
         direct_side(a.b, J::FB == kAlong ? 8 : a.cols)) {
-      using Tl = DirectTile<J::FA, J::FB>;
-      const int64_t tiles = (a.rows + Tl::BM - 1) / Tl::BM * ((a.cols + Tl::BN - 1) / Tl::BN);
-      hipLaunchKernelGGL(k_dense_direct<J>, grid_of(tiles * c.splits), dim3(Tl::THREADS), 0, st, a);
-      E3_HIP(hipGetLastError());
-      return E3_OK;
+      if constexpr (J::FA == kAcross) return dense_direct_dw(a, st);
+      else if constexpr (J::FB == kAlong) return dense_direct_dx(a, st);
+      else return dense_direct_fwd(a, st);
     }
   }
   if constexpr (sizeof(typename J::T) == 2 && J::KA != kGradPacked && J::KB != kGradPacked) {

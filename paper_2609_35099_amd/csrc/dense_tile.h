@@ -25,6 +25,16 @@
 #pragma once
 #include "layers.h"
 
+// One operand of a tile product, or the pre-activation beside it.
+struct Side {
+  const void* p;      // full: memory rows (kAlong: of an output index, kAcross: of a reduction index) at p + i ld
+  int64_t ld;
+  const int8_t* q;    // packed (p null): ld values and ldc exponents a row
+  const uint8_t* c;
+  int64_t ldc;
+  int64_t total;      // values from the first to the last, at least a piece
+};
+
 namespace {
 
 typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
@@ -47,16 +57,6 @@ __device__ __forceinline__ unsigned term2(float& a, float& b) {
   a -= __uint_as_float(t << 16), b -= __uint_as_float(t & 0xffff0000u);
   return t;
 }
-
-// One operand of a tile product, or the pre-activation beside it.
-struct Side {
-  const void* p;      // full: memory rows (kAlong: of an output index, kAcross: of a reduction index) at p + i ld
-  int64_t ld;
-  const int8_t* q;    // packed (p null): ld values and ldc exponents a row
-  const uint8_t* c;
-  int64_t ldc;
-  int64_t total;      // values from the first to the last, at least a piece
-};
 
 // LDS planes of R rows (or columns) by BK reduction indexes.  16-byte slots are
 // exchanged so that the lanes of one pass of a read cover all banks: along, by

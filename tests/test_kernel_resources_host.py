@@ -11,7 +11,7 @@ msgpack = pytest.importorskip("msgpack")
 
 @pytest.fixture(scope="module")
 def kernels():
-    """{mangled name: its metadata} of every kernel of the invariant layers."""
+    """{mangled name: its metadata and "object", where its code object lies in the library} of every kernel."""
     e3mi.lib()
     data = open(e3mi.LIB_PATH, "rb").read()
     out, at = {}, 0
@@ -29,7 +29,7 @@ def kernels():
                     name = p + 12 + (n + 3) // 4 * 4
                     if note == 32:
                         meta = msgpack.unpackb(data[name:name + d], strict_map_key=False)
-                        out.update({k[".name"]: k for k in meta["amdhsa.kernels"]})
+                        out.update({k[".name"]: {**k, "object": at} for k in meta["amdhsa.kernels"]})
                     p = name + (d + 3) // 4 * 4
         at += 4
     return out
@@ -47,3 +47,10 @@ def test_the_largest_dense_tiles_keep_their_registers(kernels):
     assert len(tiles) >= 8
     spills = {n: k[".vgpr_spill_count"] for n, k in tiles.items() if k[".vgpr_spill_count"]}
     assert all(v <= 28 for v in spills.values()), spills
+
+
+def test_the_direct_tiles_lie_apart(kernels):
+    """In front of the register kernels their code moved those to where they took up to an eighth longer."""
+    direct = {k["object"] for n, k in kernels.items() if "k_dense_direct" in n}
+    others = {k["object"] for n, k in kernels.items() if "k_dense_two" in n or "k_dense_panel" in n}
+    assert len(direct) == 1 and len(others) >= 3 and not direct & others
