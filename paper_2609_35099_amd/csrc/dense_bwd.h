@@ -207,7 +207,7 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
                       : dense_bwd_products<T, kd, kFull, f>(ax, aw, part, st);
   };
   using Full = std::integral_constant<Kind, kFull>;
-  if (!fly) return run(Full{}, std::false_type{});
+  if (!fly || (act == E3_ACT_NONE && !db)) return run(Full{}, std::false_type{});  // nothing to form or to sum
   if (act == E3_ACT_NONE) return run(Full{}, std::true_type{});
   return z.x ? run(std::integral_constant<Kind, kGradFull>{}, std::true_type{})
              : run(std::integral_constant<Kind, kGradPacked>{}, std::true_type{});

@@ -1,6 +1,7 @@
 """How the gated layers, dropout and the residual norms are called: outputs in the memory of inputs, and the kernels
 that sizes and alignments choose."""
-import numpy as np
+import re
+
 import pytest
 
 from oracle import blocks as ob
@@ -60,7 +61,7 @@ def test_residual_norm_backward_in_place(e3, dt, cols, norm, after, before, gate
 
 # ---------------------------------------------------------------- which kernels run
 def launched(f):
-    """The (mangled) names of the kernels that f launches."""
+    """The names of the kernels that f launches, mangled where a type's name is unknown to the profiler (bfloat16)."""
     import torch
     from torch.profiler import ProfilerActivity, profile
     f()
@@ -108,3 +109,36 @@ def test_dw_goes_direct_from_many_rows_only(e3, K, N, M, want):  # noqa: F811
     x, W, dy = bf16(1, M, K), bf16(2, K, N), bf16(3, M, N)
     assert direct(lambda: e3.dense_bwd(x, W, dy, want=("dW",))) == want
     assert not direct(lambda: e3.dense_bwd(bf16(1, M, K, gap=1), W, dy, want=("dW",)))
+
+
+def sums_columns(names):
+    """Whether one of the products sums the columns of its second operand (the last argument of its Job)."""
+    return any(re.search(r"3JobI\w*?ELb1EE|Job<[^<>]*, true>", n) for n in names)
+
+
+@pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("M,K,N,gap", [(3000, 128, 150, 0), (700, 40, 200, 3), (20011, 256, 96, 0), (65536, 256, 1024, 0)])
+def test_products_from_a_finished_dz_sum_nothing(e3, dt, M, K, N, gap):  # noqa: F811
+    """The gated backward has summed db when its products run, and a plain layer's without db has nothing to sum: dW
+    does not form column sums for nobody, and has the bits it has beside them."""
+    import torch
+    x, W, dy, z = (v.to(getattr(torch, dt)) for v in (bf16(1, M, K, gap=gap), bf16(2, K, 2 * N) / K ** 0.5,
+                                                      bf16(3, M, N, gap=gap), bf16(4, M, 2 * N)))
+    names = launched(lambda: e3.gated_bwd(x, W, dy, z))
+    assert any("k_gated_dz" in n for n in names) and not sums_columns(names), names
+    if M == 65536 and dt == "bfloat16":
+        assert sum("k_dense_direct" in n for n in names) == 2, names          # dx and dW
+    dx, dW, db = e3.gated_bwd(x, W, dy, z)
+    pick = torch.tensor([0, 1, M // 2, M - 1]).cuda()
+    dz = ob.gated_dz(host(dy), host(z))
+    dzr = host(torch.from_numpy(dz).to(getattr(torch, dt))) if dt == "bfloat16" else dz
+    close(dx[pick], dzr[pick.cpu().numpy()] @ host(W).T, dt)
+    cols = slice(0, 2 * N, max(1, N // 8))
+    close(dW[:, cols], host(x).T @ dzr[:, cols], dt)
+    close(db, dz.sum(0), dt)
+
+    d = z                              # any cotangent of a plain layer [K, 2 N]
+    assert sums_columns(launched(lambda: e3.dense_bwd(x, W, d)))
+    assert not sums_columns(launched(lambda: e3.dense_bwd(x, W, d, want=("dx", "dW"))))
+    for a, b in zip(e3.dense_bwd(x, W, d)[:2], e3.dense_bwd(x, W, d, want=("dx", "dW"))[:2]):
+        assert torch.equal(a, b)
