@@ -14,6 +14,7 @@ struct DenseBwdCall {
   int64_t ldx, ldz, lddy, lddx, M, K, N;
   int act;
   hipStream_t st;
+  bool given;  // dy is a finished dz, db is not wanted: ws has no room for either
 };
 e3_status dense_bwd_f32(const DenseBwdCall& c);
 e3_status dense_bwd_bf16(const DenseBwdCall& c);
@@ -706,10 +707,10 @@ struct DenseBwdWs {
   size_t dz, db, part, total;
   int64_t db_blocks, db_rows;
 };
-DenseBwdWs dense_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
+DenseBwdWs dense_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N, bool given = false) {
   const size_t e = t == E3_F32 ? 4 : 2;
   DenseBwdWs w{};
-  if (!forms_dz(t, M, K, N, true)) {  // from z in full or packed
+  if (!given && !forms_dz(t, M, K, N, true)) {  // from z in full or packed
     w.db_blocks = std::max<int64_t>(1, std::min<int64_t>(512, (M + 63) / 64));
     w.db_rows = (M + w.db_blocks - 1) / w.db_blocks;
     w.dz = up256(M * N * e);

@@ -152,7 +152,7 @@ e3_status dense_bwd_products(DenseArgs x, DenseArgs w, float* part, hipStream_t 
 
 template <class T>
 e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, int64_t lddy, T* dx, int64_t lddx, T* dW,
-                    T* db, char* ws, int64_t M, int64_t K, int64_t N, hipStream_t st) {
+                    T* db, char* ws, int64_t M, int64_t K, int64_t N, hipStream_t st, bool given) {
   constexpr e3_dtype t = std::is_same_v<T, float> ? E3_F32 : E3_BF16;
   constexpr int V = Elem<T>::V;
   // x or dy shorter than a piece; a short W (copied to a whole piece below) where its
@@ -167,8 +167,8 @@ e3_status dense_bwd(RowsIn<T> x, const T* W, RowsIn<T> z, int act, const T* dy, 
     E3_HIP(hipGetLastError());
     return E3_OK;
   }
-  const DenseBwdWs w = dense_bwd_ws(t, M, K, N);
-  const bool fly = forms_dz(t, M, K, N, act != E3_ACT_NONE && z.q);
+  const DenseBwdWs w = dense_bwd_ws(t, M, K, N, given);
+  const bool fly = !given && forms_dz(t, M, K, N, act != E3_ACT_NONE && z.q);
   T* dz = reinterpret_cast<T*>(ws);
   float* dbp = reinterpret_cast<float*>(ws + w.dz);
   float* part = reinterpret_cast<float*>(ws + w.dz + w.db);
@@ -218,7 +218,7 @@ e3_status dense_bwd_call(const DenseBwdCall& c) {
   return dense_bwd<T>({static_cast<const T*>(c.x), c.ldx, c.xq, c.xc}, static_cast<const T*>(c.W),
                       {static_cast<const T*>(c.z), c.ldz, c.zq, c.zc}, c.act, static_cast<const T*>(c.dy), c.lddy,
                       static_cast<T*>(c.dx), c.lddx, static_cast<T*>(c.dW), static_cast<T*>(c.db), c.ws, c.M, c.K, c.N,
-                      c.st);
+                      c.st, c.given);
 }
 
 }  // namespace

@@ -75,7 +75,7 @@ GatedBwdWs gated_bwd_ws(e3_dtype t, int64_t M, int64_t K, int64_t N) {
   w.rows = (M + w.blocks - 1) / w.blocks;
   w.dz = up256((size_t)M * 2 * N * (t == E3_F32 ? 4 : 2));
   w.db = up256((size_t)w.blocks * 2 * N * 4);
-  w.products = dense_bwd_ws(t, M, K, 2 * N).total;
+  w.products = dense_bwd_ws(t, M, K, 2 * N, true).total;
   w.total = w.dz + w.db + w.products;
   if (gated_fused(M, K, N))  // from z in full or packed
     w.total = std::max(w.total, up256((size_t)gated_fused_groups(t, M, N) * (K * 2 * N + 2 * N) * 4));
@@ -106,7 +106,7 @@ e3_status gated_bwd(const GatedCall& c) {
   }
   if (!products) return E3_OK;
   const DenseBwdCall d{c.dtype, c.x,   c.W,     nullptr, dz,     c.xq,   nullptr, c.xc, nullptr, c.dx, c.dW,        nullptr,
-                       c.ws + w.dz + w.db, c.ldx, 0, 2 * c.N, c.lddx, c.M, c.K, 2 * c.N, E3_ACT_NONE, c.st};
+                       c.ws + w.dz + w.db, c.ldx, 0, 2 * c.N, c.lddx, c.M, c.K, 2 * c.N, E3_ACT_NONE, c.st, true};
   return t == E3_F32 ? dense_bwd_f32(d) : dense_bwd_bf16(d);
 }
 
