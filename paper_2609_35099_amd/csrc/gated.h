@@ -318,11 +318,10 @@ __global__ __launch_bounds__(256, 2) void k_gated_panel(GatedArgs a) {
 // once for NG groups of 32 columns of y instead of once for each.  Against the kernel
 // above, us: 156,000 x 64 x 64 24 and 30, 624,000 70 and 92, 1,248,000 x 32 x 128 194 and
 // 223; bfloat16, which has no terms to form, 17 and 14, 42 and 37.
-template <class T, int KK, int NG, bool NT>
+template <int KK, int NG, bool NT>
 __global__ __launch_bounds__(512, 2) void k_gated_walk(GatedArgs a) {
-  using R = Rows32<T, 2>;
-  constexpr bool f32 = sizeof(T) == 4;
-  constexpr int V = Elem<T>::V, P = f32 ? 3 : 1, Q = 8 / V, WAVES = 8;
+  using R = Rows32<float, 2>;
+  constexpr int V = Elem<float>::V, P = 3, Q = 8 / V, WAVES = 8;
   __shared__ __align__(16) bf8v wf[NG][KK][2][P][kWave];
   __shared__ __align__(16) float out[WAVES][32][R::PITCH];
   const int l = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), h = 8 * (l / 32);
@@ -331,10 +330,8 @@ __global__ __launch_bounds__(512, 2) void k_gated_walk(GatedArgs a) {
     const int c = f % 2, k = f / 2 % KK, g = f / 2 / KK;
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = Elem<T>::one(static_cast<const T*>(a.b.p)[(16 * k + h + e) * a.b.ld + c * a.cols + col0 + 32 * g + l % 32]);
-      if (f32) v[e] *= kTermScale;
-    }
+    for (int e = 0; e < 8; ++e)
+      v[e] = static_cast<const float*>(a.b.p)[(16 * k + h + e) * a.b.ld + c * a.cols + col0 + 32 * g + l % 32] * kTermScale;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       u4v t;
@@ -344,8 +341,8 @@ __global__ __launch_bounds__(512, 2) void k_gated_walk(GatedArgs a) {
     }
   }
   __syncthreads();
-  typename Elem<T>::vec x[KK][Q];
-  const T* xp = static_cast<const T*>(a.a.p);
+  Elem<float>::vec x[KK][Q];
+  const float* xp = static_cast<const float*>(a.a.p);
   auto load = [&](auto fast, int64_t block) {
     constexpr bool F = decltype(fast)::value;
     const int last = F ? 31 : (int)(a.rows - block * 32) - 1;
@@ -353,27 +350,23 @@ __global__ __launch_bounds__(512, 2) void k_gated_walk(GatedArgs a) {
 #pragma unroll
     for (int k = 0; k < KK; ++k)
 #pragma unroll
-      for (int q = 0; q < Q; ++q) x[k][q] = ld_raw<T>(xp + block * 32 * a.a.ld + (m * a.a.ld + 16 * k + h + q * V), V);
+      for (int q = 0; q < Q; ++q) x[k][q] = ld_raw<float>(xp + block * 32 * a.a.ld + (m * a.a.ld + 16 * k + h + q * V), V);
   };
   bf8v xf[P][KK];
   auto terms = [&]() {
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
-      if constexpr (!f32) {
-        xf[0][k] = __builtin_bit_cast(bf8v, x[k][0]);
-      } else {
-        float v[8];
+      float v[8];
 #pragma unroll
-        for (int q = 0; q < Q; ++q) Elem<T>::get(x[k][q], reinterpret_cast<float(&)[V]>(v[q * V]));
+      for (int q = 0; q < Q; ++q) Elem<float>::get(x[k][q], reinterpret_cast<float(&)[V]>(v[q * V]));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= kTermScale;
+      for (int e = 0; e < 8; ++e) v[e] *= kTermScale;
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          u4v t;
+      for (int p = 0; p < P; ++p) {
+        u4v t;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) t[e] = term2(v[2 * e], v[2 * e + 1]);
-          xf[p][k] = __builtin_bit_cast(bf8v, t);
-        }
+        for (int e = 0; e < 4; ++e) t[e] = term2(v[2 * e], v[2 * e + 1]);
+        xf[p][k] = __builtin_bit_cast(bf8v, t);
       }
     }
   };
@@ -393,7 +386,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_walk(GatedArgs a) {
 #pragma unroll
           for (int p = 0; p < P; ++p) y[c][p] = wf[g][k][c][p][l];
 #pragma unroll
-        for (int s = 2 * P - 2 < 2 ? 2 * P - 2 : 2; s >= 0; --s)
+        for (int s = 2; s >= 0; --s)
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             const int q = s - p;
@@ -402,7 +395,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_walk(GatedArgs a) {
             for (int c = 0; c < 2; ++c) acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[c][q], xf[p][k], acc[c], 0, 0, 0);
           }
       }
-      gated_rows32<T, 2, decltype(fast)::value, NT>(a, block * 32, col0 + 32 * g, out[wave], acc);
+      gated_rows32<float, 2, decltype(fast)::value, NT>(a, block * 32, col0 + 32 * g, out[wave], acc);
     }
   };
   const int64_t blocks = a.rows / 32, stride = (int64_t)gridDim.x * WAVES;
@@ -593,7 +586,7 @@ e3_status gated_walk(const GatedArgs& a, hipStream_t st) {
   TimedLaunch t_("gated_fwd_walk", st);
   const unsigned tiles = (unsigned)(a.cols / (32 * NG));  // of columns; a workgroup per CU among them
   const int64_t rows = std::min<int64_t>((a.rows + 255) / 256, std::max<int64_t>(1, 256 / tiles));
-  auto* k = a.nt ? k_gated_walk<float, KK, NG, true> : k_gated_walk<float, KK, NG, false>;
+  auto* k = a.nt ? k_gated_walk<KK, NG, true> : k_gated_walk<KK, NG, false>;
   hipLaunchKernelGGL(k, dim3((unsigned)rows, tiles), dim3(512), 0, st, a);
   E3_HIP(hipGetLastError());
   return E3_OK;
