@@ -175,8 +175,10 @@ __global__ __launch_bounds__((GatedTileOf<T, B>::THREADS), (GatedTileOf<T, B>::O
   t.finish(sh, [&](int r, int c, auto out, auto& acc) { gated_rows32<T, Tl::RN>(a, r0 + r, c0 + c / 2, out, acc); });
 }
 
-// bfloat16 with operands straight to LDS.
+// bfloat16 with operands straight to LDS.  (A template, so that only its unit compiles it.)
+template <class T>
 __global__ __launch_bounds__(512, 2) void k_gated_direct(GatedArgs a) {
+  static_assert(sizeof(T) == 2);
   using Tl = DirectTile<kAlong, kPaired>;
   __shared__ __align__(16) Tl::Buf s0, s1;
   const int64_t tm = (a.rows + Tl::BM - 1) / Tl::BM, u = block_id();
@@ -186,12 +188,12 @@ __global__ __launch_bounds__(512, 2) void k_gated_direct(GatedArgs a) {
   const int64_t r0 = at.m * Tl::BM;
   const int c0 = at.n * (Tl::BN / 2);
   // (loaded here, so that no wait for a load is one for stores)
-  const GatedTail<__bf16> tail(a, c0 + Tl::col0() / 2 + gated_col<__bf16, Tl::RN>());
+  const GatedTail<T> tail(a, c0 + Tl::col0() / 2 + gated_col<T, Tl::RN>());
   Tl t;
   t.run(s0, s1, a.a, a.b, r0, a.rows, c0, a.cols, 0, a.red);
   auto* out = Tl::stage(s0, s1);
   each_of([&](auto i) {
-    gated_rows32<__bf16, Tl::RN>(a, tail, r0 + Tl::row0() + 32 * i, c0 + Tl::col0() / 2, out, t.acc[i]);
+    gated_rows32<T, Tl::RN>(a, tail, r0 + Tl::row0() + 32 * i, c0 + Tl::col0() / 2, out, t.acc[i]);
   }, std::make_integer_sequence<int, Tl::RM>{});
 }
 
@@ -675,7 +677,7 @@ e3_status gated_fwd(const GatedCall& c) {
           using Tl = DirectTile<kAlong, kPaired>;
           TimedLaunch t_("gated_fwd_direct", c.st);
           const int64_t tiles = (c.M + Tl::BM - 1) / Tl::BM * ((c.N + Tl::BN / 2 - 1) / (Tl::BN / 2));
-          hipLaunchKernelGGL(k_gated_direct, grid_of(tiles), dim3(Tl::THREADS), 0, c.st, a);
+          hipLaunchKernelGGL(k_gated_direct<T>, grid_of(tiles), dim3(Tl::THREADS), 0, c.st, a);
           break;
         }
       }

@@ -5,7 +5,7 @@ import re
 import pytest
 
 from oracle import blocks as ob
-from test_gpu_blocks import DTS, _host_pair, _pair, _residual_inputs, close
+from test_gpu_blocks import DTS, _host_pair, _pair, _residual_inputs, close, names_of
 from test_gpu_layers import dev, e3, host  # noqa: F401 (e3: a fixture)
 
 pytestmark = pytest.mark.gpu
@@ -142,3 +142,45 @@ def test_products_from_a_finished_dz_sum_nothing(e3, dt, M, K, N, gap):  # noqa:
     assert not sums_columns(launched(lambda: e3.dense_bwd(x, W, d, want=("dx", "dW"))))
     for a, b in zip(e3.dense_bwd(x, W, d)[:2], e3.dense_bwd(x, W, d, want=("dx", "dW"))[:2]):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("M,K,N", [(16384, 1600, 2048), (16384, 2048, 2056)])
+def test_dense_products_straight_to_lds_have_the_same_bits(e3, M, K, N):  # noqa: F811
+    """Whole aligned rows take the direct tiles and rows at odd strides the register ones, to the same sums."""
+    import torch
+    x, W, dy, b = bf16(1, M, K), bf16(2, K, N) / K ** 0.5, bf16(3, M, N), bf16(4, N)
+    xo, dyo = bf16(1, M, K, gap=1), bf16(3, M, N, gap=1)
+    calls = [(lambda x, dy: e3.dense_fwd(x, W, b, act="gelu"), True), (lambda x, dy: e3.dense_bwd(x, W, dy, want=("dW",))[1], True),
+             (lambda x, dy: e3.dense_bwd(None, W, dy, want=("dx",))[0], N % 64 == 0)]
+    for call, want in calls:
+        print("[case] dense direct", M, K, N, want, flush=True)
+        assert direct(lambda: call(x, dy)) == want and not direct(lambda: call(xo, dyo))
+        assert torch.equal(call(x, dy), call(xo, dyo))
+    rows, cols = torch.tensor([0, 255, 256, M - 1]).cuda(), slice(0, N, N // 7)
+    close(calls[1][0](x, dy)[:, cols], host(x).T @ host(dy[:, cols]), "bfloat16")
+    close(calls[2][0](x, dy)[rows], host(dy[rows]) @ host(W).T, "bfloat16")
+
+
+# what is launched for whole aligned rows, for rows at odd strides, and whether the former's product is direct
+@pytest.mark.parametrize("M,K,N,one,two", [
+    (16387, 576, 1000, {"gated_fwd_direct"}, {"gated_fwd_256"}), (8200, 1088, 2056, {"gated_fwd_direct"}, {"gated_fwd_256"}),
+    (2048, 4096, 2048, {"gated_fwd_split_256", "gated_fwd_join"}, {"gated_fwd_split_256", "gated_fwd_join"}),
+    (2000, 4160, 2040, {"gated_fwd_split_256", "gated_fwd_join"}, {"gated_fwd_split_256", "gated_fwd_join"})])
+def test_gated_products_straight_to_lds_have_the_same_bits(e3, M, K, N, one, two):  # noqa: F811
+    import torch
+    x, xo, W, b = bf16(1, M, K), bf16(1, M, K, gap=1), bf16(2, K, 2 * N) / K ** 0.5, bf16(3, 2 * N)
+    print("[case] gated direct", M, K, N, flush=True)
+    assert names_of(e3, lambda: e3.gated_fwd(x, W, b)) == one and names_of(e3, lambda: e3.gated_fwd(xo, W, b)) == two
+    for v, fast in ((x, True), (xo, False)):
+        names = launched(lambda: e3.gated_fwd(v, W, b))
+        assert any("k_gated_direct" in n or "k_dense_direct" in n for n in names) == fast, names
+    got, other = (e3.gated_fwd(v, W, b, keep=("z", "z8", "y8")) for v in (x, xo))
+    for u, v in zip(got, other):
+        for p, q in zip(u if isinstance(u, tuple) else (u,), v if isinstance(v, tuple) else (v,)):
+            for r, s in ((p.q, q.q), (p.c, q.c)) if isinstance(p, e3.Packed8) else ((p, q),):
+                assert torch.equal(r, s)
+    assert torch.equal(e3.gated_fwd(x, W, b), got[0])
+    rows = torch.tensor([0, 255, 256, M - 1]).cuda()
+    y, z = ob.gated_fwd(host(x[rows]), host(W), host(b))
+    close(got[0][rows], y, "bfloat16")
+    close(got[1][rows], z, "bfloat16")

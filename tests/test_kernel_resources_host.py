@@ -11,7 +11,7 @@ msgpack = pytest.importorskip("msgpack")
 
 @pytest.fixture(scope="module")
 def kernels():
-    """{mangled name: its metadata and "object", where its code object lies in the library} of every kernel."""
+    """{mangled name: its metadata and "objects", where its code objects lie in the library} of every kernel."""
     e3mi.lib()
     data = open(e3mi.LIB_PATH, "rb").read()
     out, at = {}, 0
@@ -29,7 +29,8 @@ def kernels():
                     name = p + 12 + (n + 3) // 4 * 4
                     if note == 32:
                         meta = msgpack.unpackb(data[name:name + d], strict_map_key=False)
-                        out.update({k[".name"]: {**k, "object": at} for k in meta["amdhsa.kernels"]})
+                        for k in meta["amdhsa.kernels"]:
+                            out.setdefault(k[".name"], {**k, "objects": set()})["objects"].add(at)
                     p = name + (d + 3) // 4 * 4
         at += 4
     return out
@@ -51,6 +52,16 @@ def test_the_largest_dense_tiles_keep_their_registers(kernels):
 
 def test_the_direct_tiles_lie_apart(kernels):
     """In front of the register kernels their code moved those to where they took up to an eighth longer."""
-    direct = {k["object"] for n, k in kernels.items() if "k_dense_direct" in n}
-    others = {k["object"] for n, k in kernels.items() if "k_dense_two" in n or "k_dense_panel" in n}
+    direct, others = set(), set()
+    for n, k in kernels.items():
+        direct |= k["objects"] if "k_dense_direct" in n else set()
+        others |= k["objects"] if "k_dense_two" in n or "k_dense_panel" in n else set()
     assert len(direct) == 1 and len(others) >= 3 and not direct & others
+
+
+@pytest.mark.parametrize("name", ["k_gated_direct", "k_gated_walk", "k_gated_few", "k_gated_panel", "k_gated_join",
+                                  "k_gated_bwd", "k_gated_dz", "k_res_", "k_dropout"])
+def test_a_kernel_is_compiled_where_it_is_launched(kernels, name):
+    """Once, by the unit that launches it, and not by every one that reads its header."""
+    copies = {n: len(k["objects"]) for n, k in kernels.items() if name in n}
+    assert copies and all(v == 1 for v in copies.values()), copies
