@@ -62,10 +62,11 @@ __device__ __forceinline__ unsigned term2(float& a, float& b) {
 // exchanged so that the lanes of one pass of a read cover all banks: along, by
 // the row's number among those that share the banks; across, the pairs of slots of the
 // four rows that one transposing read takes, or (FOURS) the four slots of each of the four
-// rows that half a wave's read takes.  The forwards' tiles and the direct ones have FOURS:
-// float32 16,384 x 1,024 x 1,024 219 us against 223, bfloat16 16,387 x 515 x 1,021 49 against
-// 50.  dW's largest tiles lack the registers for it: with an operand formed on the way they
-// spilled 136 for 9, the backward of 60,003 x 192 x 2,048 with silu 978 us against 328.
+// rows that half a wave's read takes.  FOURS is faster: float32 forward 16,384 x 1,024 x
+// 1,024 219 us against 223, a gated backward of 16,384 x 1,024 x 2,048 1,728 against 1,775,
+// bfloat16 forward 16,387 x 515 x 1,021 49 against 50.  But bfloat16 dW's largest tiles lack
+// the registers for it: with an operand formed on the way they spilled 136 for 9, the
+// backward of 60,003 x 192 x 2,048 with silu 978 us against 328.
 template <Form F, int R, int BK, int P, bool FOURS>
 struct Plane {
   static constexpr int W = F == kAlong ? BK : R;          // values of an LDS row
@@ -272,7 +273,7 @@ struct Loader {
 template <class T, Form FA, Form FB, int BM, int BN, int BK, int WM, int WN, Kind KA, Kind KB, bool SUM, int BUFS>
 struct Tile {
   static constexpr int THREADS = WM * WN * kWave, TM = BM / WM, TN = BN / WN, RM = TM / 32, RN = TN / 32;
-  static constexpr bool FOURS = FA == kAlong && FB != kAlong;  // a forward's (Plane)
+  static constexpr bool FOURS = sizeof(T) == 4 || FA == kAlong;  // all but bfloat16 dW (Plane)
   using LA = Loader<T, FA, BM, BK, THREADS, KA, FOURS>;
   using LB = Loader<T, FB, BN, BK, THREADS, KB, FOURS>;
   union Shared {
