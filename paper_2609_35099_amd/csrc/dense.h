@@ -198,9 +198,10 @@ __device__ __forceinline__ void rows32_out(const DenseArgs& a, int split, int64_
 }
 
 // Tiles by type and size, with us per call in turn with the other side.
-//   bfloat16, 256 x 256 (where DirectTile cannot read the operands): 16 waves of 64 x
-//     64, steps of 32, two buffers, one workgroup per CU: 16,384 x 1,024 x 4,096 dx 142, dW 149 (the library's products
-//     100, 166).  The forward takes 256 x 128 by 8 waves, two workgroups per CU, so
+//   bfloat16, 256 x 256 (where DirectTile cannot read the operands, or the reduction is
+//     short): 16 waves of 64 x 64, steps of 32, two buffers, one workgroup per CU:
+//     16,384 x 1,024 x 4,096 dx 142, dW 149 (the library's products 100, 166).  The
+//     forward takes 256 x 128 by 8 waves, two workgroups per CU, so
 //     that one's activations run beside the other's product: 164 for the bare product
 //     (155 with 256 x 256, the library's 132), but with gelu 185 (187), and a training
 //     step with z in 8 bits 656 (670).

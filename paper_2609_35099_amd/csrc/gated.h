@@ -5,8 +5,9 @@
 //
 // Forward: a tile takes the columns of both halves in turns of 32 (kPaired), so
 // that the two of a pair meet in one wave's staging and neither g nor u goes to
-// memory unless it is kept.  Backward: dz is written once, by the pass that sums db,
-// and the products are those of a dense layer of 2 N columns.
+// memory unless it is kept.  Backward: narrow layers form dz block by block in LDS, in
+// one pass over the rows (gated_bwd.h); otherwise it is written once, by the pass that sums
+// db, and the products are those of a dense layer of 2 N columns.
 #pragma once
 #include "dense.h"
 
@@ -319,7 +320,11 @@ __global__ __launch_bounds__(256, 2) void k_gated_panel(GatedArgs a) {
 // workgroup's waves, and each forms a row block's terms, a third of the vector work,
 // once for NG groups of 32 columns of y instead of once for each.  Against the kernel
 // above, us: 156,000 x 64 x 64 24 and 30, 624,000 70 and 92, 1,248,000 x 32 x 128 194 and
-// 223; bfloat16, which has no terms to form, 17 and 14, 42 and 37.
+// 223; bfloat16, which has no terms to form, 17 and 14, 42 and 37 (float32 alone has it).
+// A CU holds one workgroup, by its 116 KB of LDS: two waves a SIMD, whose loads, terms,
+// products and stores follow each other.  Of a SIMD's busy cycles at 156,000 x 64 x 64 vector
+// instructions take 49% (920 for 32 rows, 280 of them for the terms of x, most of the others
+// for the epilogue) and matrix instructions 38%.
 template <int KK, int NG, bool NT>
 __global__ __launch_bounds__(512, 2) void k_gated_walk(GatedArgs a) {
   using R = Rows32<float, 2>;
@@ -579,7 +584,10 @@ int gated_fused_groups(e3_dtype t, int64_t M, int64_t N) {
   return (int)std::min<int64_t>((M + rows - 1) / rows, 256);
 }
 
-// Whether k_gated_walk takes it: whole steps and groups of columns.
+// Whether k_gated_walk takes it: whole steps and groups of columns, and y alone.  (With z,
+// as a training step has it, k_gated_panel runs with branches around its stores: 156,000 x
+// 64 x 64 float32 38 us, its bytes at a copy's rate 31, bfloat16 19 and 16; 624,000 127 and
+// 125, 65 and 63.)
 bool gated_walks(const GatedArgs& a) {
   return a.rows >= 32 && GatedTail<float>::plain(a) && (a.red == 32 || a.red == 64) && a.cols % 64 == 0;
 }

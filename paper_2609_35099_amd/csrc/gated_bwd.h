@@ -10,7 +10,8 @@
 // terms of W in registers for good, dW's into registers that stay for all blocks; what
 // is left is to add the workgroups' dW and db in order.  The next block's rows are in
 // flight meanwhile.  100,003 x 64 x 128 float32 71 us and 9 for the sums, with dz
-// written and two products 123; its bytes, once, at a copy's rate are 40.  bfloat16 45.
+// written and two products 123; its bytes, once, at a copy's rate are 40.  bfloat16 49 in all
+// of 20, 156,000 x 64 x 64 39 of 20 (float32 56 of 39).
 // A round of a block is bound by its steps behind each other (loads, dz, terms to LDS,
 // products, barriers): 16 waves, or two buffers of LDS with waves that form the one
 // while others multiply the other, were no faster.
@@ -388,7 +389,7 @@ template <class T, int KB, int NB>
 e3_status gated_bwd_fused_of(const FusedArgs<T>& a, int groups, hipStream_t st) {
   TimedLaunch t_("gated_bwd_fused", st);
   constexpr int V = Elem<T>::V;
-  constexpr int64_t near = 1 << 25;  // strides whose 32 rows stay in 31 bits
+  constexpr int64_t near = 1 << 25;  // strides whose 64 rows and two halves of z stay in 31 bits
   const bool packed = a.dw && !a.x.x;
   const bool fast = a.N % V == 0 && a.lddy < near && a.ldz < near && (!a.dw || packed || (a.K % V == 0 && a.x.ld < near));
   auto* k = packed ? (fast ? k_gated_bwd<T, KB, NB, true, true> : k_gated_bwd<T, KB, NB, true, false>)

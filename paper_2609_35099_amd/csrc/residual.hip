@@ -10,13 +10,21 @@
 //   dh = rstd1 (a1 - n1 mean(a1 n1) [- mean(a1)])
 //   dgamma2 = sum dy n2, dbeta2 = sum dy, dgamma1 = sum t gate n1, dbeta1 = sum t gate
 //
-// All of it is bound by memory (and the mask by its multiplications, of which half
-// as many fit beside a bfloat16 read and write): rows are read once, kept in
-// registers and written once.  bfloat16 65,536 x 1,024, rms: forward 103 us (5.2 TB/s),
-// backward 155 (the rate of a copy of its bytes), dropout of it 53 to 65; float32
-// 100,003 x 515 with layer norms and a gate by row and column, backward 345 (a copy 326).  N2 sees the float32 sum, not the s that is stored.
+// Rows are read once, kept in registers and written once.  From 32 float32 or 64 bfloat16
+// columns to the registers' end, whole pieces are bound by memory (and the mask by its
+// multiplications, of which half as many fit beside a bfloat16 read and write): bfloat16
+// 65,536 x 1,024, rms: forward 103 us (5.2 TB/s), backward 155 (the rate of a copy of its
+// bytes), dropout of it 53 to 65; float32 100,003 x 515 with layer norms and a gate by row
+// and column, backward 345 (a copy 326).  N2 sees the float32 sum, not the s that is stored.
 // L lanes share a row, J 16-byte pieces each; rows past the registers are read
 // again for each pass.
+// Not so bound, us and a copy of the bytes (rms, both norms, a row gate, dropout; forward,
+// backward): narrow rows, by rounds of latency, as eight lanes share a row at least and a CU
+// has 64 of them in the backward, 600,000 x 16 float32 38 of 30 and 72 of 45, bfloat16 46 of
+// 15 and 93 of 23, 1,000,000 x 8 55 of 25 and 107 of 38, 73 of 13 and 141 of 19; bfloat16 rows
+// of odd lengths, whose last pieces go value by value, 100,003 x 515 135 of 81 and 351 of 121;
+// rows past the registers, by reading them two to three times, 2,001 x 10,001 float32 87 of
+// 63 and 229 of 94, bfloat16 61 of 31 and 204 of 47.
 #include "drop.h"
 
 namespace {

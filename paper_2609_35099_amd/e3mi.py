@@ -1057,7 +1057,8 @@ def gated_fwd(x, W, bias=None, act: str = "silu", keep=(), out=None, ws=None, st
 @_on_stream
 def gated_bwd(x, W, dy, z, act: str = "silu", want=("dx", "dW", "db"), dx=None, ws=None, stream=None):
     """(dx, dW, db) of a gated dense layer from dy and the forward's x (a tensor or a Packed8) and z (a tensor
-    [M, 2 N], or the pair of "z8"); cotangents not in `want` are not computed (None).  x is needed for dW only."""
+    [M, 2 N], or the pair of "z8"); cotangents not in `want` are not computed (None).  x is needed for dW only.
+    In bfloat16 dz is rounded for the products of dx and dW, but for K <= 64 and N <= 128 from a tensor z."""
     code, dt = _layer_dtype(dy, "dy")
     M, N = shape = _matrix(dy, "dy")
     K = _matrix(W, "W")[0]
